@@ -28,6 +28,18 @@
  *   sparcml_validate_streams -- input check: indices strictly ascending
  *                             and in range (§5.1)
  *
+ * and, at both ends of that path, the losses that a gradient comes from and
+ * the update of Alg. 1 that the summed gradient goes into:
+ *
+ *   sparcml_token_logprob  -- log probability of given tokens
+ *   sparcml_policy_loss    -- clipped policy loss with a KL term, and its
+ *                             gradient
+ *   sparcml_preference_loss -- loss of paired log ratios, and its gradient
+ *   sparcml_tensors_prepare -- a model's tensors, laid out once for
+ *   sparcml_grad_norm      -- the norm of all gradients, a clipping factor
+ *   sparcml_adamw          -- one AdamW step over all tensors, moments in
+ *                             32 or in 8 bits
+ *
  * Conventions shared by every call:
  *   - All data pointers are DEVICE pointers (HBM of the current HIP device),
  *     except the descriptor arrays (sparcml_stream[], pointer tables), which
@@ -45,7 +57,8 @@
  *   - Return value: SPARCML_OK (0) or a negative status.  Argument errors
  *     are detected on the host before any device work is enqueued; on error
  *     the outputs are unspecified.  No exception crosses the ABI.
- *   - Values are finite fp32; NaN/Inf inputs give unspecified results.
+ *   - Values are finite fp32; NaN/Inf inputs give unspecified results, except
+ *     where a call says otherwise.
  */
 #ifndef SPARCML_H
 #define SPARCML_H
@@ -78,6 +91,15 @@ extern "C" {
 #define SPARCML_OP_QUANTIZE_BUCKETED 5
 #define SPARCML_OP_CONCAT 6
 #define SPARCML_OP_VALIDATE 7
+#define SPARCML_OP_TENSORS 8
+#define SPARCML_OP_LOGPROB 9
+#define SPARCML_OP_POLICY 10
+#define SPARCML_OP_PREFERENCE 11
+
+/* Element types of logits, gradients and weight copies. */
+#define SPARCML_F32 0
+#define SPARCML_BF16 1
+#define SPARCML_F16 2
 
 /*
  * Sparse stream (§5.1 "Vector Representations" and "Switching to a Dense
@@ -106,11 +128,13 @@ typedef struct sparcml_stream {
 /*
  * Workspace bytes needed by an operation.
  *   op       SPARCML_OP_*.
- *   P        number of ranks (streams / rows).
- *   N        dimension.
+ *   P        number of ranks (streams / rows); TENSORS: of tensors;
+ *            PREFERENCE: of pairs; LOGPROB, POLICY: 1.
+ *   N        dimension; TENSORS: elements of all tensors together; LOGPROB,
+ *            POLICY, PREFERENCE: rows of logits.
  *   max_nnz  TOPK: k; QUANTIZE: largest stream length; REDUCE: largest
- *            input stream nnz; DENSIFY, QUANTIZE_BUCKETED, CONCAT, VALIDATE:
- *            ignored.
+ *            input stream nnz; LOGPROB, POLICY, PREFERENCE: vocabulary;
+ *            DENSIFY, QUANTIZE_BUCKETED, CONCAT, VALIDATE, TENSORS: ignored.
  *   delta    REDUCE only (switch threshold as a fraction of N).
  * A workspace sized with max_nnz >= the actual largest nnz is sufficient.
  * Returns SPARCML_OK and *bytes, or SPARCML_EINVAL.
@@ -426,6 +450,211 @@ SPARCML_API int sparcml_split_bounds(int P, uint64_t N, uint64_t* bounds);
 SPARCML_API int sparcml_densify(const sparcml_stream* in, uint64_t N, float* dense, void* stream);
 
 /*
+ * A model's tensors for the update of Alg. 1 (the summed gradient applied to
+ * the weights), laid out once: their addresses, sizes and rates go to the
+ * workspace, where sparcml_grad_norm and sparcml_adamw read them on every
+ * step.  A program keeps the filled plan and the workspace as long as the
+ * addresses hold, and prepares again when one changes.
+ *   param    n fp32 weights.
+ *   grad     n gradient entries of grad_type.
+ *   m, v     state_bits == 32: n fp32 first and second moments.
+ *            state_bits == 8: n E4M3 codes (OCP: 4 exponent, 3 mantissa
+ *            bits) each, of the first moment and of the second moment's
+ *            root; all zero bytes and zero scales at the start of training.
+ *   m_scale, v_scale  state_bits == 8: a power of two per 256 consecutive
+ *            elements, ceil(n / 256) each.  A moment is code * scale.
+ *   copy     NULL, or n entries of copy_type that receive the new weights
+ *            rounded to nearest.
+ *   decay    weight decay; lr_scale: factor on the step's learning rate.
+ * Data pointers need no alignment beyond their element's.
+ */
+typedef struct sparcml_tensor {
+    float* param;
+    const void* grad;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* copy;
+    uint64_t n;
+    float decay;
+    float lr_scale;
+} sparcml_tensor;
+
+/* The plan of a model's tensors (HOST memory, filled by the library). */
+typedef struct sparcml_tensors {
+    void* ws;
+    uint64_t total;   /* elements of all tensors */
+    uint64_t chunks;  /* pieces of work */
+    uint32_t count;   /* tensors */
+    uint32_t grad_type;
+    uint32_t copy_type;
+    uint32_t state_bits;
+    uint64_t check;
+} sparcml_tensors;
+
+/*
+ *   count      1 <= count <= 65535 tensors, each of n <= 2^34 elements (the
+ *              Philox counter word below is 32 bits); n == 0 is allowed.
+ *   grad_type, copy_type  SPARCML_F32 / BF16 / F16 (copy_type: BF16 or F16,
+ *              read where a copy is not NULL).
+ *   state_bits 32, 8, or 0: gradients only (sparcml_grad_norm).
+ *   ws         sparcml_workspace_size(SPARCML_OP_TENSORS, count, total, ...)
+ *              bytes, kept with the plan.
+ * Does not synchronize; later calls on another stream have to come after it.
+ * Errors: EINVAL, EWORKSPACE, EHIP.
+ */
+SPARCML_API int sparcml_tensors_prepare(int count, const sparcml_tensor* tensors, int grad_type, int copy_type,
+                            int state_bits, sparcml_tensors* plan, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Norm of all gradients of a plan and the factor that clips them:
+ *   out[0] = grad_scale * sqrt(sum of squares over all tensors)
+ *   out[1] = min(1, max_norm / (out[0] + 1e-6)), or 0 if out[0] is not
+ *            finite (Inf or NaN among the gradients: the step that reads
+ *            the factor then changes nothing).
+ * Squares are summed in fp64 in a fixed order (the same bits on every call).
+ *   grad_scale > 0, finite; max_norm > 0 (INFINITY: no clipping).
+ *   out        device float[2].
+ * Uses the plan's workspace: calls on one plan must not overlap.
+ * Errors: EINVAL, EHIP.
+ */
+SPARCML_API int sparcml_grad_norm(const sparcml_tensors* plan, double grad_scale, double max_norm, float* out,
+                      void* stream);
+
+/*
+ * One AdamW step (decoupled weight decay) over all tensors of a plan, in one
+ * launch.  Element j of tensor t at step s, each operation rounded to fp32:
+ *   f  = grad_scale, or fl(grad_scale * clip[1])
+ *   g  = grad * f
+ *   m' = beta1 * m + (1 - beta1) * g
+ *   v' = beta2 * v + (1 - beta2) * (g * g)
+ *   p' = p * (1 - lr_t decay_t) - lr_t / (1 - beta1^s) *
+ *        (m' / (sqrt(v') / sqrt(1 - beta2^s) + eps)),   lr_t = lr * lr_scale_t
+ * (the factors in parentheses of scalars are formed in fp64 and rounded
+ * once).  With state_bits == 8 the new moments m' and r' = sqrt(v') of each
+ * 256 elements share the least power of two that brings their largest
+ * magnitude to at most 448 (never below 2^-100), and each is rounded to one
+ * of its two neighbouring codes, up with the probability that makes it
+ * unbiased: of the Philox4x32-10 word j&3 at counter (j >> 2, t, s, 0), key
+ * (seed & 0xffffffff, seed >> 32), the low 16 bits decide for m', the high
+ * ones for r'.  r' is held at the lowest code (2^-9) at least, so that no
+ * step divides by a root that rounding took to zero.
+ *   clip     NULL, or device float[2] as sparcml_grad_norm writes it.  With
+ *            clip[1] == 0 the call writes nothing.
+ *   lr >= 0, 0 <= beta < 1, eps > 0 (as fp32 too), step >= 1, all finite.
+ * In place; no host round trip; capturable in a HIP graph (which replays the
+ * captured step number).
+ * Errors: EINVAL (also for a plan with state_bits == 0), EHIP.
+ */
+typedef struct sparcml_adamw_args {
+    double lr, beta1, beta2, eps, grad_scale;
+    uint64_t seed;
+    uint32_t step;
+    uint32_t reserved; /* 0 */
+} sparcml_adamw_args;
+SPARCML_API int sparcml_adamw(const sparcml_tensors* plan, const sparcml_adamw_args* args, const float* clip,
+                  void* stream);
+
+/*
+ * Rows of logits with a token each.
+ *   x        device, element (t, v) at x[t * ld + v], of `type`
+ *            (SPARCML_F32 / BF16 / F16); no alignment beyond the element's.
+ *   rows, vocab, ld   rows >= 1, 1 <= vocab < 2^31, ld >= vocab,
+ *            rows < 2^31.
+ *   label    device int32[rows]; a label outside [0, vocab) marks a row
+ *            without a token.
+ *   scale    inverse temperature, > 0: the distribution of row t is the
+ *            softmax of scale * x[t].
+ * Logits may be -Inf (a token that cannot come).  A row that holds nothing
+ * but -Inf has lse -Inf, log probability -Inf and a zero gradient.  Rows
+ * without a token (or with weight 0) are not read: they may hold anything.
+ * Sums of exponentials are taken in fp32 over the differences to the row's
+ * maximum.
+ */
+typedef struct sparcml_logits {
+    const void* x;
+    const int32_t* label;
+    uint64_t rows, vocab, ld;
+    uint32_t type;
+    float scale;
+} sparcml_logits;
+
+/*
+ * Log probability of each row's token, the forward pass of both losses (and
+ * where their old and reference values come from):
+ *   lse[t]  = log sum_v exp(scale x[t][v])
+ *   logp[t] = scale x[t][label[t]] - lse[t]
+ * both 0 for a row without a token.  lse may be NULL.
+ *   ws       sparcml_workspace_size(SPARCML_OP_LOGPROB, 1, rows, vocab, ...)
+ * Does not synchronize.  Errors: EINVAL, EWORKSPACE, EHIP.
+ */
+SPARCML_API int sparcml_token_logprob(const sparcml_logits* in, float* logp, float* lse, void* ws,
+                          size_t ws_bytes, void* stream);
+
+/*
+ * Clipped policy loss with a KL term, and its gradient.  For a row t with a
+ * token and weight w != 0, lp its log probability, A its advantage:
+ *   rho = exp(lp - old[t]);  u = rho A;  c = min(max(rho, 1 - clip_lo), 1 + clip_hi) A
+ *   gain = min(u, c)
+ *   far = ref[t] - lp;  k = exp(far) - far - 1       (0 without ref)
+ *   loss = sum_t w (kl k - gain)
+ *   coef = w (kl (1 - exp(far)) - (u <= c ? u : 0))   = d loss / d lp
+ *   dlogits[t][v] = grad_scale * scale * coef * ([v == label] - softmax_v)
+ * Rows without a token or with w == 0 add nothing, have logp 0 and a zero
+ * gradient.  Sums over rows are taken in fp64 in a fixed order.
+ *   old, adv, weight  device float[rows];  ref: the same, or NULL (then kl
+ *            is not read).
+ *   clip_lo in [0, 1], clip_hi >= 0, kl finite, grad_scale finite.
+ *   logp     device float[rows].
+ *   stats    device float[4]: the loss, sum w (-gain), sum w k, sum of w
+ *            where u > c.
+ *   dlogits  NULL (forward only), or device, of in->type, element (t, v) at
+ *            dlogits[t * ld_d + v]; every v < vocab of every row is
+ *            written.  May be in->x itself (ld_d == in->ld), else it must
+ *            not overlap it.
+ *   ws       sparcml_workspace_size(SPARCML_OP_POLICY, 1, rows, vocab, ...)
+ * Does not synchronize.  Errors: EINVAL, EWORKSPACE, EHIP.
+ */
+typedef struct sparcml_policy_args {
+    const float* old_logp;
+    const float* ref_logp;
+    const float* adv;
+    const float* weight;
+    float clip_lo, clip_hi, kl, grad_scale;
+} sparcml_policy_args;
+SPARCML_API int sparcml_policy_loss(const sparcml_logits* in, const sparcml_policy_args* args, float* logp,
+                        float* stats, void* dlogits, uint64_t ld_d, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Loss of paired log ratios, and its gradient.  The rows are the tokens of
+ * 2 * pairs sequences, sequence i at rows [bounds[i], bounds[i + 1]); of pair
+ * b, sequence 2b is the preferred one.  Over a sequence's rows with a token,
+ *   reward_i = beta * sum (lp - ref[t])
+ *   h = reward_2b - reward_2b+1
+ *   loss = mean over pairs of -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h)
+ * and the gradient with respect to the logits, scaled by grad_scale.  Rows
+ * without a token add nothing, have logp 0 and a zero gradient; an empty
+ * sequence has reward 0.  Sums over rows and pairs are taken in fp64 in a
+ * fixed order.
+ *   pairs    1 <= pairs <= 65535.
+ *   bounds   HOST array of 2 * pairs + 1: bounds[0] == 0, not decreasing,
+ *            bounds[2 * pairs] == rows.
+ *   ref      device float[rows], or NULL (0 everywhere).
+ *   beta, grad_scale finite, 0 <= smoothing <= 1.
+ *   logp     device float[rows].
+ *   stats    device float[4]: the loss, the share of pairs with h > 0, the
+ *            mean reward of the preferred and of the other sequences.
+ *   dlogits, ld_d   as for sparcml_policy_loss.
+ *   ws       sparcml_workspace_size(SPARCML_OP_PREFERENCE, pairs, rows, vocab, ...)
+ * Does not synchronize.  Errors: EINVAL, EWORKSPACE, EHIP.
+ */
+SPARCML_API int sparcml_preference_loss(const sparcml_logits* in, int pairs, const uint64_t* bounds,
+                            const float* ref_logp, float beta, float smoothing, float grad_scale,
+                            float* logp, float* stats, void* dlogits, uint64_t ld_d, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/*
  * Kernel timing for benchmarks and profiling (off by default; per calling
  * thread).  While enabled, each call records a pair of HIP events on its
  * stream around each of its main kernels; sparcml_timing_read returns the
@@ -447,6 +676,10 @@ SPARCML_API int sparcml_densify(const sparcml_stream* in, uint64_t N, float* den
 #define SPARCML_TIMER_CONCAT 8
 #define SPARCML_TIMER_TOPK_BUCKETED 9
 #define SPARCML_TIMER_REDUCE_MERGE 10 /* small-data reduce: the whole merge tree in one workgroup */
+#define SPARCML_TIMER_GRAD_NORM 11    /* gradient norm */
+#define SPARCML_TIMER_ADAMW 12        /* AdamW step */
+#define SPARCML_TIMER_LOSS_ROWS 13    /* losses: the pass over the logits' rows */
+#define SPARCML_TIMER_LOSS_GRAD 14    /* losses: the gradient pass, where it is one of its own */
 SPARCML_API int sparcml_timing_enable(int on);
 SPARCML_API int sparcml_timing_read(int group, float* ms);
 

@@ -40,6 +40,11 @@ int hip_fail(hipError_t e, const char* where)
 }
 
 bool valid_n(uint64_t N) { return N >= 1 && N < (1ull << 32); }
+bool valid_rows(uint64_t rows, uint64_t vocab)
+{
+    return rows >= 1 && rows < (1ull << 31) && vocab >= 1 && vocab < (1ull << 31);
+}
+constexpr uint64_t kMaxElements = 1ull << 42;  // of all tensors of a plan (their pieces' number fits 32 bits)
 bool valid_bits(uint32_t b) { return b == 2 || b == 4 || b == 8; }
 bool is_pow2(int p) { return p >= 1 && (p & (p - 1)) == 0; }
 
@@ -331,6 +336,19 @@ int sparcml_workspace_size(int op, int P, uint64_t N, uint64_t max_nnz, double d
         if (P < 1 || P > 65535) return fail(SPARCML_EINVAL, "P must be in [1, 65535]");
         *bytes = validate_workspace(P);
         return SPARCML_OK;
+    case SPARCML_OP_TENSORS:
+        if (P < 1 || P > 65535 || N > kMaxElements) return fail(SPARCML_EINVAL, "bad tensor sizes");
+        // pieces of every tensor: at most one that is not full each
+        tensors_carve(nullptr, (uint32_t)P, N / kTensorChunk + (uint64_t)P, bytes);
+        return SPARCML_OK;
+    case SPARCML_OP_LOGPROB:
+    case SPARCML_OP_POLICY:
+    case SPARCML_OP_PREFERENCE:
+        if (P < 1 || P > 65535 || !valid_rows(N, max_nnz)) return fail(SPARCML_EINVAL, "bad sizes of logits");
+        *bytes = op == SPARCML_OP_LOGPROB  ? logprob_workspace(N, max_nnz)
+                 : op == SPARCML_OP_POLICY ? policy_workspace(N, max_nnz)
+                                           : preference_workspace((uint32_t)P, N, max_nnz);
+        return SPARCML_OK;
     default: return fail(SPARCML_EINVAL, "unknown op %d", op);
     }
 }
@@ -579,6 +597,201 @@ int sparcml_densify(const sparcml_stream* in, uint64_t N, float* dense, void* st
                                in->is_dense ? 1 : 0, dense, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, "densify");
     return SPARCML_OK;
+}
+
+static uint64_t plan_check(const sparcml_tensors& p)
+{
+    uint64_t h = 0x9E3779B97F4A7C15ull ^ (uint64_t)(uintptr_t)p.ws;
+    for (uint64_t v : {p.total, p.chunks, (uint64_t)p.count, (uint64_t)p.grad_type, (uint64_t)p.copy_type,
+                       (uint64_t)p.state_bits})
+        h = (h ^ v) * 0xBF58476D1CE4E5B9ull;
+    return h;
+}
+
+int sparcml_tensors_prepare(int count, const sparcml_tensor* tensors, int grad_type, int copy_type, int state_bits,
+                            sparcml_tensors* plan, void* ws, size_t ws_bytes, void* stream)
+{
+    try {
+        if (count < 1 || count > 65535) return fail(SPARCML_EINVAL, "count must be in [1, 65535]");
+        if (!tensors || !plan) return fail(SPARCML_EINVAL, "NULL argument");
+        if (grad_type < SPARCML_F32 || grad_type > SPARCML_F16) return fail(SPARCML_EINVAL, "unknown grad_type %d", grad_type);
+        if (state_bits != 0 && state_bits != 8 && state_bits != 32)
+            return fail(SPARCML_EINVAL, "state_bits must be 0, 8 or 32");
+        std::vector<TensorDesc> d(count);
+        uint64_t total = 0, chunks = 0;
+        for (int t = 0; t < count; ++t) {
+            const sparcml_tensor& a = tensors[t];
+            // the random draw of element j comes from counter word j >> 2 (32 bits)
+            if (a.n > (1ull << 34)) return fail(SPARCML_EINVAL, "tensor %d: more than 2^34 elements", t);
+            if (a.n && !a.grad) return fail(SPARCML_EINVAL, "tensor %d: grad is NULL", t);
+            if (a.n && state_bits) {
+                if (!a.param || !a.m || !a.v) return fail(SPARCML_EINVAL, "tensor %d: NULL pointer", t);
+                if (state_bits == 8 && (!a.m_scale || !a.v_scale)) return fail(SPARCML_EINVAL, "tensor %d: scales are NULL", t);
+                if (a.copy && copy_type != SPARCML_BF16 && copy_type != SPARCML_F16)
+                    return fail(SPARCML_EINVAL, "tensor %d: copy_type must be SPARCML_BF16 or SPARCML_F16", t);
+            }
+            if (state_bits && !(isfinite(a.decay) && isfinite(a.lr_scale)))
+                return fail(SPARCML_EINVAL, "tensor %d: decay and lr_scale must be finite", t);
+            d[t] = TensorDesc{a.param, a.grad, a.m, a.v, a.m_scale, a.v_scale, a.copy, a.n, a.decay, a.lr_scale};
+            total += a.n;
+            chunks += (a.n + kTensorChunk - 1) / kTensorChunk;
+        }
+        if (total > kMaxElements) return fail(SPARCML_EINVAL, "more than 2^42 elements");
+        size_t need = 0;
+        tensors_carve(nullptr, (uint32_t)count, total / kTensorChunk + (uint64_t)count, &need);
+        if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+        hipError_t e = tensors_prepare_run((uint32_t)count, d.data(), chunks, ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "tensors_prepare");
+        sparcml_tensors p;
+        memset(&p, 0, sizeof(p));
+        p.ws = ws;
+        p.total = total;
+        p.chunks = chunks;
+        p.count = (uint32_t)count;
+        p.grad_type = (uint32_t)grad_type;
+        p.copy_type = (uint32_t)copy_type;
+        p.state_bits = (uint32_t)state_bits;
+        p.check = plan_check(p);
+        *plan = p;
+        return SPARCML_OK;
+    } catch (const std::exception& ex) {
+        return fail(SPARCML_EHIP, "host exception: %s", ex.what());
+    }
+}
+
+int sparcml_grad_norm(const sparcml_tensors* plan, double grad_scale, double max_norm, float* out, void* stream)
+{
+    if (!plan || plan->check != plan_check(*plan)) return fail(SPARCML_EINVAL, "no plan of sparcml_tensors_prepare");
+    if (!out) return fail(SPARCML_EINVAL, "out is NULL");
+    if (!(grad_scale > 0.0) || !isfinite(grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be positive and finite");
+    if (!(max_norm > 0.0)) return fail(SPARCML_EINVAL, "max_norm must be positive");
+    hipError_t e = grad_norm_run(plan->count, plan->chunks, plan->grad_type, grad_scale, max_norm, out, plan->ws,
+                                 (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "grad_norm");
+    return SPARCML_OK;
+}
+
+int sparcml_adamw(const sparcml_tensors* plan, const sparcml_adamw_args* args, const float* clip, void* stream)
+{
+    if (!plan || plan->check != plan_check(*plan)) return fail(SPARCML_EINVAL, "no plan of sparcml_tensors_prepare");
+    if (!args) return fail(SPARCML_EINVAL, "args is NULL");
+    if (!plan->state_bits) return fail(SPARCML_EINVAL, "the plan holds gradients only");
+    const sparcml_adamw_args& a = *args;
+    if (!(a.lr >= 0.0) || !isfinite(a.lr)) return fail(SPARCML_EINVAL, "lr must be finite and not negative");
+    if (!(a.beta1 >= 0.0 && a.beta1 < 1.0 && a.beta2 >= 0.0 && a.beta2 < 1.0))
+        return fail(SPARCML_EINVAL, "betas must be in [0, 1)");
+    if (!((float)a.eps > 0.0f) || !isfinite((float)a.eps)) return fail(SPARCML_EINVAL, "eps must be positive and finite");
+    if (!isfinite((float)a.grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be finite");
+    if (a.step < 1) return fail(SPARCML_EINVAL, "step must be at least 1");
+    AdamwStep s;
+    s.lr = a.lr;
+    s.rate = a.lr / (1.0 - pow(a.beta1, (double)a.step));
+    s.b1 = (float)a.beta1;
+    s.omb1 = (float)(1.0 - a.beta1);
+    s.b2 = (float)a.beta2;
+    s.omb2 = (float)(1.0 - a.beta2);
+    s.ibc2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)a.step)));
+    s.eps = (float)a.eps;
+    s.gs = (float)a.grad_scale;
+    s.step = a.step;
+    s.key0 = (uint32_t)a.seed;
+    s.key1 = (uint32_t)(a.seed >> 32);
+    hipError_t e = adamw_run(plan->count, plan->chunks, plan->grad_type, plan->copy_type, plan->state_bits, s, clip,
+                             plan->ws, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "adamw");
+    return SPARCML_OK;
+}
+
+// Shared argument checks of the losses.
+static int logits_validate(const sparcml_logits* in, Logits* l)
+{
+    if (!in || !in->x || !in->label) return fail(SPARCML_EINVAL, "NULL logits or labels");
+    if (!valid_rows(in->rows, in->vocab)) return fail(SPARCML_EINVAL, "rows and vocab must be in [1, 2^31)");
+    if (in->ld < in->vocab || in->ld >= (1ull << 31)) return fail(SPARCML_EINVAL, "need vocab <= ld < 2^31");
+    if (in->type > SPARCML_F16) return fail(SPARCML_EINVAL, "unknown type %u", in->type);
+    if (!(in->scale > 0.0f) || !isfinite(in->scale)) return fail(SPARCML_EINVAL, "scale must be positive and finite");
+    *l = Logits{in->x, in->label, in->rows, in->vocab, in->ld, in->type, in->scale};
+    return SPARCML_OK;
+}
+
+// The gradient is the logits' own place or none of their rows' (the ends of
+// the two arrays decide).
+static int gradient_validate(const sparcml_logits* in, const void* d, uint64_t ldd)
+{
+    if (!d) return SPARCML_OK;
+    if (ldd < in->vocab || ldd >= (1ull << 31)) return fail(SPARCML_EINVAL, "need vocab <= ld_d < 2^31");
+    if (d == in->x) return ldd == in->ld ? SPARCML_OK : fail(SPARCML_EINVAL, "in place, ld_d must be ld");
+    const uint64_t size = in->type == SPARCML_F32 ? 4 : 2;
+    const uintptr_t x0 = (uintptr_t)in->x, x1 = x0 + ((in->rows - 1) * in->ld + in->vocab) * size;
+    const uintptr_t d0 = (uintptr_t)d, d1 = d0 + ((in->rows - 1) * ldd + in->vocab) * size;
+    if (d0 < x1 && x0 < d1) return fail(SPARCML_EINVAL, "dlogits overlaps the logits");
+    return SPARCML_OK;
+}
+
+int sparcml_token_logprob(const sparcml_logits* in, float* logp, float* lse, void* ws, size_t ws_bytes, void* stream)
+{
+    Logits l;
+    int rc = logits_validate(in, &l);
+    if (rc != SPARCML_OK) return rc;
+    if (!logp) return fail(SPARCML_EINVAL, "logp is NULL");
+    const size_t need = logprob_workspace(l.rows, l.vocab);
+    if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+    hipError_t e = logprob_run(l, logp, lse, ws, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "token_logprob");
+    return SPARCML_OK;
+}
+
+int sparcml_policy_loss(const sparcml_logits* in, const sparcml_policy_args* args, float* logp, float* stats,
+                        void* dlogits, uint64_t ld_d, void* ws, size_t ws_bytes, void* stream)
+{
+    Logits l;
+    int rc = logits_validate(in, &l);
+    if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
+    if (rc != SPARCML_OK) return rc;
+    if (!args || !args->old_logp || !args->adv || !args->weight || !logp || !stats)
+        return fail(SPARCML_EINVAL, "NULL argument");
+    if (!(args->clip_lo >= 0.0f && args->clip_lo <= 1.0f)) return fail(SPARCML_EINVAL, "clip_lo must be in [0, 1]");
+    if (!(args->clip_hi >= 0.0f)) return fail(SPARCML_EINVAL, "clip_hi must not be negative");
+    if (!isfinite(args->grad_scale) || (args->ref_logp && !isfinite(args->kl)))
+        return fail(SPARCML_EINVAL, "kl and grad_scale must be finite");
+    const size_t need = policy_workspace(l.rows, l.vocab);
+    if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+    const PolicyArgs a{args->old_logp, args->ref_logp, args->adv, args->weight, (float)(1.0 - (double)args->clip_lo),
+                       (float)(1.0 + (double)args->clip_hi), args->kl, args->grad_scale};
+    hipError_t e = policy_run(l, a, logp, stats, dlogits, ld_d, ws, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_fail(e, "policy_loss");
+    return SPARCML_OK;
+}
+
+int sparcml_preference_loss(const sparcml_logits* in, int pairs, const uint64_t* bounds, const float* ref_logp,
+                            float beta, float smoothing, float grad_scale, float* logp, float* stats, void* dlogits,
+                            uint64_t ld_d, void* ws, size_t ws_bytes, void* stream)
+{
+    try {
+        Logits l;
+        int rc = logits_validate(in, &l);
+        if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
+        if (rc != SPARCML_OK) return rc;
+        if (pairs < 1 || pairs > 65535) return fail(SPARCML_EINVAL, "pairs must be in [1, 65535]");
+        if (!bounds || !logp || !stats) return fail(SPARCML_EINVAL, "NULL argument");
+        std::vector<uint32_t> b(2 * (size_t)pairs + 1);
+        for (int i = 0; i <= 2 * pairs; ++i) {
+            if (bounds[i] > l.rows || (i ? bounds[i] < bounds[i - 1] : bounds[0] != 0) ||
+                (i == 2 * pairs && bounds[i] != l.rows))
+                return fail(SPARCML_EINVAL, "bounds[%d]: need 0 = bounds[0] <= ... <= bounds[2 pairs] = rows", i);
+            b[i] = (uint32_t)bounds[i];
+        }
+        if (!isfinite(beta) || !isfinite(grad_scale)) return fail(SPARCML_EINVAL, "beta and grad_scale must be finite");
+        if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return fail(SPARCML_EINVAL, "smoothing must be in [0, 1]");
+        const size_t need = preference_workspace((uint32_t)pairs, l.rows, l.vocab);
+        if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+        hipError_t e = preference_run(l, PreferenceArgs{ref_logp, beta, smoothing, grad_scale}, (uint32_t)pairs,
+                                      b.data(), logp, stats, dlogits, ld_d, ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "preference_loss");
+        return SPARCML_OK;
+    } catch (const std::exception& ex) {
+        return fail(SPARCML_EHIP, "host exception: %s", ex.what());
+    }
 }
 
 }  // extern "C"

@@ -51,7 +51,11 @@ enum TimerSlot {
     kTConcat = 8,       // concatenation of disjoint parts
     kTTopkBuckets = 9,  // bucketed top-k with error feedback
     kTReduceMerge = 10, // small-data reduce: the whole merge tree in one workgroup
-    kTSlots = 11
+    kTGradNorm = 11,    // gradient norm
+    kTAdamw = 12,       // AdamW step
+    kTLossRows = 13,    // losses: the pass over the logits' rows
+    kTLossGrad = 14,    // losses: the gradient pass
+    kTSlots = 15
 };
 void timer_begin(int slot, hipStream_t s);
 void timer_end(int slot, hipStream_t s);
@@ -235,5 +239,73 @@ hipError_t quant_buckets_run(int P, const float* const* vals, const uint64_t* n,
 size_t validate_workspace(int P);
 hipError_t validate_run(int P, const uint32_t* const* idx, const uint64_t* nnz, uint64_t lo, uint64_t hi,
                         void* ws, hipStream_t s, int* bad_stream, uint64_t* bad_pos);
+
+// ---------------------------------------------------------------- tensors
+enum ElemType : uint32_t { kF32 = 0, kBf16 = 1, kF16 = 2 };
+constexpr uint32_t kStateBlock = 256;    // elements that share a scale (8-bit moments)
+constexpr uint32_t kTensorChunk = 4096;  // elements of a tensor that the work map lists as one piece
+
+// Device copy of one tensor descriptor (72 bytes).
+struct TensorDesc {
+    float* param;
+    const void* grad;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    void* copy;
+    uint64_t n;
+    float decay, lr_scale;
+};
+
+// What a prepared workspace holds; the same carving for every call on it.
+struct TensorTab {
+    TensorDesc* desc;  // [count]
+    uint32_t* first;   // [count] a tensor's first chunk
+    uint2* map;        // [chunks] {tensor, chunk of it}
+    double* partial;   // [kNormParts]
+};
+constexpr uint32_t kNormParts = 2048;
+TensorTab tensors_carve(void* ws, uint32_t count, uint64_t chunks, size_t* bytes);
+hipError_t tensors_prepare_run(uint32_t count, const TensorDesc* host, uint64_t chunks, void* ws, hipStream_t s);
+hipError_t grad_norm_run(uint32_t count, uint64_t chunks, uint32_t gtype, double grad_scale, double max_norm,
+                         float* out, void* ws, hipStream_t s);
+
+// One step's scalars: factors in fp64 that are rounded once on their way in.
+struct AdamwStep {
+    double lr, rate;                          // lr and lr / (1 - beta1^s), before a tensor's lr_scale
+    float b1, omb1, b2, omb2, ibc2, eps, gs;  // betas, 1 - betas, 1 / sqrt(1 - beta2^s), eps, grad_scale
+    uint32_t step, key0, key1;
+};
+hipError_t adamw_run(uint32_t count, uint64_t chunks, uint32_t gtype, uint32_t ctype, uint32_t bits,
+                     const AdamwStep& a, const float* clip, void* ws, hipStream_t s);
+
+// ---------------------------------------------------------------- losses
+// Rows of logits with a token each (device pointers).
+struct Logits {
+    const void* x;
+    const int32_t* label;
+    uint64_t rows, vocab, ld;
+    uint32_t type;
+    float scale;
+};
+struct PolicyArgs {
+    const float *old_logp, *ref_logp, *adv, *weight;
+    float lo, hi, kl;  // ratio bounds 1 - clip_lo and 1 + clip_hi
+    float grad_scale;
+};
+struct PreferenceArgs {
+    const float* ref_logp;
+    float beta, smoothing, grad_scale;
+};
+size_t logprob_workspace(uint64_t rows, uint64_t vocab);
+size_t policy_workspace(uint64_t rows, uint64_t vocab);
+size_t preference_workspace(uint32_t pairs, uint64_t rows, uint64_t vocab);
+hipError_t logprob_run(const Logits& in, float* logp, float* lse, void* ws, hipStream_t s);
+hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float* stats, void* dlogits, uint64_t ldd,
+                      void* ws, hipStream_t s);
+// bounds: host array of 2 * pairs + 1 row numbers (each below 2^31).
+hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pairs, const uint32_t* bounds,
+                          float* logp, float* stats, void* dlogits, uint64_t ldd, void* ws, hipStream_t s);
 
 }  // namespace sparcml

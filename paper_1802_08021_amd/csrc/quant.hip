@@ -8,6 +8,7 @@
 // by a lane butterfly, 32 such groups by a second butterfly, waves and
 // blocks in tree order, and block partials by further aligned trees.
 #include "internal.h"
+#include "philox_device.h"
 
 #include <algorithm>
 #include <cstring>
@@ -131,27 +132,6 @@ __global__ void __launch_bounds__(1024) k_sum_f64(const double* in, uint32_t cou
         out[(uint64_t)r * out_count + b] = t[0];
         if (scale) scale[r] = (float)sqrt(t[0]);
     }
-}
-
-// Philox4x32-10 (Salmon et al., SC'11): ten rounds of two 32x32->64
-// multiplies with the high halves mixed into the other words and the key,
-// the key advanced by the Weyl constants between rounds.
-__device__ __forceinline__ uint4 philox(uint4 c, uint32_t k0, uint32_t k1)
-{
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-        if (i) {
-            k0 += 0x9E3779B9u;
-            k1 += 0xBB67AE85u;
-        }
-        // full 64-bit products: one v_mad_u64_u32 each instead of a low and
-        // a high multiply
-        const uint64_t p0 = (uint64_t)0xD2511F53u * c.x, p1 = (uint64_t)0xCD9E8D57u * c.z;
-        const uint32_t lo0 = (uint32_t)p0, hi0 = (uint32_t)(p0 >> 32);
-        const uint32_t lo1 = (uint32_t)p1, hi1 = (uint32_t)(p1 >> 32);
-        c = make_uint4(hi1 ^ c.y ^ k0, lo1, hi0 ^ c.w ^ k1, lo0);
-    }
-    return c;
 }
 
 // Four dequantized values from element e on, those below n: one store where

@@ -1,0 +1,323 @@
+// The update of Alg. 1 on gfx950: norm of a model's gradients, AdamW step
+// over all its tensors, moments in 32 or in 8 bits.
+//
+// Both walk a map of pieces of 4096 elements, {tensor, piece of it}, that
+// tensors_prepare_run lays out once: a workgroup finds its tensor with two
+// loads, whatever the number and the lengths of the tensors, and one launch
+// covers them all.
+#include "internal.h"
+#include "philox_device.h"
+#include "types_device.h"
+
+#include <algorithm>
+#include <vector>
+
+namespace sparcml {
+namespace {
+
+// map[first[t] + i] = {t, i} for the pieces i of tensor t.
+__global__ void k_tensor_map(const TensorDesc* desc, const uint32_t* first, uint2* map)
+{
+    const uint32_t t = blockIdx.x;
+    const uint32_t pieces = (uint32_t)((desc[t].n + kTensorChunk - 1) / kTensorChunk);
+    for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) map[first[t] + i] = make_uint2(t, i);
+}
+
+// Elements e .. e + 3 of an array of n as fp32, zeros past the end.
+template <int TYPE>
+__device__ __forceinline__ f32x4 get4(const void* p, uint64_t e, uint64_t n)
+{
+    typedef typename Elem<TYPE>::type E;
+    const E* q = static_cast<const E*>(p) + e;
+    if (e + 4 <= n) return __builtin_convertvector(load4<typename Elem<TYPE>::vec4>(q), f32x4);
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (e + i < n) x[i] = (float)q[i];
+    return x;
+}
+
+// The same elements written, rounded to nearest where TYPE is narrower.
+template <int TYPE>
+__device__ __forceinline__ void put4(void* p, uint64_t e, uint64_t n, f32x4 x)
+{
+    typedef typename Elem<TYPE>::type E;
+    E* q = static_cast<E*>(p) + e;
+    if (e + 4 <= n) {
+        store4(q, __builtin_convertvector(x, typename Elem<TYPE>::vec4));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (e + i < n) q[i] = (E)x[i];
+    }
+}
+
+// Four codes as bytes of a word, zeros past the end.
+__device__ __forceinline__ uint32_t get_codes(const void* p, uint64_t e, uint64_t n)
+{
+    const uint8_t* q = static_cast<const uint8_t*>(p) + e;
+    typedef uint32_t U __attribute__((aligned(1)));
+    if (e + 4 <= n) return *reinterpret_cast<const U*>(q);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (e + i < n) w |= (uint32_t)q[i] << (8 * i);
+    return w;
+}
+
+__device__ __forceinline__ void put_codes(void* p, uint64_t e, uint64_t n, uint32_t w)
+{
+    uint8_t* q = static_cast<uint8_t*>(p) + e;
+    typedef uint32_t U __attribute__((aligned(1)));
+    if (e + 4 <= n) {
+        *reinterpret_cast<U*>(q) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (e + i < n) q[i] = (uint8_t)(w >> (8 * i));
+    }
+}
+
+__device__ __forceinline__ f32x4 decode4(uint32_t w, float scale)
+{
+    f32x4 x;
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0) * scale;
+    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1) * scale;
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2) * scale;
+    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3) * scale;
+    return x;
+}
+
+// E4M3 codes of y, |y| <= 448: a code's neighbour above is taken when the
+// value's bits below the code's last one and the draw's carry out of them
+// (the conversion's stochastic form; the draw's 16 bits are its top ones).
+__device__ __forceinline__ uint32_t encode4(f32x4 y, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3)
+{
+    int w = 0;
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], (int)r0, w, 0);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], (int)r1, w, 1);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], (int)r2, w, 2);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], (int)r3, w, 3);
+    return (uint32_t)w;
+}
+
+// Biased exponent of the least power of two (at least 2^-100) that brings a
+// block's largest magnitude to at most 448 = 1.75 * 2^8: the magnitude's own
+// exponent less 8, one more above 1.75 * 2^e.
+__device__ __forceinline__ uint32_t block_exponent(f32x4 x)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    const uint32_t e = (wave_max(top) + 0x1FFFFFu) >> 23;
+    return max(e, 35u) - 8u;
+}
+
+// One AdamW step of piece blockIdx.x / (4096 / (1024 U)) of the map: 1024
+// elements a workgroup and round, four a lane, so that a wave holds exactly
+// one block of the 8-bit form.
+template <int BITS, int GT, int CT, int U>
+__global__ void __launch_bounds__(256) k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
+                                               uint64_t pieces, AdamwStep a, const float* __restrict__ clip)
+{
+    constexpr uint32_t kSub = kTensorChunk / (1024 * U);
+    float f = a.gs;
+    if (clip) {
+        const float c = clip[1];
+        if (c == 0.0f) return;
+        f = a.gs * c;
+    }
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    for (uint64_t w = blockIdx.x; w < pieces * kSub; w += gridDim.x) {
+        const uint2 at = map[w / kSub];
+        const TensorDesc d = desc[at.x];
+        const float keep = (float)(1.0 - a.lr * (double)d.lr_scale * (double)d.decay);
+        const float rate = (float)(a.rate * (double)d.lr_scale);
+        const uint64_t e0 = (uint64_t)at.y * kTensorChunk + (uint64_t)(w % kSub) * (1024 * U) + (uint32_t)wv * 256;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint64_t b = e0 + (uint32_t)u * 1024, e = b + (uint32_t)lane * 4;
+            if (b >= d.n) break;  // a whole wave's elements
+            f32x4 p = get4<kF32>(d.param, e, d.n);
+            const f32x4 g = get4<GT>(d.grad, e, d.n) * f;
+            f32x4 m, v;
+            if (BITS == 32) {
+                m = get4<kF32>(d.m, e, d.n);
+                v = get4<kF32>(d.v, e, d.n);
+            } else {
+                m = decode4(get_codes(d.m, e, d.n), d.m_scale[b / kStateBlock]);
+                v = decode4(get_codes(d.v, e, d.n), d.v_scale[b / kStateBlock]);
+                v = v * v;
+            }
+            m = a.b1 * m + a.omb1 * g;
+            v = a.b2 * v + a.omb2 * (g * g);
+            f32x4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r[i] = sqrtf(v[i]);  // (both correctly rounded)
+                p[i] = p[i] * keep - rate * (m[i] / (r[i] * a.ibc2 + a.eps));
+            }
+            put4<kF32>(d.param, e, d.n, p);
+            if (d.copy) put4<CT>(d.copy, e, d.n, p);
+            if (BITS == 32) {
+                put4<kF32>(d.m, e, d.n, m);
+                put4<kF32>(d.v, e, d.n, v);
+            } else {
+                // lanes past the end hold zeros (of weights and states alike)
+                const uint4 z = philox(make_uint4((uint32_t)(e >> 2), at.x, a.step, 0u), a.key0, a.key1);
+                const uint32_t em = block_exponent(m), er = block_exponent(r);
+                const f32x4 ym = m * __uint_as_float((254u - em) << 23);
+                f32x4 yr = r * __uint_as_float((254u - er) << 23);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) yr[i] = fmaxf(yr[i], 0x1p-9f);
+                put_codes(d.m, e, d.n, encode4(ym, z.x << 16, z.y << 16, z.z << 16, z.w << 16));
+                put_codes(d.v, e, d.n,
+                          encode4(yr, z.x & 0xFFFF0000u, z.y & 0xFFFF0000u, z.z & 0xFFFF0000u, z.w & 0xFFFF0000u));
+                if (lane == 0) {
+                    d.m_scale[b / kStateBlock] = __uint_as_float(em << 23);
+                    d.v_scale[b / kStateBlock] = __uint_as_float(er << 23);
+                }
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ double block_sum(double x, double* s_w)
+{
+    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
+}
+
+// partial[b] = sum of squares of pieces b, b + gridDim.x, ...
+template <int GT>
+__global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
+                                              uint64_t pieces, double* partial)
+{
+    __shared__ double s_w[4];
+    double acc = 0.0;
+    for (uint64_t c = blockIdx.x; c < pieces; c += gridDim.x) {
+        const uint2 at = map[c];
+        const TensorDesc d = desc[at.x];
+        const uint64_t e0 = (uint64_t)at.y * kTensorChunk + (uint64_t)threadIdx.x * 4;
+#pragma unroll
+        for (int u = 0; u < (int)kTensorChunk / 1024; ++u) {
+            const f32x4 g = get4<GT>(d.grad, e0 + (uint32_t)u * 1024, d.n);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc = fma((double)g[i], (double)g[i], acc);
+        }
+    }
+    acc = block_sum(acc, s_w);
+    if (threadIdx.x == 0) partial[blockIdx.x] = acc;
+}
+
+__global__ void __launch_bounds__(256) k_norm_end(const double* partial, uint32_t parts, double gs, double max_norm,
+                                                  float* out)
+{
+    __shared__ double s_w[4];
+    double acc = 0.0;
+    for (uint32_t i = threadIdx.x; i < parts; i += 256) acc += partial[i];
+    acc = block_sum(acc, s_w);
+    if (threadIdx.x == 0) {
+        const float norm = (float)(gs * sqrt(acc));
+        const float c = (float)(max_norm / ((double)norm + 1e-6));
+        out[0] = norm;
+        out[1] = isfinite(norm) ? fminf(1.0f, c) : 0.0f;
+    }
+}
+
+template <int BITS, int GT, int CT>
+void launch_adamw(const TensorTab& t, uint64_t pieces, const AdamwStep& a, const float* clip, hipStream_t s)
+{
+    constexpr int U = 4;
+    const uint64_t grid = std::min<uint64_t>(pieces * (kTensorChunk / (1024 * U)), 1u << 22);
+    hipLaunchKernelGGL((k_adamw<BITS, GT, CT, U>), dim3((uint32_t)grid), dim3(256), 0, s, t.desc, t.map, pieces, a, clip);
+}
+
+template <int BITS, int GT>
+void launch_adamw(uint32_t ctype, const TensorTab& t, uint64_t pieces, const AdamwStep& a, const float* clip,
+                  hipStream_t s)
+{
+    if (ctype == kF16)
+        launch_adamw<BITS, GT, kF16>(t, pieces, a, clip, s);
+    else
+        launch_adamw<BITS, GT, kBf16>(t, pieces, a, clip, s);
+}
+
+template <int BITS>
+void launch_adamw(uint32_t gtype, uint32_t ctype, const TensorTab& t, uint64_t pieces, const AdamwStep& a,
+                  const float* clip, hipStream_t s)
+{
+    if (gtype == kF32)
+        launch_adamw<BITS, kF32>(ctype, t, pieces, a, clip, s);
+    else if (gtype == kBf16)
+        launch_adamw<BITS, kBf16>(ctype, t, pieces, a, clip, s);
+    else
+        launch_adamw<BITS, kF16>(ctype, t, pieces, a, clip, s);
+}
+
+}  // namespace
+
+TensorTab tensors_carve(void* ws, uint32_t count, uint64_t chunks, size_t* bytes)
+{
+    Carve c(ws);
+    TensorTab t;
+    t.desc = c.take<TensorDesc>(count);
+    t.first = c.take<uint32_t>(count);
+    t.map = c.take<uint2>(chunks);
+    t.partial = c.take<double>(kNormParts);
+    if (bytes) *bytes = c.used;
+    return t;
+}
+
+hipError_t tensors_prepare_run(uint32_t count, const TensorDesc* host, uint64_t chunks, void* ws, hipStream_t s)
+{
+    const TensorTab t = tensors_carve(ws, count, chunks, nullptr);
+    std::vector<uint32_t> first(count);
+    uint64_t at = 0;
+    for (uint32_t i = 0; i < count; ++i) {
+        first[i] = (uint32_t)at;
+        at += (host[i].n + kTensorChunk - 1) / kTensorChunk;
+    }
+    hipError_t e = upload(t.desc, host, count * sizeof(TensorDesc), s);
+    if (e == hipSuccess) e = upload(t.first, first.data(), count * sizeof(uint32_t), s);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_tensor_map, dim3(count), dim3(256), 0, s, t.desc, t.first, t.map);
+    return hipGetLastError();
+}
+
+hipError_t grad_norm_run(uint32_t count, uint64_t chunks, uint32_t gtype, double grad_scale, double max_norm,
+                         float* out, void* ws, hipStream_t s)
+{
+    const TensorTab t = tensors_carve(ws, count, chunks, nullptr);
+    const uint32_t parts = (uint32_t)std::min<uint64_t>(chunks, kNormParts);
+    timer_begin(kTGradNorm, s);
+    if (parts) {
+        if (gtype == kF32)
+            hipLaunchKernelGGL((k_norm<kF32>), dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial);
+        else if (gtype == kBf16)
+            hipLaunchKernelGGL((k_norm<kBf16>), dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial);
+        else
+            hipLaunchKernelGGL((k_norm<kF16>), dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial);
+    }
+    hipLaunchKernelGGL(k_norm_end, dim3(1), dim3(256), 0, s, t.partial, parts, grad_scale, max_norm, out);
+    timer_end(kTGradNorm, s);
+    return hipGetLastError();
+}
+
+hipError_t adamw_run(uint32_t count, uint64_t chunks, uint32_t gtype, uint32_t ctype, uint32_t bits,
+                     const AdamwStep& a, const float* clip, void* ws, hipStream_t s)
+{
+    if (!chunks) return hipSuccess;
+    const TensorTab t = tensors_carve(ws, count, chunks, nullptr);
+    timer_begin(kTAdamw, s);
+    if (bits == 32)
+        launch_adamw<32>(gtype, ctype, t, chunks, a, clip, s);
+    else
+        launch_adamw<8>(gtype, ctype, t, chunks, a, clip, s);
+    timer_end(kTAdamw, s);
+    return hipGetLastError();
+}
+
+}  // namespace sparcml

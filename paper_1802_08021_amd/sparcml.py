@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "_lib", "libsparcml.so")
 
 OK, EINVAL, ECAPACITY, EWORKSPACE, EUNSORTED, EHIP = 0, -1, -2, -3, -4, -5
 OP_TOPK, OP_QUANTIZE, OP_REDUCE, OP_DENSIFY, OP_QUANTIZE_BUCKETED, OP_CONCAT, OP_VALIDATE = 1, 2, 3, 4, 5, 6, 7
+OP_TENSORS, OP_LOGPROB, OP_POLICY, OP_PREFERENCE = 8, 9, 10, 11
+F32, BF16, F16 = 0, 1, 2
 
 
 class Stream(ctypes.Structure):
@@ -30,6 +32,57 @@ class Stream(ctypes.Structure):
         ("is_dense", ctypes.c_uint32),
         ("qbits", ctypes.c_uint32),
     ]
+
+
+class Tensor(ctypes.Structure):
+    """Mirror of ``sparcml_tensor``."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("n", ctypes.c_uint64),
+        ("decay", ctypes.c_float),
+        ("lr_scale", ctypes.c_float),
+    ]
+
+
+class Tensors(ctypes.Structure):
+    """Mirror of ``sparcml_tensors`` (the plan of a model's tensors)."""
+    _fields_ = [
+        ("ws", ctypes.c_void_p),
+        ("total", ctypes.c_uint64),
+        ("chunks", ctypes.c_uint64),
+        ("count", ctypes.c_uint32),
+        ("grad_type", ctypes.c_uint32),
+        ("copy_type", ctypes.c_uint32),
+        ("state_bits", ctypes.c_uint32),
+        ("check", ctypes.c_uint64),
+    ]
+
+
+class AdamwArgs(ctypes.Structure):
+    """Mirror of ``sparcml_adamw_args``."""
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [
+        ("seed", ctypes.c_uint64),
+        ("step", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+    ]
+
+
+class Logits(ctypes.Structure):
+    """Mirror of ``sparcml_logits``."""
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("label", ctypes.c_void_p),
+        ("rows", ctypes.c_uint64),
+        ("vocab", ctypes.c_uint64),
+        ("ld", ctypes.c_uint64),
+        ("type", ctypes.c_uint32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class PolicyArgs(ctypes.Structure):
+    """Mirror of ``sparcml_policy_args``."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("old_logp", "ref_logp", "adv", "weight")] + [
+        (name, ctypes.c_float) for name in ("clip_lo", "clip_hi", "kl", "grad_scale")]
 
 
 class SparcmlError(RuntimeError):
@@ -87,6 +140,22 @@ def lib() -> ctypes.CDLL:
     L.sparcml_split_bounds.restype = i32
     L.sparcml_densify.argtypes = [ctypes.POINTER(Stream), u64, vp, vp]
     L.sparcml_densify.restype = i32
+    f32 = ctypes.c_float
+    L.sparcml_tensors_prepare.argtypes = [i32, ctypes.POINTER(Tensor), i32, i32, i32, ctypes.POINTER(Tensors), vp,
+                                          ctypes.c_size_t, vp]
+    L.sparcml_tensors_prepare.restype = i32
+    L.sparcml_grad_norm.argtypes = [ctypes.POINTER(Tensors), ctypes.c_double, ctypes.c_double, vp, vp]
+    L.sparcml_grad_norm.restype = i32
+    L.sparcml_adamw.argtypes = [ctypes.POINTER(Tensors), ctypes.POINTER(AdamwArgs), vp, vp]
+    L.sparcml_adamw.restype = i32
+    L.sparcml_token_logprob.argtypes = [ctypes.POINTER(Logits), vp, vp, vp, ctypes.c_size_t, vp]
+    L.sparcml_token_logprob.restype = i32
+    L.sparcml_policy_loss.argtypes = [ctypes.POINTER(Logits), ctypes.POINTER(PolicyArgs), vp, vp, vp, u64, vp,
+                                      ctypes.c_size_t, vp]
+    L.sparcml_policy_loss.restype = i32
+    L.sparcml_preference_loss.argtypes = [ctypes.POINTER(Logits), i32, ctypes.POINTER(u64), vp, f32, f32, f32, vp, vp,
+                                          vp, u64, vp, ctypes.c_size_t, vp]
+    L.sparcml_preference_loss.restype = i32
     L.sparcml_timing_enable.argtypes = [i32]
     L.sparcml_timing_enable.restype = i32
     L.sparcml_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_float)]
@@ -102,6 +171,7 @@ def lib() -> ctypes.CDLL:
 TIMER_REDUCE_PASS, TIMER_REDUCE_WRITE, TIMER_REDUCE_SLOW = 0, 1, 2
 TIMER_QUANT_NORM, TIMER_QUANT_CODES, TIMER_TOPK_SELECT, TIMER_TOPK_WRITE, TIMER_DENSIFY = 3, 4, 5, 6, 7
 TIMER_CONCAT, TIMER_TOPK_BUCKETED, TIMER_REDUCE_MERGE = 8, 9, 10
+TIMER_GRAD_NORM, TIMER_ADAMW, TIMER_LOSS_ROWS, TIMER_LOSS_GRAD = 11, 12, 13, 14
 
 
 def timing_enable(on: bool) -> None:
@@ -594,3 +664,293 @@ class TopkCall:
         _check(lib().sparcml_topk_sparsify(
             self.P, _ptr(self.x), self.N, self.k, _ptr(self.idx), _ptr(self.val), self.res_ptr,
             _ptr(self.ws), self.ws.numel(), _stream_ptr(self.x.device)), "sparcml_topk_sparsify")
+
+
+# ---------------------------------------------------------------------------
+# Training operators: the losses that a gradient comes from, the update that
+# the summed gradient goes into.
+
+STATE_BLOCK = 256  # elements that share a scale (8-bit moments)
+
+
+def _type_id(t, name: str) -> int:
+    torch = _torch()
+    ids = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if t.dtype not in ids:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16")
+    return ids[t.dtype]
+
+
+def _require(t, name: str, dtype, numel: int, device) -> None:
+    _require_cuda(t, name)
+    if t.dtype != dtype or t.numel() != numel or t.device != device:
+        raise ValueError(f"{name} must hold {numel} {dtype} entries on {device}")
+
+
+def adamw_state(params, state_bits: int = 32):
+    """Moments of a model at the start of training: (m, v) lists of fp32
+    tensors, or (m, v, m_scale, v_scale) with E4M3 codes and a scale per 256
+    elements (``state_bits`` 8), all zero."""
+    torch = _torch()
+    if state_bits == 32:
+        return [torch.zeros_like(p) for p in params], [torch.zeros_like(p) for p in params]
+    if state_bits != 8:
+        raise ValueError("state_bits must be 8 or 32")
+    codes = lambda: [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)  # noqa: E731
+                     for p in params]
+    scales = lambda: [torch.zeros(-(-p.numel() // STATE_BLOCK), device=p.device) for p in params]  # noqa: E731
+    return codes(), codes(), scales(), scales()
+
+
+class _TensorPlan:
+    """A prepared plan of a model's tensors and its workspace."""
+
+    def __init__(self, grads, state_bits=0, copy_type=BF16, fill=None):
+        torch = _torch()
+        if not grads:
+            raise ValueError("no tensors")
+        self.dev = grads[0].device
+        gtype = _type_id(grads[0], "grads[0]")
+        arr = (Tensor * len(grads))()
+        total = 0
+        for t, g in enumerate(grads):
+            _require_cuda(g, f"grads[{t}]")
+            if g.dtype != grads[0].dtype or g.device != self.dev:
+                raise ValueError(f"grads[{t}] must have the type and device of grads[0]")
+            arr[t].grad, arr[t].n, arr[t].lr_scale = _ptr(g), g.numel(), 1.0
+            total += g.numel()
+            if fill:
+                fill(arr[t], t, g.numel())
+        self.plan = Tensors()
+        self.ws = alloc_workspace(workspace_size(OP_TENSORS, len(grads), total, 0), self.dev)
+        _check(lib().sparcml_tensors_prepare(len(grads), arr, gtype, copy_type, state_bits, ctypes.byref(self.plan),
+                                             _ptr(self.ws), self.ws.numel(), _stream_ptr(self.dev)),
+               "sparcml_tensors_prepare")
+        self.out = torch.empty(2, dtype=torch.float32, device=self.dev)
+
+    def _norm(self, max_norm, grad_scale):
+        _check(lib().sparcml_grad_norm(ctypes.byref(self.plan), grad_scale, max_norm, self.out.data_ptr(),
+                                       _stream_ptr(self.dev)), "sparcml_grad_norm")
+
+
+class GradNormCall(_TensorPlan):
+    """Repeated norm of a list of gradients (fp32, bf16 or fp16, one type):
+    run() fills ``out`` (device fp32 [2]) with the norm and the factor
+    min(1, max_norm / norm) that clips it (0 if the norm is not finite)."""
+
+    def __init__(self, grads):
+        super().__init__(grads)
+        self._keep = grads
+
+    def run(self, max_norm: float = float("inf"), grad_scale: float = 1.0) -> None:
+        self._norm(max_norm, grad_scale)
+
+
+def grad_norm(grads, max_norm: float = float("inf"), grad_scale: float = 1.0):
+    """Norm of all gradients and the factor that clips it (device fp32 [2])."""
+    c = GradNormCall(grads)
+    c.run(max_norm, grad_scale)
+    return c.out
+
+
+class AdamwCall(_TensorPlan):
+    """AdamW over a fixed set of tensors.  ``params``, ``grads``, ``m``, ``v``:
+    lists of contiguous tensors (fp32 weights; fp32, bf16 or fp16 gradients;
+    moments fp32, or one-byte codes with ``m_scale`` / ``v_scale``, as
+    adamw_state makes them).  ``copies``: tensors of one 16-bit type that
+    receive the new weights, or None (for all, or for a tensor).  ``decay``,
+    ``lr_scale``: a number, or one for each tensor."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None, decay=0.0, lr_scale=1.0):
+        torch = _torch()
+        count = len(grads)
+        bits = 8 if m_scale is not None else 32
+        lists = {"params": params, "m": m, "v": v, "copies": copies, "m_scale": m_scale, "v_scale": v_scale}
+        if (m_scale is None) != (v_scale is None):
+            raise ValueError("m_scale and v_scale go together")
+        for name, x in lists.items():
+            if x is not None and len(x) != count:
+                raise ValueError(f"{name} must hold {count} tensors")
+        per = lambda x: [float(x)] * count if isinstance(x, (int, float)) else [float(y) for y in x]  # noqa: E731
+        decay, lr_scale = per(decay), per(lr_scale)
+        if len(decay) != count or len(lr_scale) != count:
+            raise ValueError(f"decay and lr_scale must hold {count} numbers")
+        dev = grads[0].device if count else None
+        given = [c for c in copies or [] if c is not None]
+        ctype = _type_id(given[0], "copies") if given else BF16
+        if ctype == F32:
+            raise ValueError("copies must be bfloat16 or float16")
+
+        def moment(x, name, n):
+            _require_cuda(x, name)
+            ok = x.dtype == torch.float32 if bits == 32 else x.dtype in (torch.uint8, torch.float8_e4m3fn)
+            if not ok or x.numel() != n or x.device != dev:
+                raise ValueError(f"{name} must hold {n} {'fp32 moments' if bits == 32 else 'E4M3 codes'} on {dev}")
+
+        def fill(a, t, n):
+            _require(params[t], f"params[{t}]", torch.float32, n, dev)
+            moment(m[t], f"m[{t}]", n)
+            moment(v[t], f"v[{t}]", n)
+            a.param, a.m, a.v = _ptr(params[t]), _ptr(m[t]), _ptr(v[t])
+            if bits == 8:
+                for name, x in (("m_scale", m_scale[t]), ("v_scale", v_scale[t])):
+                    _require(x, f"{name}[{t}]", torch.float32, -(-n // STATE_BLOCK), dev)
+                a.m_scale, a.v_scale = _ptr(m_scale[t]), _ptr(v_scale[t])
+            if copies is not None and copies[t] is not None:
+                _require(copies[t], f"copies[{t}]", given[0].dtype, n, dev)
+                a.copy = _ptr(copies[t])
+            a.decay, a.lr_scale = decay[t], lr_scale[t]
+
+        super().__init__(grads, bits, ctype, fill)
+        self.args = AdamwArgs()
+        self._keep = (params, grads, m, v, m_scale, v_scale, copies)
+
+    def grad_norm(self, max_norm: float = float("inf"), grad_scale: float = 1.0):
+        """Norm of the gradients and the factor that clips it, in ``out``
+        (device fp32 [2]), for run's ``clip``."""
+        self._norm(max_norm, grad_scale)
+        return self.out
+
+    def run(self, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+            grad_scale: float = 1.0, clip=None, seed: int = 0) -> None:
+        """Step number ``step`` (from 1 on), in place.  ``clip``: a device
+        tensor as grad_norm fills it, or None."""
+        if clip is not None:
+            _require(clip, "clip", _torch().float32, 2, self.dev)
+        if not 1 <= step < 2**32:
+            raise ValueError("step must be in [1, 2^32)")
+        a = self.args
+        a.lr, a.beta1, a.beta2, a.eps, a.grad_scale = lr, beta1, beta2, eps, grad_scale
+        a.seed, a.step = seed & (2**64 - 1), step
+        _check(lib().sparcml_adamw(ctypes.byref(self.plan), ctypes.byref(a), _ptr(clip), _stream_ptr(self.dev)),
+               "sparcml_adamw")
+
+
+class _LogitsCall:
+    def __init__(self, logits, labels, scale, op, pairs=1):
+        torch = _torch()
+        if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+            raise ValueError("logits must be a CUDA (HIP) tensor")
+        if logits.dim() != 2 or not logits.numel() or (logits.stride(1) != 1 and logits.shape[1] > 1):
+            raise ValueError("logits must be a 2-D tensor with adjacent columns")
+        self.rows, self.vocab = logits.shape
+        self.dev = logits.device
+        ld = logits.stride(0) if self.rows > 1 else self.vocab
+        _require(labels, "labels", torch.int32, self.rows, self.dev)
+        self.logits = Logits(logits.data_ptr(), _ptr(labels), self.rows, self.vocab, ld, _type_id(logits, "logits"),
+                             scale)
+        self.ws = alloc_workspace(workspace_size(op, pairs, self.rows, self.vocab), self.dev)
+        self.logp = torch.empty(self.rows, dtype=torch.float32, device=self.dev)
+        self._keep = [logits, labels]
+
+    def _per_row(self, t, name):
+        if t is not None:
+            _require(t, name, _torch().float32, self.rows, self.dev)
+            self._keep.append(t)
+        return _ptr(t)
+
+    def _gradient(self, dlogits):
+        """Place of the gradient: a new tensor, "inplace", None or a tensor."""
+        torch = _torch()
+        logits = self._keep[0]
+        if isinstance(dlogits, str):
+            if dlogits not in ("new", "inplace"):
+                raise ValueError("dlogits must be 'new', 'inplace', None or a tensor")
+            dlogits = logits if dlogits == "inplace" else torch.empty(self.rows, self.vocab, dtype=logits.dtype,
+                                                                      device=self.dev)
+        if dlogits is not None:
+            if (dlogits.shape != logits.shape or dlogits.dtype != logits.dtype or dlogits.device != self.dev
+                    or (dlogits.stride(1) != 1 and self.vocab > 1)):
+                raise ValueError("dlogits must have the logits' shape, type and adjacent columns")
+            self._ldd = dlogits.stride(0) if self.rows > 1 else self.vocab
+        else:
+            self._ldd = 0
+        self.dlogits = dlogits
+        self.stats = torch.empty(4, dtype=torch.float32, device=self.dev)
+
+
+class TokenLogprobCall(_LogitsCall):
+    """Repeated log probability of each row's token: logits [T, V] (fp32, bf16
+    or fp16, rows at any stride), labels int32 [T] (outside [0, V): no token);
+    run() fills ``logp`` and ``lse`` (fp32 [T]; 0 without a token)."""
+
+    def __init__(self, logits, labels, scale: float = 1.0):
+        super().__init__(logits, labels, scale, OP_LOGPROB)
+        self.lse = _torch().empty_like(self.logp)
+
+    def run(self) -> None:
+        _check(lib().sparcml_token_logprob(ctypes.byref(self.logits), _ptr(self.logp), _ptr(self.lse), _ptr(self.ws),
+                                           self.ws.numel(), _stream_ptr(self.dev)), "sparcml_token_logprob")
+
+
+def token_logprob(logits, labels, scale: float = 1.0):
+    """Log probability of each row's token under softmax(scale * logits) and
+    the rows' log sums: (logp, lse), fp32 [T]."""
+    c = TokenLogprobCall(logits, labels, scale)
+    c.run()
+    return c.logp, c.lse
+
+
+class PolicyLossCall(_LogitsCall):
+    """Repeated clipped policy loss with a KL term.  ``old``, ``adv``,
+    ``weight``, ``ref`` (or None): fp32 [T]; a row of weight 0 counts for
+    nothing and is not read.  run() fills ``stats`` (loss, its clipped part,
+    KL, clipped share), ``logp`` and ``dlogits`` ("new", "inplace": the
+    logits' own place, a tensor, or None: forward only)."""
+
+    def __init__(self, logits, labels, old, adv, weight, ref=None, clip_lo: float = 0.2, clip_hi: float = 0.2,
+                 kl: float = 0.0, scale: float = 1.0, grad_scale: float = 1.0, dlogits="new"):
+        super().__init__(logits, labels, scale, OP_POLICY)
+        if old is None or adv is None or weight is None:
+            raise ValueError("old, adv and weight must be given")
+        self.args = PolicyArgs(self._per_row(old, "old"), self._per_row(ref, "ref"), self._per_row(adv, "adv"),
+                               self._per_row(weight, "weight"), clip_lo, clip_hi, kl, grad_scale)
+        self._gradient(dlogits)
+
+    def run(self) -> None:
+        _check(lib().sparcml_policy_loss(ctypes.byref(self.logits), ctypes.byref(self.args), _ptr(self.logp),
+                                         _ptr(self.stats), _ptr(self.dlogits), self._ldd, _ptr(self.ws),
+                                         self.ws.numel(), _stream_ptr(self.dev)), "sparcml_policy_loss")
+
+
+def policy_loss(logits, labels, old, adv, weight, **more):
+    """One clipped policy loss and its gradient (see PolicyLossCall):
+    dict(stats, logp, dlogits)."""
+    c = PolicyLossCall(logits, labels, old, adv, weight, **more)
+    c.run()
+    return {"stats": c.stats, "logp": c.logp, "dlogits": c.dlogits}
+
+
+class PreferenceLossCall(_LogitsCall):
+    """Repeated loss of paired log ratios.  ``bounds``: row numbers at which
+    the 2 * pairs sequences begin, and the end (of pair b, sequence 2b is the
+    preferred one); ``ref``: fp32 [T] or None.  run() fills ``stats`` (loss,
+    share of pairs in order, mean rewards of the preferred and the others),
+    ``logp`` and ``dlogits`` (as PolicyLossCall)."""
+
+    def __init__(self, logits, labels, bounds, ref=None, beta: float = 0.1, smoothing: float = 0.0,
+                 scale: float = 1.0, grad_scale: float = 1.0, dlogits="new"):
+        if len(bounds) < 3 or len(bounds) % 2 == 0:
+            raise ValueError("bounds must hold 2 * pairs + 1 row numbers")
+        self.pairs = len(bounds) // 2
+        super().__init__(logits, labels, scale, OP_PREFERENCE, self.pairs)
+        if any(int(b) < 0 for b in bounds):
+            raise ValueError("bounds must not be negative")
+        self.bounds = (ctypes.c_uint64 * len(bounds))(*[int(b) for b in bounds])
+        self.ref = self._per_row(ref, "ref")
+        self.rates = (beta, smoothing, grad_scale)
+        self._gradient(dlogits)
+
+    def run(self) -> None:
+        _check(lib().sparcml_preference_loss(ctypes.byref(self.logits), self.pairs, self.bounds, self.ref, *self.rates,
+                                             _ptr(self.logp), _ptr(self.stats), _ptr(self.dlogits), self._ldd,
+                                             _ptr(self.ws), self.ws.numel(), _stream_ptr(self.dev)),
+               "sparcml_preference_loss")
+
+
+def preference_loss(logits, labels, bounds, **more):
+    """One loss of paired log ratios and its gradient (see
+    PreferenceLossCall): dict(stats, logp, dlogits)."""
+    c = PreferenceLossCall(logits, labels, bounds, **more)
+    c.run()
+    return {"stats": c.stats, "logp": c.logp, "dlogits": c.dlogits}
