@@ -2,13 +2,18 @@
 // clipped policy loss with a KL term, loss of paired log ratios, and their
 // gradients.
 //
-// With x the row's logits, M their maximum, s the inverse temperature and
-// Z = sum_v exp(s (x_v - M)): the token's log probability is s (x_label - M)
-// - log Z, and for a loss whose derivative by it is q the gradient is
-// s q ([v == label] - exp(s (x_v - M)) / Z).  A pass over the rows finds M and
-// Z (one read, running maximum and sum), a second writes the gradient.  Rows
-// are cut into slices, a workgroup each, whose (M, Z) are joined by whoever
-// reads them.
+// With x the row's logits, M their maximum, s the inverse temperature, c = s
+// log2(e) and Z = sum_v 2^(c (x_v - M)): the token's log probability is ln 2
+// (c (x_label - M) - log2 Z), and for a loss whose derivative by it is q the
+// gradient is s q ([v == label] - 2^(c (x_v - M)) / Z).  The difference is
+// taken first (c x - c M in one fused multiply-add would overflow where all of
+// a row is masked by the type's lowest value).
+//
+// Many rows: a workgroup a row, the row in registers between the passes over
+// it, so that the logits are read once even where the gradient follows
+// (k_row).  Few rows, or rows beyond the registers: slices of rows, a
+// workgroup each, whose (M, Z) are joined by whoever reads them (k_slices,
+// then the gradient by slices again).
 #include "internal.h"
 #include "types_device.h"
 
@@ -17,120 +22,117 @@
 namespace sparcml {
 namespace {
 
-constexpr uint32_t kStep = 2048;       // elements a workgroup takes at a time
 constexpr float kLog2e = 1.44269504088896341f;
-
-// Maximum of a part of a row and the sum of 2^(c (x - max)) over it;
-// nothing (or nothing but -Inf): (-Inf, 0).
-struct Part {
-    float top, sum;
-};
+constexpr float kLn2 = 0.693147180559945309f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// What a part's sum counts for under the maximum `top`.
-__device__ __forceinline__ float rescaled(Part p, float top, float c)
-{
-    return p.sum == 0.0f ? 0.0f : p.sum * exp2_fast((p.top - top) * c);
-}
+// ---------------------------------------------------------------- rows
 
-__device__ __forceinline__ Part join(Part a, Part b, float c)
-{
-    Part r;
-    r.top = fmaxf(a.top, b.top);
-    r.sum = rescaled(a, r.top, c) + rescaled(b, r.top, c);
-    return r;
-}
+// 16 bytes of a row.
+template <int TYPE>
+struct Piece {
+    typedef typename Elem<TYPE>::type E;
+    static constexpr int N = TYPE == kF32 ? 4 : 8;  // elements
+    // A word of a piece that holds nothing but -Inf.
+    static constexpr uint32_t kNone = TYPE == kF32 ? 0xFF800000u : TYPE == kBf16 ? 0xFF80FF80u : 0xFC00FC00u;
+    u32x4 w;
+    __device__ __forceinline__ float get(int i) const
+    {
+        if (TYPE == kF32) return __uint_as_float(w[i]);
+        if (TYPE == kBf16) return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]));
+    }
+    // The elements rounded to nearest.
+    __device__ __forceinline__ void put(const float* x)
+    {
+        E y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = (E)x[i];
+        w = __builtin_bit_cast(u32x4, y);
+    }
+    __device__ __forceinline__ void none() { w = u32x4{kNone, kNone, kNone, kNone}; }
+    // Keeps the compiler from carrying the unpacked values from one pass to
+    // the next (twice to four times the registers).
+    __device__ __forceinline__ void repack() { asm volatile("" : "+v"(w)); }
+};
 
-__device__ __forceinline__ Part join_slices(const Part* part, uint32_t S, float c)
-{
-    Part r = part[0];
-    for (uint32_t i = 1; i < S; ++i) r = join(r, part[i], c);
-    return r;
-}
+// Where a row's pieces lie: from its first 128-byte line on (a wave's accesses
+// then take whole lines; the gradient, at the same distance from a line where
+// rows and strides agree, leaves none half written), `head` elements in front
+// of them, the rest behind.  Single i (head and rest) is element single(i).
+constexpr uint32_t kLine = 128;
+template <int TYPE>
+struct RowCut {
+    static constexpr uint32_t N = Piece<TYPE>::N, kHeads = N * (kLine / 16);  // elements of a line
+    static constexpr uint32_t kSingles = kHeads + N - 2;                      // singles at most
+    uint32_t head, full, singles;
+    __device__ __forceinline__ RowCut(const void* row, uint32_t V)
+    {
+        head = min(V, (uint32_t)((0 - reinterpret_cast<uintptr_t>(row)) / (16 / N)) % kHeads);
+        full = (V - head) / N;
+        singles = V - full * N;
+    }
+    __device__ __forceinline__ uint32_t piece(uint32_t j) const { return head + j * N; }
+    __device__ __forceinline__ uint32_t single(uint32_t i) const { return i < head ? i : i + full * N; }
+    __device__ __forceinline__ bool in_piece(uint32_t v) const { return v >= head && (v - head) / N < full; }
+};
+constexpr uint32_t kMinThreads = 128;  // a thread for each single
 
 __device__ __forceinline__ bool has_token(const Logits& in, uint64_t t)
 {
     return (uint32_t)in.label[t] < (uint32_t)in.vocab;
 }
-
-// Eight elements of a row from v on as fp32, -Inf past the end.
-template <int TYPE>
-__device__ __forceinline__ void get8(const typename Elem<TYPE>::type* row, uint64_t v, uint64_t end, float* x)
+// Whether a row is read at all.
+__device__ __forceinline__ bool in_use(const Logits& in, const float* weight, uint64_t t)
 {
-    if (v + 8 <= end) {
-        const f32x4 a = __builtin_convertvector(load4<typename Elem<TYPE>::vec4>(row + v), f32x4);
-        const f32x4 b = __builtin_convertvector(load4<typename Elem<TYPE>::vec4>(row + v + 4), f32x4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = a[i];
-            x[4 + i] = b[i];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = v + i < end ? (float)row[v + i] : -INFINITY;
-    }
+    return has_token(in, t) && !(weight && weight[t] == 0.0f);
 }
 
-// (M, Z) of every slice of every row in use; the token's logit beside them.
+// M of a part of a row and the sum of 2^(c (x - M)) over it; nothing (or
+// nothing but -Inf): (0, 0).
+struct Part {
+    float top, sum;
+};
+
+// The parts of a row's S slices joined by a group of g lanes (g a power of two
+// up to 64, S <= g; every lane of the wave takes part).
+__device__ __forceinline__ Part join_slices(const Part* part, uint32_t S, uint32_t g, float c)
+{
+    const uint32_t i = threadIdx.x & (g - 1);
+    const Part p = i < S ? part[i] : Part{0.0f, 0.0f};
+    float top = p.sum == 0.0f ? -INFINITY : p.top;  // (without a sum, top means nothing)
+    for (uint32_t o = 1; o < g; o <<= 1) top = fmaxf(top, __shfl_xor(top, (int)o));
+    if (top == -INFINITY) top = 0.0f;
+    float sum = p.sum == 0.0f ? 0.0f : p.sum * exp2_fast((p.top - top) * c);
+    for (uint32_t o = 1; o < g; o <<= 1) sum += __shfl_xor(sum, (int)o);
+    return Part{top, sum};
+}
+
+__device__ __forceinline__ float part_logp(Part p, float x, float c)
+{
+    return p.sum == 0.0f ? -INFINITY : ((x - p.top) * c - log2f(p.sum)) * kLn2;
+}
+__device__ __forceinline__ float part_lse(Part p, float scale)
+{
+    return p.sum == 0.0f ? -INFINITY : p.top * scale + log2f(p.sum) * kLn2;
+}
+
+// One gradient entry before the label's own term.
+__device__ __forceinline__ float entry(float x, float c, float top, float k) { return k * exp2_fast((x - top) * c); }
+
+// Zeros in the row of the calling workgroup.
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_rows(Logits in, const float* weight, uint32_t S, uint64_t W, float c,
-                                              Part* part, float* at_label)
+__device__ __forceinline__ void clear_row(typename Elem<TYPE>::type* out, uint32_t V)
 {
     typedef typename Elem<TYPE>::type E;
-    __shared__ Part s_p[4];
-    for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
-        const uint64_t t = b / S, lo = (b % S) * W, end = min(lo + W, in.vocab);
-        if (!has_token(in, t) || (weight && weight[t] == 0.0f)) continue;
-        const E* row = static_cast<const E*>(in.x) + t * in.ld;
-        Part p = {-INFINITY, 0.0f};
-        for (uint64_t v = lo + threadIdx.x * 8; v < end; v += kStep) {
-            float x[8];
-            get8<TYPE>(row, v, end, x);
-            float top = p.top;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
-            const float base = top == -INFINITY ? 0.0f : top;
-            float sum = p.sum * exp2_fast((p.top - base) * c);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += exp2_fast((x[i] - base) * c);
-            p.top = top;
-            p.sum = sum;
-        }
-        for (int o = 1; o < 64; o <<= 1) {
-            const Part q = {__shfl_xor(p.top, o), __shfl_xor(p.sum, o)};
-            p = join(p, q, c);
-        }
-        if ((threadIdx.x & 63) == 0) s_p[threadIdx.x >> 6] = p;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            part[b] = join(join(s_p[0], s_p[1], c), join(s_p[2], s_p[3], c), c);
-            if (lo == 0) at_label[t] = (float)row[in.label[t]];
-        }
-        __syncthreads();
-    }
+    const RowCut<TYPE> r(out, V);
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    for (uint32_t j = threadIdx.x; j < r.full; j += blockDim.x) store_vec(out + r.piece(j), zero);
+    for (uint32_t i = threadIdx.x; i < r.singles; i += blockDim.x) out[r.single(i)] = (E)0.0f;
 }
 
-// Log probability and log sum of a row from its joined part.
-__device__ __forceinline__ float row_logp(Part p, float x, float scale)
-{
-    return p.sum == 0.0f ? -INFINITY : (x - p.top) * scale - logf(p.sum);
-}
-
-__global__ void __launch_bounds__(256) k_logprob(Logits in, uint32_t S, float c, const Part* part,
-                                                 const float* at_label, float* logp, float* lse)
-{
-    for (uint64_t t = (uint64_t)blockIdx.x * 256 + threadIdx.x; t < in.rows; t += (uint64_t)gridDim.x * 256) {
-        float lp = 0.0f, l = 0.0f;
-        if (has_token(in, t)) {
-            const Part p = join_slices(part + t * S, S, c);
-            lp = row_logp(p, at_label[t], in.scale);
-            l = p.sum == 0.0f ? -INFINITY : p.top * in.scale + logf(p.sum);
-        }
-        logp[t] = lp;
-        if (lse) lse[t] = l;
-    }
-}
+// ---------------------------------------------------------------- policy terms
 
 // One token of the policy loss: its terms and the loss' derivative by its
 // log probability (both before the weight).
@@ -155,124 +157,356 @@ __device__ __forceinline__ PolicyToken policy_token(const PolicyArgs& a, uint64_
     return r;
 }
 
-__device__ __forceinline__ double block_sum(double x, double* s_w)
+// Sums of `count` numbers over a workgroup, in every thread (fixed order).
+__device__ __forceinline__ void block_sum(double* x, double (*s_w)[4], int count)
 {
-    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+    for (int o = 1; o < 64; o <<= 1)
+        for (int i = 0; i < count; ++i) x[i] += __shfl_xor(x[i], o);
+    if ((threadIdx.x & 63) == 0)
+        for (int i = 0; i < count; ++i) s_w[threadIdx.x >> 6][i] = x[i];
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
-}
-
-// Elements [lo, end) of a gradient row: coef ([v == label] - 2^(c (x - M)) / Z),
-// zeros where coef is 0 (the logits are then not read).
-template <int TYPE>
-__device__ __forceinline__ void grad_slice(const typename Elem<TYPE>::type* row, typename Elem<TYPE>::type* out,
-                                           uint64_t lo, uint64_t end, uint32_t label, float coef, Part p, float c)
-{
-    typedef typename Elem<TYPE>::type E;
-    typedef typename Elem<TYPE>::vec4 V;
-    const bool none = coef == 0.0f || p.sum == 0.0f;
-    const float k = -coef / p.sum;
-    for (uint64_t v = lo + threadIdx.x * 8; v < end; v += kStep) {
-        float x[8];
-        if (none) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-        } else {
-            get8<TYPE>(row, v, end, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = k * exp2_fast((x[i] - p.top) * c);
-                if (v + i == label) x[i] += coef;
-            }
-        }
-        if (v + 8 <= end) {
-            const f32x4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
-            store4(out + v, __builtin_convertvector(a, V));
-            store4(out + v + 4, __builtin_convertvector(b, V));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (v + i < end) out[v + i] = (E)x[i];
-        }
+    for (int i = 0; i < count; ++i) {
+        x[i] = s_w[0][i];
+        for (uint32_t q = 1; q < blockDim.x >> 6; ++q) x[i] += s_w[q][i];
     }
 }
 
-// Workgroup 0: every token's log probability and the sums over tokens; the
-// others a slice of the gradient each.
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_policy(Logits in, PolicyArgs a, uint32_t S, uint64_t W, float c,
-                                                const Part* part, const float* at_label, float* logp, float* stats,
-                                                void* dlogits, uint64_t ldd)
+// What one token adds to the sums over tokens: gain, KL, clipped.
+__device__ __forceinline__ void add_token(const PolicyArgs& a, uint64_t t, float lp, double* x)
+{
+    const double w = (double)a.weight[t];
+    const PolicyToken r = policy_token(a, t, lp);
+    x[0] += w * (double)r.gain;
+    x[1] += w * (double)r.k;
+    x[2] += r.clipped ? w : 0.0;
+}
+
+__device__ __forceinline__ void put_policy_stats(const PolicyArgs& a, double* x, double (*s_w)[4], float* stats)
+{
+    block_sum(x, s_w, 3);
+    if (threadIdx.x == 0) {
+        stats[0] = (float)((a.ref_logp ? (double)a.kl * x[1] : 0.0) - x[0]);
+        stats[1] = (float)-x[0];
+        stats[2] = (float)x[1];
+        stats[3] = (float)x[2];
+    }
+}
+
+// The sums over tokens, their log probabilities given.
+__global__ void __launch_bounds__(1024) k_policy_stats(Logits in, PolicyArgs a, const float* logp, float* stats)
+{
+    __shared__ double s_w[16][4];
+    double x[3] = {0.0, 0.0, 0.0};
+    for (uint64_t t = threadIdx.x; t < in.rows; t += 1024)
+        if (in_use(in, a.weight, t)) add_token(a, t, logp[t], x);
+    put_policy_stats(a, x, s_w, stats);
+}
+
+// ---------------------------------------------------------------- a workgroup a row
+
+template <bool SUM>
+__device__ __forceinline__ float join_waves(float x, float* s)
+{
+    x = wave_join<SUM>(x);
+    if (blockDim.x == 64) return x;
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = s[0];
+    for (uint32_t i = 1; i < blockDim.x >> 6; ++i) x = SUM ? x + s[i] : fmaxf(x, s[i]);
+    return x;
+}
+
+// What a thread has of its row so far: the maximum and the sum against it.
+struct Own {
+    float top, sum;
+    template <int TYPE, int U>
+    __device__ __forceinline__ void add(Piece<TYPE> (&x)[U], float c)
+    {
+        float high = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < Piece<TYPE>::N; ++i) high = fmaxf(high, x[u].get(i));
+        const float base = high == -INFINITY ? 0.0f : high;
+        float more[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u].repack();
+#pragma unroll
+            for (int i = 0; i < Piece<TYPE>::N; ++i) more[i & 3] += exp2_fast((x[u].get(i) - base) * c);
+        }
+        sum = sum * exp2_fast((top - base) * c) + ((more[0] + more[1]) + (more[2] + more[3]));
+        top = high;
+    }
+};
+
+// Row blockIdx.x by one workgroup: the first NV pieces of a thread stay in
+// registers between the two passes over them, the rest of a longer row is
+// read once more (mostly from the cache), the singles one a thread.  Writes
+// the log probability, lse and part where wanted, and with GRAD the gradient
+// of the policy loss.
+template <int TYPE, int THREADS, int NV, bool GRAD>
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
+k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
-    __shared__ double s_w[4];
-    if (blockIdx.x == 0) {
-        double gain = 0.0, k = 0.0, clipped = 0.0;
-        for (uint64_t t = threadIdx.x; t < in.rows; t += 256) {
-            const float w = a.weight[t];
-            float lp = 0.0f;
-            if (has_token(in, t) && w != 0.0f) {
-                lp = row_logp(join_slices(part + t * S, S, c), at_label[t], in.scale);
-                const PolicyToken r = policy_token(a, t, lp);
-                gain += (double)w * (double)r.gain;
-                k += (double)w * (double)r.k;
-                clipped += r.clipped ? (double)w : 0.0;
-            }
-            logp[t] = lp;
+    constexpr int N = Piece<TYPE>::N, U = 2;
+    __shared__ float s_top[THREADS / 64], s_sum[THREADS / 64], s_x, s_coef;
+    const uint64_t t = blockIdx.x;
+    const uint32_t V = (uint32_t)in.vocab, label = (uint32_t)in.label[t], tid = threadIdx.x, step = blockDim.x;
+    const E* row = static_cast<const E*>(in.x) + t * in.ld;
+    E* out = static_cast<E*>(dlogits) + t * ldd;
+    if (!in_use(in, a.weight, t)) {
+        if (tid == 0) {
+            logp[t] = 0.0f;
+            if (lse) lse[t] = 0.0f;
         }
-        gain = block_sum(gain, s_w);
-        k = block_sum(k, s_w);
-        clipped = block_sum(clipped, s_w);
-        if (threadIdx.x == 0) {
-            stats[0] = (float)((a.ref_logp ? (double)a.kl * k : 0.0) - gain);
-            stats[1] = (float)-gain;
-            stats[2] = (float)k;
-            stats[3] = (float)clipped;
-        }
+        if (GRAD) clear_row<TYPE>(out, V);
         return;
     }
-    for (uint64_t b = blockIdx.x - 1; b < in.rows * S; b += gridDim.x - 1) {
-        const uint64_t t = b / S, lo = (b % S) * W, end = min(lo + W, in.vocab);
-        const float w = a.weight[t];
+    const RowCut<TYPE> r(row, V);
+    Piece<TYPE> x[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        x[j].none();
+        if (tid + step * j < r.full) x[j].w = load_vec<u32x4>(row + r.piece(tid + step * j));
+    }
+    const float single = tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
+    if (tid == 0) s_x = (float)row[label];
+    Own own = {single, single == -INFINITY ? 0.0f : 1.0f};
+    for (uint32_t j = tid + step * NV; j < r.full; j += step * U) {
+        Piece<TYPE> y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            y[u].none();
+            if (j + step * u < r.full) y[u].w = load_keep<u32x4>(row + r.piece(j + step * u));
+        }
+        own.add(y, c);
+    }
+    own.add(x, c);
+    float top = join_waves<false>(own.top, s_top);
+    if (top == -INFINITY) top = 0.0f;
+    const Part p = {top, join_waves<true>(own.sum * exp2_fast((own.top - top) * c), s_sum)};
+    if (tid == 0) {
+        const float lp = part_logp(p, s_x, c);
+        logp[t] = lp;
+        if (lse) lse[t] = part_lse(p, in.scale);
+        if (part) part[t] = p;
+        if (GRAD) s_coef = p.sum == 0.0f ? 0.0f : a.grad_scale * in.scale * (a.weight[t] * policy_token(a, t, lp).coef);
+    }
+    if (!GRAD) return;
+    uint32_t j = tid + step * NV;
+    Piece<TYPE> next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (j + step * u < r.full) next[u].w = load_vec<u32x4>(row + r.piece(j + step * u));
+    __syncthreads();
+    const float coef = s_coef, xl = s_x;
+    const float k = coef == 0.0f ? 0.0f : -coef / p.sum;
+    auto write = [&](Piece<TYPE>& q, uint32_t at) {
+        q.repack();
+        float y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = entry(q.get(i), c, top, k);
+        q.put(y);
+        if (at < r.full) store_vec(out + r.piece(at), q.w);
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) write(x[i], tid + step * i);
+    while (j < r.full) {
+        Piece<TYPE> now[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            now[u] = next[u];
+            if (j + step * (U + u) < r.full) next[u].w = load_vec<u32x4>(row + r.piece(j + step * (U + u)));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) write(now[u], j + step * u);
+        j += step * U;
+    }
+    if (tid < r.singles) out[r.single(tid)] = (E)entry(single, c, top, k);
+    // the label's own entry once more, by the thread that has just written it
+    const bool mine = r.in_piece(label) ? (label - r.head) / N % step == tid
+                                        : tid < r.singles && r.single(tid) == label;
+    if (mine) out[label] = (E)(entry(xl, c, top, k) + coef);
+}
+
+// ---------------------------------------------------------------- slices of rows
+
+// Slice s of a row: pieces [s W, (s + 1) W); slice 0 takes the singles too.
+// (M, Z) of every slice of every row in use, the token's logit beside them;
+// with one slice a row its log probability (and lse) at once.
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, uint32_t S, uint32_t W, float c,
+                                                Part* part, float* at_label, float* logp, float* lse)
+{
+    typedef typename Elem<TYPE>::type E;
+    __shared__ float s_top[4], s_sum[4];
+    for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
+        const uint64_t t = b / S;
+        const uint32_t s = (uint32_t)(b % S);
+        if (!in_use(in, weight, t)) {
+            if (S == 1 && threadIdx.x == 0) {
+                logp[t] = 0.0f;
+                if (lse) lse[t] = 0.0f;
+            }
+            continue;
+        }
+        const E* row = static_cast<const E*>(in.x) + t * in.ld;
+        const RowCut<TYPE> r(row, (uint32_t)in.vocab);
+        const uint32_t end = (uint32_t)min((uint64_t)r.full, (uint64_t)(s + 1) * W);
+        const float single = s == 0 && threadIdx.x < r.singles ? (float)row[r.single(threadIdx.x)] : -INFINITY;
+        const float at = threadIdx.x == 0 && s == 0 ? (float)row[in.label[t]] : 0.0f;
+        Own own = {single, single == -INFINITY ? 0.0f : 1.0f};
+        for (uint32_t j = s * W + threadIdx.x; j < end; j += 1024) {
+            Piece<TYPE> x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                x[u].none();
+                if (j + 256 * u < end) x[u].w = load_vec<u32x4>(row + r.piece(j + 256 * u));
+            }
+            own.add(x, c);
+        }
+        float high = join_waves<false>(own.top, s_top);
+        if (high == -INFINITY) high = 0.0f;
+        const float sum = join_waves<true>(own.sum * exp2_fast((own.top - high) * c), s_sum);
+        if (threadIdx.x == 0) {
+            const Part p = {high, sum};
+            part[b] = p;
+            if (s == 0) at_label[t] = at;
+            if (S == 1) {
+                logp[t] = part_logp(p, at, c);
+                if (lse) lse[t] = part_lse(p, in.scale);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Calls f(t, lp, p) for rows first, first + 1, ... below end from one workgroup of 256
+// threads, by the first lane of each row's group; lp and p are those of a row
+// in use.
+template <class F>
+__device__ __forceinline__ void each_joined(const Logits& in, const float* weight, uint64_t first, uint64_t end,
+                                            uint32_t S, uint32_t g, float c, const Part* part, const float* at_label,
+                                            F f)
+{
+    for (uint64_t t0 = first; t0 < end; t0 += 256 / g) {
+        const uint64_t t = t0 + threadIdx.x / g;
+        const bool use = t < end && in_use(in, weight, t);
+        const Part p = join_slices(part + (use ? t * S : 0), use ? S : 0, g, c);
+        if (t < end && (threadIdx.x & (g - 1)) == 0) f(t, use, use ? part_logp(p, at_label[t], c) : 0.0f, p);
+    }
+}
+
+// Log probabilities from the slices, 256 / g rows a workgroup.
+__global__ void __launch_bounds__(256) k_join(Logits in, const float* weight, uint32_t S, uint32_t g, float c,
+                                              const Part* part, const float* at_label, float* logp, float* lse)
+{
+    const uint32_t rows = 256 / g;
+    for (uint64_t t0 = (uint64_t)blockIdx.x * rows; t0 < in.rows; t0 += (uint64_t)gridDim.x * rows)
+        each_joined(in, weight, t0, min(t0 + rows, in.rows), S, g, c, part, at_label,
+                    [&](uint64_t t, bool use, float lp, Part p) {
+                        logp[t] = lp;
+                        if (lse) lse[t] = use ? part_lse(p, in.scale) : 0.0f;
+                    });
+}
+
+// Slice s of a gradient row, for slices of 256 U pieces: zeros where coef is
+// 0 (the logits are then not read).
+template <int TYPE, int U>
+__device__ __forceinline__ void grad_slice(const typename Elem<TYPE>::type* row, typename Elem<TYPE>::type* out,
+                                           uint32_t V, uint32_t s, uint32_t label, float coef, Part p, float c)
+{
+    typedef typename Elem<TYPE>::type E;
+    constexpr int N = Piece<TYPE>::N;
+    const RowCut<TYPE> r(row, V);
+    const bool none = coef == 0.0f || p.sum == 0.0f;
+    const float k = none ? 0.0f : -coef / p.sum;
+    const uint32_t first = s * (256 * U) + threadIdx.x;
+    Piece<TYPE> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (!none && first + 256 * u < r.full) x[u].w = load_vec<u32x4>(row + r.piece(first + 256 * u));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t v = r.piece(first + 256 * u);
+        if (first + 256 * u >= r.full) continue;
+        float y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            y[i] = none ? 0.0f : entry(x[u].get(i), c, p.top, k);
+            if (!none && label - v == (uint32_t)i) y[i] += coef;
+        }
+        x[u].put(y);
+        store_vec(out + v, x[u].w);
+    }
+    if (s == 0 && threadIdx.x < r.singles) {
+        const uint32_t v = r.single(threadIdx.x);
+        out[v] = (E)(none ? 0.0f : entry((float)row[v], c, p.top, k) + (v == label ? coef : 0.0f));
+    }
+}
+
+constexpr int kGradU = 2;
+
+// The policy loss' gradient by slices (S of them for the parts, G for the
+// gradient).  Workgroup 0: every token's log probability and the sums over
+// tokens.
+template <int TYPE>
+__global__ void __launch_bounds__(256) k_policy_grad(Logits in, PolicyArgs a, uint32_t S, uint32_t g, uint32_t G,
+                                                     float c, const Part* part, const float* at_label, float* logp,
+                                                     float* stats, void* dlogits, uint64_t ldd)
+{
+    typedef typename Elem<TYPE>::type E;
+    __shared__ double s_w[4][4];
+    if (blockIdx.x == 0) {
+        double x[3] = {0.0, 0.0, 0.0};
+        each_joined(in, a.weight, 0, in.rows, S, g, c, part, at_label, [&](uint64_t t, bool use, float lp, Part) {
+            logp[t] = lp;
+            if (use) add_token(a, t, lp, x);
+        });
+        put_policy_stats(a, x, s_w, stats);
+        return;
+    }
+    for (uint64_t b = blockIdx.x - 1; b < in.rows * G; b += gridDim.x - 1) {
+        const uint64_t t = b / G;
         Part p = {0.0f, 0.0f};
         float coef = 0.0f;
-        if (has_token(in, t) && w != 0.0f) {
-            p = join_slices(part + t * S, S, c);
-            coef = a.grad_scale * in.scale *
-                   (w * policy_token(a, t, row_logp(p, at_label[t], in.scale)).coef);
+        if (in_use(in, a.weight, t)) {
+            p = join_slices(part + t * S, S, g, c);
+            coef = a.grad_scale * in.scale * (a.weight[t] * policy_token(a, t, part_logp(p, at_label[t], c)).coef);
         }
-        grad_slice<TYPE>(static_cast<const E*>(in.x) + t * in.ld, static_cast<E*>(dlogits) + t * ldd, lo, end,
-                         (uint32_t)in.label[t], coef, p, c);
+        grad_slice<TYPE, kGradU>(static_cast<const E*>(in.x) + t * in.ld, static_cast<E*>(dlogits) + t * ldd,
+                                 (uint32_t)in.vocab, (uint32_t)(b % G), (uint32_t)in.label[t], coef, p, c);
     }
 }
 
 struct PairSums {
-    double loss, won, good, bad;
+    double x[4];  // loss, 1 if in order, rewards
 };
 
-// Pair blockIdx.x: rewards of its two sequences, loss, and the derivative by
-// every token's log probability.
-__global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint32_t pairs, const uint32_t* bounds,
-                                               uint32_t S, float c, const Part* part, const float* at_label,
-                                               float* logp, float* coef, PairSums* sums)
+// Pair blockIdx.x: its tokens' log probabilities (S > 1: from the slices),
+// rewards of its two sequences, loss, and the derivative by every token's log
+// probability.  The sequences' bounds: the launch's arguments, or a table.
+__global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint32_t pairs, Blob few,
+                                               const uint32_t* many, uint32_t S, uint32_t g, float c, const Part* part,
+                                               const float* at_label, float* logp, float* coef, PairSums* sums)
 {
-    __shared__ double s_w[4];
+    __shared__ double s_w[4][4];
     const uint32_t b = blockIdx.x;
-    const uint32_t lo = bounds[2 * b], mid = bounds[2 * b + 1], end = bounds[2 * b + 2];
-    double good = 0.0, bad = 0.0;
-    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256) {
-        float lp = 0.0f;
-        if (has_token(in, t)) {
-            lp = row_logp(join_slices(part + t * S, S, c), at_label[t], in.scale);
-            const double r = (double)lp - (a.ref_logp ? (double)a.ref_logp[t] : 0.0);
-            (t < mid ? good : bad) += r;
-        }
-        logp[t] = lp;
-    }
-    good = (double)a.beta * block_sum(good, s_w);
-    bad = (double)a.beta * block_sum(bad, s_w);
+    const uint32_t lo = many ? many[2 * b] : few.words[2 * b], mid = many ? many[2 * b + 1] : few.words[2 * b + 1];
+    const uint32_t end = many ? many[2 * b + 2] : few.words[2 * b + 2];
+    double x[2] = {0.0, 0.0};
+    auto add = [&](uint64_t t, bool use, float lp, Part) {
+        if (S > 1) logp[t] = lp;
+        if (use) x[t < mid ? 0 : 1] += (double)lp - (a.ref_logp ? (double)a.ref_logp[t] : 0.0);
+    };
+    if (S > 1)
+        each_joined(in, nullptr, lo, end, S, g, c, part, at_label, add);
+    else
+        for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256) add(t, has_token(in, t), logp[t], Part{});
+    block_sum(x, s_w, 2);
+    const double good = (double)a.beta * x[0], bad = (double)a.beta * x[1];
     const double h = good - bad, z = exp(-fabs(h)), soft = log1p(z);
     const double up = h >= 0.0 ? 1.0 / (1.0 + z) : z / (1.0 + z);    // sigmoid(h)
     const double down = h >= 0.0 ? z / (1.0 + z) : 1.0 / (1.0 + z);  // sigmoid(-h)
@@ -280,69 +514,67 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
     const float q = (float)((double)a.beta * (eps * up - (1.0 - eps) * down) / (double)pairs);
     for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256)
         coef[t] = has_token(in, t) ? (t < mid ? q : -q) : 0.0f;
-    if (threadIdx.x == 0) {
-        PairSums r;
-        r.loss = (1.0 - eps) * (soft - fmin(h, 0.0)) + eps * (soft + fmax(h, 0.0));
-        r.won = h > 0.0 ? 1.0 : 0.0;
-        r.good = good;
-        r.bad = bad;
-        sums[b] = r;
-    }
+    if (threadIdx.x == 0)
+        sums[b] = PairSums{{(1.0 - eps) * (soft - fmin(h, 0.0)) + eps * (soft + fmax(h, 0.0)), h > 0.0 ? 1.0 : 0.0,
+                            good, bad}};
 }
 
 // Workgroup 0: the sums over pairs; the others a slice of the gradient each.
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_preference(Logits in, PreferenceArgs a, uint32_t pairs, uint32_t S,
-                                                    uint64_t W, float c, const Part* part, const float* coef,
-                                                    const PairSums* sums, float* stats, void* dlogits, uint64_t ldd)
+__global__ void __launch_bounds__(256) k_preference_grad(Logits in, PreferenceArgs a, uint32_t pairs, uint32_t S,
+                                                         uint32_t g, uint32_t G, float c, const Part* part,
+                                                         const float* coef, const PairSums* sums, float* stats,
+                                                         void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
-    __shared__ double s_w[4];
+    __shared__ double s_w[4][4];
     if (blockIdx.x == 0) {
-        double loss = 0.0, won = 0.0, good = 0.0, bad = 0.0;
-        for (uint32_t i = threadIdx.x; i < pairs; i += 256) {
-            loss += sums[i].loss;
-            won += sums[i].won;
-            good += sums[i].good;
-            bad += sums[i].bad;
-        }
-        loss = block_sum(loss, s_w);
-        won = block_sum(won, s_w);
-        good = block_sum(good, s_w);
-        bad = block_sum(bad, s_w);
-        if (threadIdx.x == 0) {
-            stats[0] = (float)(loss / pairs);
-            stats[1] = (float)(won / pairs);
-            stats[2] = (float)(good / pairs);
-            stats[3] = (float)(bad / pairs);
-        }
+        double x[4] = {0.0, 0.0, 0.0, 0.0};
+        for (uint32_t i = threadIdx.x; i < pairs; i += 256)
+            for (int q = 0; q < 4; ++q) x[q] += sums[i].x[q];
+        block_sum(x, s_w, 4);
+        if (threadIdx.x == 0)
+            for (int q = 0; q < 4; ++q) stats[q] = (float)(x[q] / pairs);
         return;
     }
-    for (uint64_t b = blockIdx.x - 1; b < in.rows * S; b += gridDim.x - 1) {
-        const uint64_t t = b / S, lo = (b % S) * W, end = min(lo + W, in.vocab);
+    for (uint64_t b = blockIdx.x - 1; b < in.rows * G; b += gridDim.x - 1) {
+        const uint64_t t = b / G;
         Part p = {0.0f, 0.0f};
         const float q = a.grad_scale * in.scale * coef[t];
-        if (q != 0.0f) p = join_slices(part + t * S, S, c);
-        grad_slice<TYPE>(static_cast<const E*>(in.x) + t * in.ld, static_cast<E*>(dlogits) + t * ldd, lo, end,
-                         (uint32_t)in.label[t], q, p, c);
+        if (q != 0.0f) p = join_slices(part + t * S, S, g, c);
+        grad_slice<TYPE, kGradU>(static_cast<const E*>(in.x) + t * in.ld, static_cast<E*>(dlogits) + t * ldd,
+                                 (uint32_t)in.vocab, (uint32_t)(b % G), (uint32_t)in.label[t], q, p, c);
     }
 }
 
-// Slices a row: enough workgroups for the chip when there are few rows, none
-// shorter than two steps of a workgroup.
+// ---------------------------------------------------------------- host
+
+// How a call's rows are taken: cut into S slices of W pieces for the sums, G
+// slices for a gradient pass; `row`: log probabilities by a workgroup a row.
 struct Cut {
-    uint32_t S;
-    uint64_t W;
-    uint32_t grid;
+    uint32_t S, W, g, G;
+    uint64_t pieces;  // of a row at most
+    bool many, row;
 };
-Cut cut_rows(uint64_t rows, uint64_t vocab)
+constexpr uint64_t kManyRows = 512;
+constexpr uint64_t kMaxRows = 1u << 21;  // of a launch with a workgroup a row (fewer than 2^32 threads)
+constexpr uint32_t kMaxGrid = 1u << 22;
+constexpr uint32_t kHold = 8;  // pieces a thread of k_row holds
+
+Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
 {
     Cut r;
-    const uint64_t most = (vocab + 2 * kStep - 1) / (2 * kStep), want = (1024 + rows - 1) / rows;
-    uint64_t S = std::max<uint64_t>(1, std::min(most, want));
-    r.W = ((vocab + S - 1) / S + kStep - 1) / kStep * kStep;
-    r.S = (uint32_t)((vocab + r.W - 1) / r.W);
-    r.grid = (uint32_t)std::min<uint64_t>(rows * r.S, 1u << 22);
+    r.pieces = vocab / (type == kF32 ? 4 : 8) + 1;
+    r.G = (uint32_t)((r.pieces + 256 * kGradU - 1) / (256 * kGradU));
+    r.many = rows >= kManyRows;
+    r.row = r.many && rows <= kMaxRows && r.pieces <= 512 * kHold;
+    // enough workgroups for the chip when there are few rows, none of less
+    // than 512 pieces
+    const uint64_t most = std::min<uint64_t>(64, (r.pieces + 511) / 512), want = 1024 / std::min<uint64_t>(rows, 1024);
+    const uint64_t S = r.many ? 1 : std::max<uint64_t>(1, std::min(most, want));
+    r.W = (uint32_t)((r.pieces + S - 1) / S);
+    r.S = (uint32_t)((r.pieces + r.W - 1) / r.W);
+    for (r.g = 1; r.g < r.S;) r.g *= 2;
     return r;
 }
 
@@ -352,11 +584,11 @@ struct Space {
     PairSums* sums;
     uint32_t* bounds;
 };
-Space carve(void* ws, uint64_t rows, const Cut& cut, uint32_t pairs, size_t* bytes)
+Space carve(void* ws, uint64_t rows, uint32_t S, uint32_t pairs, size_t* bytes)
 {
     Carve c(ws);
     Space r;
-    r.part = c.take<Part>(rows * cut.S);
+    r.part = c.take<Part>(rows * S);
     r.at_label = c.take<float>(rows);
     r.coef = c.take<float>(pairs ? rows : 0);
     r.sums = c.take<PairSums>(pairs);
@@ -364,86 +596,141 @@ Space carve(void* ws, uint64_t rows, const Cut& cut, uint32_t pairs, size_t* byt
     if (bytes) *bytes = c.used;
     return r;
 }
-
-hipError_t rows_run(const Logits& in, const float* weight, const Cut& cut, const Space& sp, float c, hipStream_t s)
+// Enough for every element type.
+size_t workspace(uint32_t pairs, uint64_t rows, uint64_t vocab)
 {
-    timer_begin(kTLossRows, s);
-    if (in.type == kF32)
-        hipLaunchKernelGGL((k_rows<kF32>), dim3(cut.grid), dim3(256), 0, s, in, weight, cut.S, cut.W, c, sp.part, sp.at_label);
-    else if (in.type == kBf16)
-        hipLaunchKernelGGL((k_rows<kBf16>), dim3(cut.grid), dim3(256), 0, s, in, weight, cut.S, cut.W, c, sp.part, sp.at_label);
+    size_t most = 0;
+    for (uint32_t type : {(uint32_t)kF32, (uint32_t)kBf16}) {
+        size_t b = 0;
+        carve(nullptr, rows, cut_rows(rows, vocab, type).S, pairs, &b);
+        most = std::max(most, b);
+    }
+    return most;
+}
+
+template <class F>
+void by_type(uint32_t type, F f)
+{
+    if (type == kF32)
+        f(std::integral_constant<int, kF32>());
+    else if (type == kBf16)
+        f(std::integral_constant<int, kBf16>());
     else
-        hipLaunchKernelGGL((k_rows<kF16>), dim3(cut.grid), dim3(256), 0, s, in, weight, cut.S, cut.W, c, sp.part, sp.at_label);
+        f(std::integral_constant<int, kF16>());
+}
+
+template <bool GRAD>
+void launch_row(const Cut& cut, const Logits& in, const PolicyArgs& a, float c, float* logp, float* lse, Part* part,
+                void* dlogits, uint64_t ldd, hipStream_t s)
+{
+    by_type(in.type, [&](auto ty) {
+        constexpr int TY = decltype(ty)::value;
+        auto go = [&](auto kern, uint64_t most) {
+            const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kHold * 64 - 1) / (kHold * 64) * 64);
+            hipLaunchKernelGGL(kern, dim3((uint32_t)in.rows), dim3((uint32_t)std::min(threads, most)), 0, s, in, a, c,
+                               logp, lse, part, dlogits, ldd);
+        };
+        if (cut.pieces <= 1024 * kHold)
+            go(k_row<TY, 512, kHold, GRAD>, 512);
+        else
+            go(k_row<TY, 1024, kHold, GRAD>, 1024);
+    });
+}
+
+// The rows in use: log probabilities (where S is 1, or a workgroup takes a
+// row), else the parts for who joins them.
+hipError_t rows_run(const Cut& cut, const Logits& in, const float* weight, const Space& sp, float* logp, float* lse,
+                    hipStream_t s)
+{
+    const float c = in.scale * kLog2e;
+    timer_begin(kTLossRows, s);
+    if (cut.row) {
+        PolicyArgs a = {};
+        a.weight = weight;
+        launch_row<false>(cut, in, a, c, logp, lse, sp.part, nullptr, 0, s);
+    } else {
+        const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kMaxGrid);
+        by_type(in.type, [&](auto ty) {
+            hipLaunchKernelGGL((k_slices<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, weight, cut.S, cut.W,
+                               c, sp.part, sp.at_label, logp, lse);
+        });
+    }
     timer_end(kTLossRows, s);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t logprob_workspace(uint64_t rows, uint64_t vocab)
-{
-    size_t b;
-    carve(nullptr, rows, cut_rows(rows, vocab), 0, &b);
-    return b;
-}
-size_t policy_workspace(uint64_t rows, uint64_t vocab) { return logprob_workspace(rows, vocab); }
-size_t preference_workspace(uint32_t pairs, uint64_t rows, uint64_t vocab)
-{
-    size_t b;
-    carve(nullptr, rows, cut_rows(rows, vocab), pairs, &b);
-    return b;
-}
+size_t logprob_workspace(uint64_t rows, uint64_t vocab) { return workspace(0, rows, vocab); }
+size_t policy_workspace(uint64_t rows, uint64_t vocab) { return workspace(0, rows, vocab); }
+size_t preference_workspace(uint32_t pairs, uint64_t rows, uint64_t vocab) { return workspace(pairs, rows, vocab); }
 
 hipError_t logprob_run(const Logits& in, float* logp, float* lse, void* ws, hipStream_t s)
 {
-    const Cut cut = cut_rows(in.rows, in.vocab);
-    const Space sp = carve(ws, in.rows, cut, 0, nullptr);
-    const float c = in.scale * kLog2e;
-    hipError_t e = rows_run(in, nullptr, cut, sp, c, s);
-    if (e != hipSuccess) return e;
-    const uint32_t grid = (uint32_t)std::min<uint64_t>((in.rows + 255) / 256, 4096);
-    hipLaunchKernelGGL(k_logprob, dim3(grid), dim3(256), 0, s, in, cut.S, c, sp.part, sp.at_label, logp, lse);
+    const Cut cut = cut_rows(in.rows, in.vocab, in.type);
+    const Space sp = carve(ws, in.rows, cut.S, 0, nullptr);
+    hipError_t e = rows_run(cut, in, nullptr, sp, logp, lse, s);
+    if (e != hipSuccess || cut.S == 1) return e;
+    const uint32_t grid = (uint32_t)((in.rows * cut.g + 255) / 256);
+    hipLaunchKernelGGL(k_join, dim3(grid), dim3(256), 0, s, in, (const float*)nullptr, cut.S, cut.g,
+                       in.scale * kLog2e, sp.part, sp.at_label, logp, lse);
     return hipGetLastError();
 }
 
 hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float* stats, void* dlogits, uint64_t ldd,
                       void* ws, hipStream_t s)
 {
-    const Cut cut = cut_rows(in.rows, in.vocab);
-    const Space sp = carve(ws, in.rows, cut, 0, nullptr);
+    const Cut cut = cut_rows(in.rows, in.vocab, in.type);
+    const Space sp = carve(ws, in.rows, cut.S, 0, nullptr);
     const float c = in.scale * kLog2e;
-    hipError_t e = rows_run(in, a.weight, cut, sp, c, s);
-    if (e != hipSuccess) return e;
-    const dim3 grid(dlogits ? cut.grid + 1 : 1);
-    timer_begin(kTLossGrad, s);
-    if (in.type == kF32)
-        hipLaunchKernelGGL((k_policy<kF32>), grid, dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part, sp.at_label, logp, stats, dlogits, ldd);
-    else if (in.type == kBf16)
-        hipLaunchKernelGGL((k_policy<kBf16>), grid, dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part, sp.at_label, logp, stats, dlogits, ldd);
-    else
-        hipLaunchKernelGGL((k_policy<kF16>), grid, dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part, sp.at_label, logp, stats, dlogits, ldd);
-    timer_end(kTLossGrad, s);
+    const bool fused = dlogits && cut.many && in.rows <= kMaxRows;
+    if (fused) {
+        timer_begin(kTLossRows, s);
+        launch_row<true>(cut, in, a, c, logp, nullptr, nullptr, dlogits, ldd, s);
+        timer_end(kTLossRows, s);
+    } else {
+        hipError_t e = rows_run(cut, in, a.weight, sp, logp, nullptr, s);
+        if (e != hipSuccess) return e;
+    }
+    if (cut.many) hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, in, a, logp, stats);
+    if (!fused && (dlogits || !cut.many)) {
+        const uint32_t grid = dlogits ? (uint32_t)std::min<uint64_t>(in.rows * cut.G, kMaxGrid) + 1 : 1;
+        timer_begin(kTLossGrad, s);
+        by_type(in.type, [&](auto ty) {
+            hipLaunchKernelGGL((k_policy_grad<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a, cut.S, cut.g,
+                               cut.G, c, sp.part, sp.at_label, logp, stats, dlogits, ldd);
+        });
+        timer_end(kTLossGrad, s);
+    }
     return hipGetLastError();
 }
 
 hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pairs, const uint32_t* bounds,
                           float* logp, float* stats, void* dlogits, uint64_t ldd, void* ws, hipStream_t s)
 {
-    const Cut cut = cut_rows(in.rows, in.vocab);
-    const Space sp = carve(ws, in.rows, cut, pairs, nullptr);
+    const Cut cut = cut_rows(in.rows, in.vocab, in.type);
+    const Space sp = carve(ws, in.rows, cut.S, pairs, nullptr);
     const float c = in.scale * kLog2e;
-    hipError_t e = rows_run(in, nullptr, cut, sp, c, s);
-    if (e == hipSuccess) e = upload(sp.bounds, bounds, (2 * (size_t)pairs + 1) * sizeof(uint32_t), s);
+    hipError_t e = rows_run(cut, in, nullptr, sp, logp, nullptr, s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_pairs, dim3(pairs), dim3(256), 0, s, in, a, pairs, sp.bounds, cut.S, c, sp.part, sp.at_label, logp, sp.coef, sp.sums);
-    const dim3 grid(dlogits ? cut.grid + 1 : 1);
+    const size_t words = 2 * (size_t)pairs + 1;
+    Blob few = {};
+    const uint32_t* many = nullptr;
+    if (words <= kBlobWords) {
+        std::copy(bounds, bounds + words, few.words);
+    } else {
+        e = upload(sp.bounds, bounds, words * sizeof(uint32_t), s);
+        if (e != hipSuccess) return e;
+        many = sp.bounds;
+    }
+    hipLaunchKernelGGL(k_pairs, dim3(pairs), dim3(256), 0, s, in, a, pairs, few, many, cut.S, cut.g, c, sp.part,
+                       sp.at_label, logp, sp.coef, sp.sums);
+    const uint32_t grid = dlogits ? (uint32_t)std::min<uint64_t>(in.rows * cut.G, kMaxGrid) + 1 : 1;
     timer_begin(kTLossGrad, s);
-    if (in.type == kF32)
-        hipLaunchKernelGGL((k_preference<kF32>), grid, dim3(256), 0, s, in, a, pairs, cut.S, cut.W, c, sp.part, sp.coef, sp.sums, stats, dlogits, ldd);
-    else if (in.type == kBf16)
-        hipLaunchKernelGGL((k_preference<kBf16>), grid, dim3(256), 0, s, in, a, pairs, cut.S, cut.W, c, sp.part, sp.coef, sp.sums, stats, dlogits, ldd);
-    else
-        hipLaunchKernelGGL((k_preference<kF16>), grid, dim3(256), 0, s, in, a, pairs, cut.S, cut.W, c, sp.part, sp.coef, sp.sums, stats, dlogits, ldd);
+    by_type(in.type, [&](auto ty) {
+        hipLaunchKernelGGL((k_preference_grad<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a, pairs, cut.S,
+                           cut.g, cut.G, c, sp.part, sp.coef, sp.sums, stats, dlogits, ldd);
+    });
     timer_end(kTLossGrad, s);
     return hipGetLastError();
 }

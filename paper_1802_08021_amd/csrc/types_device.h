@@ -30,19 +30,50 @@ struct Elem<kF16> {
     typedef f16x4 vec4;
 };
 
-// Four consecutive elements from p on, at any element-aligned address (one
-// access: gfx950 takes unaligned vector accesses to global memory).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// A vector from p on, at any element-aligned address (one access: gfx950 takes
+// unaligned vector accesses to global memory), streamed: marked nontemporal.
 template <class V, class E>
-__device__ __forceinline__ V load4(const E* p)
+__device__ __forceinline__ V load_vec(const E* p)
+{
+    typedef V U __attribute__((aligned(sizeof(E))));
+    return __builtin_nontemporal_load(reinterpret_cast<const U*>(p));
+}
+// The same for data that is read once more soon.
+template <class V, class E>
+__device__ __forceinline__ V load_keep(const E* p)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
     return *reinterpret_cast<const U*>(p);
 }
 template <class V, class E>
-__device__ __forceinline__ void store4(E* p, V v)
+__device__ __forceinline__ void store_vec(E* p, V v)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
-    *reinterpret_cast<U*>(p) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<U*>(p));
+}
+
+// Sum and maximum of the 64 lanes' values, in every lane: shifts within rows
+// of 16 lanes, then the row broadcasts (lanes that a step has no source for
+// add zero or keep their own).
+template <int CTRL, int ROWS, bool SUM>
+__device__ __forceinline__ float wave_step(float x)
+{
+    const int v = __float_as_int(x);
+    const float y = __int_as_float(__builtin_amdgcn_update_dpp(SUM ? 0 : v, v, CTRL, ROWS, 0xF, false));
+    return SUM ? x + y : fmaxf(x, y);
+}
+template <bool SUM>
+__device__ __forceinline__ float wave_join(float x)
+{
+    x = wave_step<0x111, 0xF, SUM>(x);  // row_shr:1
+    x = wave_step<0x112, 0xF, SUM>(x);  // row_shr:2
+    x = wave_step<0x114, 0xF, SUM>(x);  // row_shr:4
+    x = wave_step<0x118, 0xF, SUM>(x);  // row_shr:8
+    x = wave_step<0x142, 0xA, SUM>(x);  // row_bcast:15
+    x = wave_step<0x143, 0xC, SUM>(x);  // row_bcast:31
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
 // Largest of the 64 lanes' values, in every lane: shifts within rows of 16

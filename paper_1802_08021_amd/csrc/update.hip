@@ -29,7 +29,7 @@ __device__ __forceinline__ f32x4 get4(const void* p, uint64_t e, uint64_t n)
 {
     typedef typename Elem<TYPE>::type E;
     const E* q = static_cast<const E*>(p) + e;
-    if (e + 4 <= n) return __builtin_convertvector(load4<typename Elem<TYPE>::vec4>(q), f32x4);
+    if (e + 4 <= n) return __builtin_convertvector(load_vec<typename Elem<TYPE>::vec4>(q), f32x4);
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -44,7 +44,7 @@ __device__ __forceinline__ void put4(void* p, uint64_t e, uint64_t n, f32x4 x)
     typedef typename Elem<TYPE>::type E;
     E* q = static_cast<E*>(p) + e;
     if (e + 4 <= n) {
-        store4(q, __builtin_convertvector(x, typename Elem<TYPE>::vec4));
+        store_vec(q, __builtin_convertvector(x, typename Elem<TYPE>::vec4));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -56,8 +56,7 @@ __device__ __forceinline__ void put4(void* p, uint64_t e, uint64_t n, f32x4 x)
 __device__ __forceinline__ uint32_t get_codes(const void* p, uint64_t e, uint64_t n)
 {
     const uint8_t* q = static_cast<const uint8_t*>(p) + e;
-    typedef uint32_t U __attribute__((aligned(1)));
-    if (e + 4 <= n) return *reinterpret_cast<const U*>(q);
+    if (e + 4 <= n) return load_vec<uint32_t>(q);
     uint32_t w = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -68,9 +67,8 @@ __device__ __forceinline__ uint32_t get_codes(const void* p, uint64_t e, uint64_
 __device__ __forceinline__ void put_codes(void* p, uint64_t e, uint64_t n, uint32_t w)
 {
     uint8_t* q = static_cast<uint8_t*>(p) + e;
-    typedef uint32_t U __attribute__((aligned(1)));
     if (e + 4 <= n) {
-        *reinterpret_cast<U*>(q) = w;
+        store_vec(q, w);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -230,7 +228,7 @@ __global__ void __launch_bounds__(256) k_norm_end(const double* partial, uint32_
 template <int BITS, int GT, int CT>
 void launch_adamw(const TensorTab& t, uint64_t pieces, const AdamwStep& a, const float* clip, hipStream_t s)
 {
-    constexpr int U = 4;
+    constexpr int U = 1;
     const uint64_t grid = std::min<uint64_t>(pieces * (kTensorChunk / (1024 * U)), 1u << 22);
     hipLaunchKernelGGL((k_adamw<BITS, GT, CT, U>), dim3((uint32_t)grid), dim3(256), 0, s, t.desc, t.map, pieces, a, clip);
 }
