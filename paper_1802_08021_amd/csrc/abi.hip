@@ -338,8 +338,7 @@ int sparcml_workspace_size(int op, int P, uint64_t N, uint64_t max_nnz, double d
         return SPARCML_OK;
     case SPARCML_OP_TENSORS:
         if (P < 1 || P > 65535 || N > kMaxElements) return fail(SPARCML_EINVAL, "bad tensor sizes");
-        // pieces of every tensor: at most one that is not full each
-        tensors_carve(nullptr, (uint32_t)P, N / kTensorChunk + (uint64_t)P, bytes);
+        tensors_carve(nullptr, (uint32_t)P, tensor_chunks_most(N, (uint64_t)P), bytes);
         return SPARCML_OK;
     case SPARCML_OP_LOGPROB:
     case SPARCML_OP_POLICY:
@@ -632,13 +631,17 @@ int sparcml_tensors_prepare(int count, const sparcml_tensor* tensors, int grad_t
             }
             if (state_bits && !(isfinite(a.decay) && isfinite(a.lr_scale)))
                 return fail(SPARCML_EINVAL, "tensor %d: decay and lr_scale must be finite", t);
-            d[t] = TensorDesc{a.param, a.grad, a.m, a.v, a.m_scale, a.v_scale, a.copy, a.n, a.decay, a.lr_scale};
+            // (blocks of 8-bit moments count from the tensor's first element)
+            const uintptr_t at = (uintptr_t)(state_bits ? (const void*)a.param : a.grad);
+            const uint32_t size = state_bits || grad_type == SPARCML_F32 ? 4 : 2;
+            const uint32_t shift = state_bits == 8 ? 0 : (uint32_t)(at % 128 / size);
+            d[t] = TensorDesc{a.param, a.grad, a.m, a.v, a.m_scale, a.v_scale, a.copy, a.n, a.decay, a.lr_scale, shift, 0};
             total += a.n;
-            chunks += (a.n + kTensorChunk - 1) / kTensorChunk;
+            chunks += tensor_chunks(a.n, shift);
         }
         if (total > kMaxElements) return fail(SPARCML_EINVAL, "more than 2^42 elements");
         size_t need = 0;
-        tensors_carve(nullptr, (uint32_t)count, total / kTensorChunk + (uint64_t)count, &need);
+        tensors_carve(nullptr, (uint32_t)count, tensor_chunks_most(total, (uint64_t)count), &need);
         if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
         hipError_t e = tensors_prepare_run((uint32_t)count, d.data(), chunks, ws, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, "tensors_prepare");

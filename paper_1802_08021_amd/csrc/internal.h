@@ -245,7 +245,7 @@ enum ElemType : uint32_t { kF32 = 0, kBf16 = 1, kF16 = 2 };
 constexpr uint32_t kStateBlock = 256;    // elements that share a scale (8-bit moments)
 constexpr uint32_t kTensorChunk = 4096;  // elements of a tensor that the work map lists as one piece
 
-// Device copy of one tensor descriptor (72 bytes).
+// Device copy of one tensor descriptor (80 bytes).
 struct TensorDesc {
     float* param;
     const void* grad;
@@ -256,6 +256,9 @@ struct TensorDesc {
     void* copy;
     uint64_t n;
     float decay, lr_scale;
+    // Pieces of work begin this many elements before the tensor, so that each
+    // begins at a line of its weights (32-bit moments) or of its gradient.
+    uint32_t shift, pad;
 };
 
 // What a prepared workspace holds; the same carving for every call on it.
@@ -264,9 +267,16 @@ struct TensorTab {
     uint32_t* first;   // [count] a tensor's first chunk
     uint2* map;        // [chunks] {tensor, chunk of it}
     double* partial;   // [kNormParts]
+    uint32_t* ticket;  // [kTickets * kTicketStride], 0 between calls
 };
 constexpr uint32_t kNormParts = 2048;
+// Counters of a norm's finished workgroups: kTickets - 1 groups', and the
+// groups' own; a 128-byte line each.
+constexpr uint32_t kTickets = 33, kTicketStride = 32;
 TensorTab tensors_carve(void* ws, uint32_t count, uint64_t chunks, size_t* bytes);
+// Pieces of work of a tensor, and of `count` tensors of `total` elements at most.
+inline uint64_t tensor_chunks(uint64_t n, uint32_t shift) { return n ? (n + shift + kTensorChunk - 1) / kTensorChunk : 0; }
+inline uint64_t tensor_chunks_most(uint64_t total, uint64_t count) { return total / kTensorChunk + 2 * count; }
 hipError_t tensors_prepare_run(uint32_t count, const TensorDesc* host, uint64_t chunks, void* ws, hipStream_t s);
 hipError_t grad_norm_run(uint32_t count, uint64_t chunks, uint32_t gtype, double grad_scale, double max_norm,
                          float* out, void* ws, hipStream_t s);

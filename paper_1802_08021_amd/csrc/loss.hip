@@ -37,12 +37,7 @@ struct Piece {
     // A word of a piece that holds nothing but -Inf.
     static constexpr uint32_t kNone = TYPE == kF32 ? 0xFF800000u : TYPE == kBf16 ? 0xFF80FF80u : 0xFC00FC00u;
     u32x4 w;
-    __device__ __forceinline__ float get(int i) const
-    {
-        if (TYPE == kF32) return __uint_as_float(w[i]);
-        if (TYPE == kBf16) return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
-        return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]));
-    }
+    __device__ __forceinline__ float get(int i) const { return unpack<TYPE>(w, i); }
     // The elements rounded to nearest.
     __device__ __forceinline__ void put(const float* x)
     {
@@ -134,26 +129,48 @@ __device__ __forceinline__ void clear_row(typename Elem<TYPE>::type* out, uint32
 
 // ---------------------------------------------------------------- policy terms
 
-// One token of the policy loss: its terms and the loss' derivative by its
-// log probability (both before the weight).
-struct PolicyToken {
-    float gain, k, coef;
-    bool clipped;
+// One token's inputs of the policy loss.
+struct PolicyRow {
+    float w, old, adv, ref;
+    PolicyRow() = default;
+    __device__ __forceinline__ PolicyRow(const PolicyArgs& a, uint64_t t)
+        : w(a.weight[t]), old(a.old_logp[t]), adv(a.adv[t]), ref(a.ref_logp ? a.ref_logp[t] : 0.0f)
+    {
+    }
+    // In scalar registers (the same row in the whole wave).
+    __device__ __forceinline__ PolicyRow scalar() const
+    {
+        auto s = [](float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); };
+        PolicyRow r;
+        r.w = s(w);
+        r.old = s(old);
+        r.adv = s(adv);
+        r.ref = s(ref);
+        return r;
+    }
 };
-__device__ __forceinline__ PolicyToken policy_token(const PolicyArgs& a, uint64_t t, float lp)
+
+// Its terms and the loss' derivative by its log probability, all with the
+// weight.
+struct PolicyTerms {
+    float gain, k, clipped, coef;
+};
+__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const PolicyRow& q, float lp)
 {
-    PolicyToken r;
-    const float adv = a.adv[t], rho = expf(lp - a.old_logp[t]);
-    const float u = rho * adv, held = fminf(fmaxf(rho, a.lo), a.hi) * adv;
-    r.clipped = u > held;
-    r.gain = r.clipped ? held : u;  // (a NaN of u comes through)
+    PolicyTerms r;
+    const float rho = expf(lp - q.old);
+    const float u = rho * q.adv, held = fminf(fmaxf(rho, a.lo), a.hi) * q.adv;
+    const bool clipped = u > held;
+    r.gain = q.w * (clipped ? held : u);  // (a NaN of u comes through)
+    r.clipped = clipped ? q.w : 0.0f;
     r.k = 0.0f;
-    r.coef = r.clipped ? 0.0f : -u;
+    r.coef = clipped ? 0.0f : -u;
     if (a.ref_logp) {
-        const float far = a.ref_logp[t] - lp, em = expm1f(far);
-        r.k = em - far;
+        const float far = q.ref - lp, em = expm1f(far);
+        r.k = q.w * (em - far);
         r.coef = r.coef - a.kl * em;
     }
+    r.coef = q.w * r.coef;
     return r;
 }
 
@@ -171,14 +188,11 @@ __device__ __forceinline__ void block_sum(double* x, double (*s_w)[4], int count
     }
 }
 
-// What one token adds to the sums over tokens: gain, KL, clipped.
-__device__ __forceinline__ void add_token(const PolicyArgs& a, uint64_t t, float lp, double* x)
+__device__ __forceinline__ void add_terms(const PolicyTerms& r, double* x)
 {
-    const double w = (double)a.weight[t];
-    const PolicyToken r = policy_token(a, t, lp);
-    x[0] += w * (double)r.gain;
-    x[1] += w * (double)r.k;
-    x[2] += r.clipped ? w : 0.0;
+    x[0] += (double)r.gain;
+    x[1] += (double)r.k;
+    x[2] += (double)r.clipped;
 }
 
 __device__ __forceinline__ void put_policy_stats(const PolicyArgs& a, double* x, double (*s_w)[4], float* stats)
@@ -192,13 +206,20 @@ __device__ __forceinline__ void put_policy_stats(const PolicyArgs& a, double* x,
     }
 }
 
-// The sums over tokens, their log probabilities given.
-__global__ void __launch_bounds__(1024) k_policy_stats(Logits in, PolicyArgs a, const float* logp, float* stats)
+// The sums over tokens of their terms (four rows a thread in flight).
+__global__ void __launch_bounds__(1024) k_policy_stats(uint64_t rows, PolicyArgs a, const PolicyTerms* terms,
+                                                       float* stats)
 {
     __shared__ double s_w[16][4];
     double x[3] = {0.0, 0.0, 0.0};
-    for (uint64_t t = threadIdx.x; t < in.rows; t += 1024)
-        if (in_use(in, a.weight, t)) add_token(a, t, logp[t], x);
+    for (uint64_t t = threadIdx.x; t < rows; t += 4096) {
+        PolicyTerms r[4] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t + 1024 * i < rows) r[i] = terms[t + 1024 * i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add_terms(r[i], x);
+    }
     put_policy_stats(a, x, s_w, stats);
 }
 
@@ -219,18 +240,22 @@ __device__ __forceinline__ float join_waves(float x, float* s)
 // What a thread has of its row so far: the maximum and the sum against it.
 struct Own {
     float top, sum;
+    // The first `used` of U pieces (the same in the whole wave).
     template <int TYPE, int U>
-    __device__ __forceinline__ void add(Piece<TYPE> (&x)[U], float c)
+    __device__ __forceinline__ void add(Piece<TYPE> (&x)[U], int used, float c)
     {
         float high = top;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            if (u >= used) break;
 #pragma unroll
             for (int i = 0; i < Piece<TYPE>::N; ++i) high = fmaxf(high, x[u].get(i));
+        }
         const float base = high == -INFINITY ? 0.0f : high;
         float more[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (u >= used) break;
             x[u].repack();
 #pragma unroll
             for (int i = 0; i < Piece<TYPE>::N; ++i) more[i & 3] += exp2_fast((x[u].get(i) - base) * c);
@@ -247,11 +272,13 @@ struct Own {
 // of the policy loss.
 template <int TYPE, int THREADS, int NV, bool GRAD>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
-k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, void* dlogits, uint64_t ldd)
+k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, float* at_label, uint32_t* ticket,
+      PolicyTerms* terms, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     constexpr int N = Piece<TYPE>::N, U = 2;
     __shared__ float s_top[THREADS / 64], s_sum[THREADS / 64], s_x, s_coef;
+    if (!GRAD && blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;  // for k_policy_grad
     const uint64_t t = blockIdx.x;
     const uint32_t V = (uint32_t)in.vocab, label = (uint32_t)in.label[t], tid = threadIdx.x, step = blockDim.x;
     const E* row = static_cast<const E*>(in.x) + t * in.ld;
@@ -260,11 +287,15 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, voi
         if (tid == 0) {
             logp[t] = 0.0f;
             if (lse) lse[t] = 0.0f;
+            if (terms) terms[t] = PolicyTerms{0.0f, 0.0f, 0.0f, 0.0f};
         }
         if (GRAD) clear_row<TYPE>(out, V);
         return;
     }
+    PolicyRow q = {};
+    if (terms) q = PolicyRow(a, t).scalar();
     const RowCut<TYPE> r(row, V);
+    const int used = (int)min((r.full + step - 1) / step, (uint32_t)NV);
     Piece<TYPE> x[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -281,9 +312,9 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, voi
             y[u].none();
             if (j + step * u < r.full) y[u].w = load_keep<u32x4>(row + r.piece(j + step * u));
         }
-        own.add(y, c);
+        own.add(y, U, c);
     }
-    own.add(x, c);
+    own.add(x, used, c);
     float top = join_waves<false>(own.top, s_top);
     if (top == -INFINITY) top = 0.0f;
     const Part p = {top, join_waves<true>(own.sum * exp2_fast((own.top - top) * c), s_sum)};
@@ -291,8 +322,15 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, voi
         const float lp = part_logp(p, s_x, c);
         logp[t] = lp;
         if (lse) lse[t] = part_lse(p, in.scale);
-        if (part) part[t] = p;
-        if (GRAD) s_coef = p.sum == 0.0f ? 0.0f : a.grad_scale * in.scale * (a.weight[t] * policy_token(a, t, lp).coef);
+        if (part) {
+            part[t] = p;
+            at_label[t] = s_x;
+        }
+        if (terms) {
+            const PolicyTerms m = policy_terms(a, q, lp);
+            terms[t] = m;
+            if (GRAD) s_coef = p.sum == 0.0f ? 0.0f : a.grad_scale * in.scale * m.coef;
+        }
     }
     if (!GRAD) return;
     uint32_t j = tid + step * NV;
@@ -312,7 +350,10 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, voi
         if (at < r.full) store_vec(out + r.piece(at), q.w);
     };
 #pragma unroll
-    for (int i = 0; i < NV; ++i) write(x[i], tid + step * i);
+    for (int i = 0; i < NV; ++i) {
+        if (i >= used) break;
+        write(x[i], tid + step * i);
+    }
     while (j < r.full) {
         Piece<TYPE> now[U];
 #pragma unroll
@@ -335,13 +376,15 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, voi
 
 // Slice s of a row: pieces [s W, (s + 1) W); slice 0 takes the singles too.
 // (M, Z) of every slice of every row in use, the token's logit beside them;
-// with one slice a row its log probability (and lse) at once.
+// with one slice a row its log probability (lse, terms) at once.
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, uint32_t S, uint32_t W, float c,
-                                                Part* part, float* at_label, float* logp, float* lse)
+                                                Part* part, float* at_label, float* logp, float* lse, PolicyArgs a,
+                                                PolicyTerms* terms, uint32_t* ticket)
 {
     typedef typename Elem<TYPE>::type E;
     __shared__ float s_top[4], s_sum[4];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;  // for k_policy_grad
     for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
         const uint64_t t = b / S;
         const uint32_t s = (uint32_t)(b % S);
@@ -349,6 +392,7 @@ __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, 
             if (S == 1 && threadIdx.x == 0) {
                 logp[t] = 0.0f;
                 if (lse) lse[t] = 0.0f;
+                if (terms) terms[t] = PolicyTerms{0.0f, 0.0f, 0.0f, 0.0f};
             }
             continue;
         }
@@ -365,7 +409,7 @@ __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, 
                 x[u].none();
                 if (j + 256 * u < end) x[u].w = load_vec<u32x4>(row + r.piece(j + 256 * u));
             }
-            own.add(x, c);
+            own.add(x, 4, c);
         }
         float high = join_waves<false>(own.top, s_top);
         if (high == -INFINITY) high = 0.0f;
@@ -375,8 +419,10 @@ __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, 
             part[b] = p;
             if (s == 0) at_label[t] = at;
             if (S == 1) {
-                logp[t] = part_logp(p, at, c);
+                const float lp = part_logp(p, at, c);
+                logp[t] = lp;
                 if (lse) lse[t] = part_lse(p, in.scale);
+                if (terms) terms[t] = policy_terms(a, PolicyRow(a, t), lp);
             }
         }
         __syncthreads();
@@ -393,9 +439,11 @@ __device__ __forceinline__ void each_joined(const Logits& in, const float* weigh
 {
     for (uint64_t t0 = first; t0 < end; t0 += 256 / g) {
         const uint64_t t = t0 + threadIdx.x / g;
-        const bool use = t < end && in_use(in, weight, t);
-        const Part p = join_slices(part + (use ? t * S : 0), use ? S : 0, g, c);
-        if (t < end && (threadIdx.x & (g - 1)) == 0) f(t, use, use ? part_logp(p, at_label[t], c) : 0.0f, p);
+        const uint64_t in_range = t < end ? t : end - 1;
+        const float at = at_label[in_range];
+        const bool use = t < end && in_use(in, weight, in_range);
+        const Part p = join_slices(part + in_range * S, S, g, c);
+        if (t < end && (threadIdx.x & (g - 1)) == 0) f(t, use, use ? part_logp(p, at, c) : 0.0f, p);
     }
 }
 
@@ -412,73 +460,103 @@ __global__ void __launch_bounds__(256) k_join(Logits in, const float* weight, ui
                     });
 }
 
-// Slice s of a gradient row, for slices of 256 U pieces: zeros where coef is
-// 0 (the logits are then not read).
-template <int TYPE, int U>
-__device__ __forceinline__ void grad_slice(const typename Elem<TYPE>::type* row, typename Elem<TYPE>::type* out,
-                                           uint32_t V, uint32_t s, uint32_t label, float coef, Part p, float c)
-{
-    typedef typename Elem<TYPE>::type E;
-    constexpr int N = Piece<TYPE>::N;
-    const RowCut<TYPE> r(row, V);
-    const bool none = coef == 0.0f || p.sum == 0.0f;
-    const float k = none ? 0.0f : -coef / p.sum;
-    const uint32_t first = s * (256 * U) + threadIdx.x;
-    Piece<TYPE> x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (!none && first + 256 * u < r.full) x[u].w = load_vec<u32x4>(row + r.piece(first + 256 * u));
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const uint32_t v = r.piece(first + 256 * u);
-        if (first + 256 * u >= r.full) continue;
-        float y[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            y[i] = none ? 0.0f : entry(x[u].get(i), c, p.top, k);
-            if (!none && label - v == (uint32_t)i) y[i] += coef;
-        }
-        x[u].put(y);
-        store_vec(out + v, x[u].w);
-    }
-    if (s == 0 && threadIdx.x < r.singles) {
-        const uint32_t v = r.single(threadIdx.x);
-        out[v] = (E)(none ? 0.0f : entry((float)row[v], c, p.top, k) + (v == label ? coef : 0.0f));
-    }
-}
-
 constexpr int kGradU = 2;
 
+// Slice s of a gradient row, of 256 kGradU pieces.  The logits of a row in
+// use are under way while its coefficient is found; zeros where that is 0.
+template <int TYPE>
+struct GradSlice {
+    typedef typename Elem<TYPE>::type E;
+    static constexpr int N = Piece<TYPE>::N, U = kGradU;
+    const RowCut<TYPE> r;
+    const uint32_t first;
+    const bool singles;
+    Piece<TYPE> x[U];
+    float single;
+    __device__ __forceinline__ GradSlice(const E* row, uint32_t V, uint32_t s, bool use)
+        : r(row, V), first(s * (256 * U) + threadIdx.x), singles(s == 0 && threadIdx.x < r.singles), single(0.0f)
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u].none();
+            if (use && first + 256 * u < r.full) x[u].w = load_vec<u32x4>(row + r.piece(first + 256 * u));
+        }
+        if (use && singles) single = (float)row[r.single(threadIdx.x)];
+    }
+    __device__ __forceinline__ void write(E* out, uint32_t label, float coef, Part p, float c)
+    {
+        const bool none = coef == 0.0f || p.sum == 0.0f;
+        const float k = none ? 0.0f : -coef / p.sum;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t v = r.piece(first + 256 * u);
+            if (first + 256 * u >= r.full) continue;
+            float y[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                y[i] = none ? 0.0f : entry(x[u].get(i), c, p.top, k);
+                if (!none && label - v == (uint32_t)i) y[i] += coef;
+            }
+            x[u].put(y);
+            store_vec(out + v, x[u].w);
+        }
+        if (singles) {
+            const uint32_t v = r.single(threadIdx.x);
+            out[v] = (E)(none ? 0.0f : entry(single, c, p.top, k) + (v == label ? coef : 0.0f));
+        }
+    }
+};
+
 // The policy loss' gradient by slices (S of them for the parts, G for the
-// gradient).  Workgroup 0: every token's log probability and the sums over
-// tokens.
+// gradient).  A row's first workgroup writes its log probability and terms;
+// the last of them to finish sums the terms, in the rows' order.  (Without
+// a gradient: G == 1, nothing but that.)
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_policy_grad(Logits in, PolicyArgs a, uint32_t S, uint32_t g, uint32_t G,
                                                      float c, const Part* part, const float* at_label, float* logp,
-                                                     float* stats, void* dlogits, uint64_t ldd)
+                                                     PolicyTerms* terms, uint32_t* ticket, float* stats,
+                                                     void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     __shared__ double s_w[4][4];
-    if (blockIdx.x == 0) {
-        double x[3] = {0.0, 0.0, 0.0};
-        each_joined(in, a.weight, 0, in.rows, S, g, c, part, at_label, [&](uint64_t t, bool use, float lp, Part) {
-            logp[t] = lp;
-            if (use) add_token(a, t, lp, x);
-        });
-        put_policy_stats(a, x, s_w, stats);
-        return;
-    }
-    for (uint64_t b = blockIdx.x - 1; b < in.rows * G; b += gridDim.x - 1) {
+    __shared__ uint32_t s_last;
+    bool last = false;
+    for (uint64_t b = blockIdx.x; b < in.rows * G; b += gridDim.x) {
         const uint64_t t = b / G;
+        const uint32_t s = (uint32_t)(b % G);
+        const bool use = in_use(in, a.weight, t);
+        GradSlice<TYPE> slice(static_cast<const E*>(in.x) + t * in.ld, dlogits ? (uint32_t)in.vocab : 0, s, use);
         Part p = {0.0f, 0.0f};
-        float coef = 0.0f;
-        if (in_use(in, a.weight, t)) {
+        PolicyTerms m = {0.0f, 0.0f, 0.0f, 0.0f};
+        float lp = 0.0f;
+        if (use) {
+            const PolicyRow q(a, t);
+            const float at = at_label[t];
             p = join_slices(part + t * S, S, g, c);
-            coef = a.grad_scale * in.scale * (a.weight[t] * policy_token(a, t, part_logp(p, at_label[t], c)).coef);
+            lp = part_logp(p, at, c);
+            m = policy_terms(a, q, lp);
         }
-        grad_slice<TYPE, kGradU>(static_cast<const E*>(in.x) + t * in.ld, static_cast<E*>(dlogits) + t * ldd,
-                                 (uint32_t)in.vocab, (uint32_t)(b % G), (uint32_t)in.label[t], coef, p, c);
+        if (s == 0 && threadIdx.x == 0) {
+            logp[t] = lp;
+            // (device-scope accesses, each done before the next)
+            float* w = &terms[t].gain;
+            for (int i = 0; i < 3; ++i)
+                __hip_atomic_store(w + i, i == 0 ? m.gain : i == 1 ? m.k : m.clipped, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            last = atomicAdd(ticket, 1u) == (uint32_t)in.rows - 1;
+        }
+        if (dlogits)
+            slice.write(static_cast<E*>(dlogits) + t * ldd, (uint32_t)in.label[t], a.grad_scale * in.scale * m.coef, p, c);
     }
+    if (threadIdx.x == 0) s_last = last;
+    __syncthreads();
+    if (!s_last) return;
+    double x[3] = {0.0, 0.0, 0.0};
+    for (uint64_t t = threadIdx.x; t < in.rows; t += 256)
+        for (int i = 0; i < 3; ++i)
+            x[i] += (double)__hip_atomic_load(&terms[t].gain + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    put_policy_stats(a, x, s_w, stats);
 }
 
 struct PairSums {
@@ -488,7 +566,10 @@ struct PairSums {
 // Pair blockIdx.x: its tokens' log probabilities (S > 1: from the slices),
 // rewards of its two sequences, loss, and the derivative by every token's log
 // probability.  The sequences' bounds: the launch's arguments, or a table.
-__global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint32_t pairs, Blob few,
+struct FewBounds {
+    uint32_t words[65];
+};
+__global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint32_t pairs, FewBounds few,
                                                const uint32_t* many, uint32_t S, uint32_t g, float c, const Part* part,
                                                const float* at_label, float* logp, float* coef, PairSums* sums)
 {
@@ -539,11 +620,12 @@ __global__ void __launch_bounds__(256) k_preference_grad(Logits in, PreferenceAr
     }
     for (uint64_t b = blockIdx.x - 1; b < in.rows * G; b += gridDim.x - 1) {
         const uint64_t t = b / G;
-        Part p = {0.0f, 0.0f};
+        const bool use = has_token(in, t);
+        GradSlice<TYPE> slice(static_cast<const E*>(in.x) + t * in.ld, (uint32_t)in.vocab, (uint32_t)(b % G), use);
         const float q = a.grad_scale * in.scale * coef[t];
-        if (q != 0.0f) p = join_slices(part + t * S, S, g, c);
-        grad_slice<TYPE, kGradU>(static_cast<const E*>(in.x) + t * in.ld, static_cast<E*>(dlogits) + t * ldd,
-                                 (uint32_t)in.vocab, (uint32_t)(b % G), (uint32_t)in.label[t], q, p, c);
+        Part p = {0.0f, 0.0f};
+        if (use) p = join_slices(part + t * S, S, g, c);
+        slice.write(static_cast<E*>(dlogits) + t * ldd, (uint32_t)in.label[t], q, p, c);
     }
 }
 
@@ -556,7 +638,7 @@ struct Cut {
     uint64_t pieces;  // of a row at most
     bool many, row;
 };
-constexpr uint64_t kManyRows = 512;
+constexpr uint64_t kManyRows = 128;
 constexpr uint64_t kMaxRows = 1u << 21;  // of a launch with a workgroup a row (fewer than 2^32 threads)
 constexpr uint32_t kMaxGrid = 1u << 22;
 constexpr uint32_t kHold = 8;  // pieces a thread of k_row holds
@@ -566,12 +648,12 @@ Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
     Cut r;
     r.pieces = vocab / (type == kF32 ? 4 : 8) + 1;
     r.G = (uint32_t)((r.pieces + 256 * kGradU - 1) / (256 * kGradU));
-    r.many = rows >= kManyRows;
-    r.row = r.many && rows <= kMaxRows && r.pieces <= 512 * kHold;
+    r.many = rows >= kManyRows && rows <= kMaxRows;
+    r.row = rows <= kMaxRows && r.pieces <= 512 * kHold;
     // enough workgroups for the chip when there are few rows, none of less
     // than 512 pieces
     const uint64_t most = std::min<uint64_t>(64, (r.pieces + 511) / 512), want = 1024 / std::min<uint64_t>(rows, 1024);
-    const uint64_t S = r.many ? 1 : std::max<uint64_t>(1, std::min(most, want));
+    const uint64_t S = r.row ? 1 : std::max<uint64_t>(1, std::min(most, want));
     r.W = (uint32_t)((r.pieces + S - 1) / S);
     r.S = (uint32_t)((r.pieces + r.W - 1) / r.W);
     for (r.g = 1; r.g < r.S;) r.g *= 2;
@@ -580,6 +662,8 @@ Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
 
 struct Space {
     Part* part;
+    PolicyTerms* terms;
+    uint32_t* ticket;
     float *at_label, *coef;
     PairSums* sums;
     uint32_t* bounds;
@@ -589,6 +673,8 @@ Space carve(void* ws, uint64_t rows, uint32_t S, uint32_t pairs, size_t* bytes)
     Carve c(ws);
     Space r;
     r.part = c.take<Part>(rows * S);
+    r.terms = c.take<PolicyTerms>(pairs ? 0 : rows);
+    r.ticket = c.take<uint32_t>(1);
     r.at_label = c.take<float>(rows);
     r.coef = c.take<float>(pairs ? rows : 0);
     r.sums = c.take<PairSums>(pairs);
@@ -620,15 +706,15 @@ void by_type(uint32_t type, F f)
 }
 
 template <bool GRAD>
-void launch_row(const Cut& cut, const Logits& in, const PolicyArgs& a, float c, float* logp, float* lse, Part* part,
-                void* dlogits, uint64_t ldd, hipStream_t s)
+void launch_row(const Cut& cut, const Logits& in, const PolicyArgs& a, float c, float* logp, float* lse, const Space& sp,
+                PolicyTerms* terms, void* dlogits, uint64_t ldd, hipStream_t s)
 {
     by_type(in.type, [&](auto ty) {
         constexpr int TY = decltype(ty)::value;
         auto go = [&](auto kern, uint64_t most) {
             const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kHold * 64 - 1) / (kHold * 64) * 64);
             hipLaunchKernelGGL(kern, dim3((uint32_t)in.rows), dim3((uint32_t)std::min(threads, most)), 0, s, in, a, c,
-                               logp, lse, part, dlogits, ldd);
+                               logp, lse, GRAD ? nullptr : sp.part, sp.at_label, sp.ticket, terms, dlogits, ldd);
         };
         if (cut.pieces <= 1024 * kHold)
             go(k_row<TY, 512, kHold, GRAD>, 512);
@@ -639,20 +725,20 @@ void launch_row(const Cut& cut, const Logits& in, const PolicyArgs& a, float c, 
 
 // The rows in use: log probabilities (where S is 1, or a workgroup takes a
 // row), else the parts for who joins them.
-hipError_t rows_run(const Cut& cut, const Logits& in, const float* weight, const Space& sp, float* logp, float* lse,
-                    hipStream_t s)
+hipError_t rows_run(const Cut& cut, const Logits& in, const PolicyArgs* policy, const Space& sp, float* logp,
+                    float* lse, hipStream_t s)
 {
     const float c = in.scale * kLog2e;
+    const PolicyArgs a = policy ? *policy : PolicyArgs{};
+    PolicyTerms* terms = policy ? sp.terms : nullptr;
     timer_begin(kTLossRows, s);
     if (cut.row) {
-        PolicyArgs a = {};
-        a.weight = weight;
-        launch_row<false>(cut, in, a, c, logp, lse, sp.part, nullptr, 0, s);
+        launch_row<false>(cut, in, a, c, logp, lse, sp, terms, nullptr, 0, s);
     } else {
         const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kMaxGrid);
         by_type(in.type, [&](auto ty) {
-            hipLaunchKernelGGL((k_slices<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, weight, cut.S, cut.W,
-                               c, sp.part, sp.at_label, logp, lse);
+            hipLaunchKernelGGL((k_slices<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a.weight, cut.S, cut.W,
+                               c, sp.part, sp.at_label, logp, lse, a, terms, sp.ticket);
         });
     }
     timer_end(kTLossRows, s);
@@ -683,22 +769,24 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
     const Space sp = carve(ws, in.rows, cut.S, 0, nullptr);
     const float c = in.scale * kLog2e;
-    const bool fused = dlogits && cut.many && in.rows <= kMaxRows;
+    const bool fused = dlogits && cut.many;
     if (fused) {
         timer_begin(kTLossRows, s);
-        launch_row<true>(cut, in, a, c, logp, nullptr, nullptr, dlogits, ldd, s);
+        launch_row<true>(cut, in, a, c, logp, nullptr, sp, sp.terms, dlogits, ldd, s);
         timer_end(kTLossRows, s);
     } else {
-        hipError_t e = rows_run(cut, in, a.weight, sp, logp, nullptr, s);
+        hipError_t e = rows_run(cut, in, &a, sp, logp, nullptr, s);
         if (e != hipSuccess) return e;
     }
-    if (cut.many) hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, in, a, logp, stats);
-    if (!fused && (dlogits || !cut.many)) {
-        const uint32_t grid = dlogits ? (uint32_t)std::min<uint64_t>(in.rows * cut.G, kMaxGrid) + 1 : 1;
+    if (fused || (!dlogits && cut.S == 1))
+        hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, in.rows, a, sp.terms, stats);
+    else {
+        const uint32_t G = dlogits ? cut.G : 1;
+        const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * G, kMaxGrid);
         timer_begin(kTLossGrad, s);
         by_type(in.type, [&](auto ty) {
             hipLaunchKernelGGL((k_policy_grad<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a, cut.S, cut.g,
-                               cut.G, c, sp.part, sp.at_label, logp, stats, dlogits, ldd);
+                               G, c, sp.part, sp.at_label, logp, sp.terms, sp.ticket, stats, dlogits, ldd);
         });
         timer_end(kTLossGrad, s);
     }
@@ -714,9 +802,9 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
     hipError_t e = rows_run(cut, in, nullptr, sp, logp, nullptr, s);
     if (e != hipSuccess) return e;
     const size_t words = 2 * (size_t)pairs + 1;
-    Blob few = {};
+    FewBounds few = {};
     const uint32_t* many = nullptr;
-    if (words <= kBlobWords) {
+    if (words <= sizeof(few.words) / sizeof(few.words[0])) {
         std::copy(bounds, bounds + words, few.words);
     } else {
         e = upload(sp.bounds, bounds, words * sizeof(uint32_t), s);

@@ -32,6 +32,15 @@ struct Elem<kF16> {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// Element i of 16 bytes of a type, as fp32.
+template <int TYPE>
+__device__ __forceinline__ float unpack(u32x4 w, int i)
+{
+    if (TYPE == kF32) return __uint_as_float(w[i & 3]);
+    if (TYPE == kBf16) return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1]));
+}
+
 // A vector from p on, at any element-aligned address (one access: gfx950 takes
 // unaligned vector accesses to global memory), streamed: marked nontemporal.
 template <class V, class E>

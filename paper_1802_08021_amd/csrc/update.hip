@@ -16,20 +16,23 @@ namespace sparcml {
 namespace {
 
 // map[first[t] + i] = {t, i} for the pieces i of tensor t.
-__global__ void k_tensor_map(const TensorDesc* desc, const uint32_t* first, uint2* map)
+__global__ void k_tensor_map(const TensorDesc* desc, const uint32_t* first, uint2* map, uint32_t* ticket)
 {
     const uint32_t t = blockIdx.x;
-    const uint32_t pieces = (uint32_t)((desc[t].n + kTensorChunk - 1) / kTensorChunk);
+    if (t == 0 && threadIdx.x < kTickets) ticket[threadIdx.x * kTicketStride] = 0;
+    const TensorDesc d = desc[t];
+    const uint32_t pieces = d.n ? (uint32_t)((d.n + d.shift + kTensorChunk - 1) / kTensorChunk) : 0;
     for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) map[first[t] + i] = make_uint2(t, i);
 }
 
-// Elements e .. e + 3 of an array of n as fp32, zeros past the end.
+// Elements e .. e + 3 of an array of n as fp32, zeros outside it (e may lie
+// before the array: below zero, as a large number).
 template <int TYPE>
 __device__ __forceinline__ f32x4 get4(const void* p, uint64_t e, uint64_t n)
 {
     typedef typename Elem<TYPE>::type E;
     const E* q = static_cast<const E*>(p) + e;
-    if (e + 4 <= n) return __builtin_convertvector(load_vec<typename Elem<TYPE>::vec4>(q), f32x4);
+    if (e < n && e + 4 <= n) return __builtin_convertvector(load_vec<typename Elem<TYPE>::vec4>(q), f32x4);
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -43,7 +46,7 @@ __device__ __forceinline__ void put4(void* p, uint64_t e, uint64_t n, f32x4 x)
 {
     typedef typename Elem<TYPE>::type E;
     E* q = static_cast<E*>(p) + e;
-    if (e + 4 <= n) {
+    if (e < n && e + 4 <= n) {
         store_vec(q, __builtin_convertvector(x, typename Elem<TYPE>::vec4));
     } else {
 #pragma unroll
@@ -111,14 +114,13 @@ __device__ __forceinline__ uint32_t block_exponent(f32x4 x)
     return max(e, 35u) - 8u;
 }
 
-// One AdamW step of piece blockIdx.x / (4096 / (1024 U)) of the map: 1024
-// elements a workgroup and round, four a lane, so that a wave holds exactly
-// one block of the 8-bit form.
-template <int BITS, int GT, int CT, int U>
+// One AdamW step: a quarter of a piece of the map a workgroup, four elements
+// a lane, so that a wave holds exactly one block of the 8-bit form.
+template <int BITS, int GT, int CT>
 __global__ void __launch_bounds__(256) k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
                                                uint64_t pieces, AdamwStep a, const float* __restrict__ clip)
 {
-    constexpr uint32_t kSub = kTensorChunk / (1024 * U);
+    constexpr uint32_t kSub = kTensorChunk / 1024;
     float f = a.gs;
     if (clip) {
         const float c = clip[1];
@@ -131,11 +133,10 @@ __global__ void __launch_bounds__(256) k_adamw(const TensorDesc* __restrict__ de
         const TensorDesc d = desc[at.x];
         const float keep = (float)(1.0 - a.lr * (double)d.lr_scale * (double)d.decay);
         const float rate = (float)(a.rate * (double)d.lr_scale);
-        const uint64_t e0 = (uint64_t)at.y * kTensorChunk + (uint64_t)(w % kSub) * (1024 * U) + (uint32_t)wv * 256;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint64_t b = e0 + (uint32_t)u * 1024, e = b + (uint32_t)lane * 4;
-            if (b >= d.n) break;  // a whole wave's elements
+        // the wave's first element and the lane's (below zero: before the tensor)
+        const uint64_t b = (uint64_t)at.y * kTensorChunk + (uint32_t)(w % kSub) * 1024 + (uint32_t)wv * 256 - d.shift;
+        const uint64_t e = b + (uint32_t)lane * 4;
+        if ((int64_t)b < (int64_t)d.n) {
             f32x4 p = get4<kF32>(d.param, e, d.n);
             const f32x4 g = get4<GT>(d.grad, e, d.n) * f;
             f32x4 m, v;
@@ -188,37 +189,75 @@ __device__ __forceinline__ double block_sum(double x, double* s_w)
     return (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
 }
 
-// partial[b] = sum of squares of pieces b, b + gridDim.x, ...
+// Norm of all gradients: workgroup b sums the squares of pieces b, b + G, ...,
+// the last workgroup to finish the partial sums, in their order.
 template <int GT>
 __global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
-                                              uint64_t pieces, double* partial)
+                                              uint64_t pieces, double* partial, uint32_t* ticket, double gs,
+                                              double max_norm, float* out)
 {
-    __shared__ double s_w[4];
-    double acc = 0.0;
+    __shared__ double s_w[4], s_end[4];
+    __shared__ uint32_t s_last;
+    double acc[2] = {0.0, 0.0};
+    auto add = [&](const float* x, int n) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) acc[i & 1] = fma((double)x[i], (double)x[i], acc[i & 1]);
+    };
+    constexpr int N = GT == kF32 ? 4 : 8, R = kTensorChunk / (256 * N);  // elements of 16 bytes; accesses a piece
+    typedef typename Elem<GT>::type E;
     for (uint64_t c = blockIdx.x; c < pieces; c += gridDim.x) {
         const uint2 at = map[c];
-        const TensorDesc d = desc[at.x];
-        const uint64_t e0 = (uint64_t)at.y * kTensorChunk + (uint64_t)threadIdx.x * 4;
+        const E* grad = static_cast<const E*>(desc[at.x].grad);
+        const uint64_t n = desc[at.x].n, e0 = (uint64_t)at.y * kTensorChunk - desc[at.x].shift;
+        const uint64_t e = e0 + (uint64_t)threadIdx.x * N;
+        if (e0 < n && e0 + kTensorChunk <= n) {  // a whole piece
+            u32x4 w[R];
 #pragma unroll
-        for (int u = 0; u < (int)kTensorChunk / 1024; ++u) {
-            const f32x4 g = get4<GT>(d.grad, e0 + (uint32_t)u * 1024, d.n);
+            for (int u = 0; u < R; ++u) w[u] = load_vec<u32x4>(grad + e + u * (256 * N));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc = fma((double)g[i], (double)g[i], acc);
+            for (int u = 0; u < R; ++u) {
+                float x[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = unpack<GT>(w[u], i);
+                add(x, N);
+            }
+        } else {
+            for (int u = 0; u < R * N / 4; ++u) {
+                const f32x4 x = get4<GT>(grad, e0 + (uint64_t)threadIdx.x * 4 + (uint32_t)u * 1024, n);
+                const float y[4] = {x[0], x[1], x[2], x[3]};
+                add(y, 4);
+            }
         }
     }
-    acc = block_sum(acc, s_w);
-    if (threadIdx.x == 0) partial[blockIdx.x] = acc;
-}
-
-__global__ void __launch_bounds__(256) k_norm_end(const double* partial, uint32_t parts, double gs, double max_norm,
-                                                  float* out)
-{
-    __shared__ double s_w[4];
-    double acc = 0.0;
-    for (uint32_t i = threadIdx.x; i < parts; i += 256) acc += partial[i];
-    acc = block_sum(acc, s_w);
+    const double sum = block_sum(acc[0] + acc[1], s_w);
     if (threadIdx.x == 0) {
-        const float norm = (float)(gs * sqrt(acc));
+        __hip_atomic_store(&partial[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // Device-scope accesses only, each done before the next: they bypass
+        // the XCDs' own L2s, which a fence would write back whole (22 ns a
+        // workgroup); and a counter takes 12 ns an add, so the workgroups
+        // count in groups and the groups' last ones in one.
+        constexpr uint32_t kGroups = kTickets - 1;
+        const uint32_t group = blockIdx.x % kGroups, size = (gridDim.x - group + kGroups - 1) / kGroups;
+        uint32_t* mine = ticket + group * kTicketStride;
+        uint32_t* top = ticket + kGroups * kTicketStride;
+        bool last = false;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (atomicAdd(mine, 1u) == size - 1) {
+            __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            last = atomicAdd(top, 1u) == min(gridDim.x, kGroups) - 1;
+            if (last) __hip_atomic_store(top, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        s_last = last;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    double all = 0.0;
+    for (uint32_t i = threadIdx.x; i < gridDim.x; i += 256)
+        all += __hip_atomic_load(&partial[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    all = block_sum(all, s_end);
+    if (threadIdx.x == 0) {
+        const float norm = (float)(gs * sqrt(all));
         const float c = (float)(max_norm / ((double)norm + 1e-6));
         out[0] = norm;
         out[1] = isfinite(norm) ? fminf(1.0f, c) : 0.0f;
@@ -228,9 +267,8 @@ __global__ void __launch_bounds__(256) k_norm_end(const double* partial, uint32_
 template <int BITS, int GT, int CT>
 void launch_adamw(const TensorTab& t, uint64_t pieces, const AdamwStep& a, const float* clip, hipStream_t s)
 {
-    constexpr int U = 1;
-    const uint64_t grid = std::min<uint64_t>(pieces * (kTensorChunk / (1024 * U)), 1u << 22);
-    hipLaunchKernelGGL((k_adamw<BITS, GT, CT, U>), dim3((uint32_t)grid), dim3(256), 0, s, t.desc, t.map, pieces, a, clip);
+    const uint64_t grid = std::min<uint64_t>(pieces * (kTensorChunk / 1024), 1u << 22);
+    hipLaunchKernelGGL((k_adamw<BITS, GT, CT>), dim3((uint32_t)grid), dim3(256), 0, s, t.desc, t.map, pieces, a, clip);
 }
 
 template <int BITS, int GT>
@@ -265,6 +303,7 @@ TensorTab tensors_carve(void* ws, uint32_t count, uint64_t chunks, size_t* bytes
     t.first = c.take<uint32_t>(count);
     t.map = c.take<uint2>(chunks);
     t.partial = c.take<double>(kNormParts);
+    t.ticket = c.take<uint32_t>(kTickets * kTicketStride);
     if (bytes) *bytes = c.used;
     return t;
 }
@@ -276,12 +315,12 @@ hipError_t tensors_prepare_run(uint32_t count, const TensorDesc* host, uint64_t 
     uint64_t at = 0;
     for (uint32_t i = 0; i < count; ++i) {
         first[i] = (uint32_t)at;
-        at += (host[i].n + kTensorChunk - 1) / kTensorChunk;
+        at += tensor_chunks(host[i].n, host[i].shift);
     }
     hipError_t e = upload(t.desc, host, count * sizeof(TensorDesc), s);
     if (e == hipSuccess) e = upload(t.first, first.data(), count * sizeof(uint32_t), s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_tensor_map, dim3(count), dim3(256), 0, s, t.desc, t.first, t.map);
+    hipLaunchKernelGGL(k_tensor_map, dim3(count), dim3(256), 0, s, t.desc, t.first, t.map, t.ticket);
     return hipGetLastError();
 }
 
@@ -289,17 +328,18 @@ hipError_t grad_norm_run(uint32_t count, uint64_t chunks, uint32_t gtype, double
                          float* out, void* ws, hipStream_t s)
 {
     const TensorTab t = tensors_carve(ws, count, chunks, nullptr);
-    const uint32_t parts = (uint32_t)std::min<uint64_t>(chunks, kNormParts);
+    const uint32_t parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(chunks, kNormParts));
     timer_begin(kTGradNorm, s);
-    if (parts) {
-        if (gtype == kF32)
-            hipLaunchKernelGGL((k_norm<kF32>), dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial);
-        else if (gtype == kBf16)
-            hipLaunchKernelGGL((k_norm<kBf16>), dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial);
-        else
-            hipLaunchKernelGGL((k_norm<kF16>), dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial);
-    }
-    hipLaunchKernelGGL(k_norm_end, dim3(1), dim3(256), 0, s, t.partial, parts, grad_scale, max_norm, out);
+    auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial, t.ticket, grad_scale,
+                           max_norm, out);
+    };
+    if (gtype == kF32)
+        go(k_norm<kF32>);
+    else if (gtype == kBf16)
+        go(k_norm<kBf16>);
+    else
+        go(k_norm<kF16>);
     timer_end(kTGradNorm, s);
     return hipGetLastError();
 }

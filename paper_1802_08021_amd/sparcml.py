@@ -215,8 +215,13 @@ def _torch():
 
 
 def _stream_ptr(device) -> int:
+    """The current stream of a device as a hipStream_t.  (torch's own accessor
+    of the raw handle: building a Stream object takes 2 us of a small call.)"""
     torch = _torch()
-    return int(torch.cuda.current_stream(device).cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is None or device.index is None:
+        return int(torch.cuda.current_stream(device).cuda_stream)
+    return int(raw(device.index))
 
 
 def _ptr(t) -> int:
@@ -727,10 +732,11 @@ class _TensorPlan:
                                              _ptr(self.ws), self.ws.numel(), _stream_ptr(self.dev)),
                "sparcml_tensors_prepare")
         self.out = torch.empty(2, dtype=torch.float32, device=self.dev)
+        self._plan, self._out = ctypes.byref(self.plan), self.out.data_ptr()
 
     def _norm(self, max_norm, grad_scale):
-        _check(lib().sparcml_grad_norm(ctypes.byref(self.plan), grad_scale, max_norm, self.out.data_ptr(),
-                                       _stream_ptr(self.dev)), "sparcml_grad_norm")
+        _check(lib().sparcml_grad_norm(self._plan, grad_scale, max_norm, self._out, _stream_ptr(self.dev)),
+               "sparcml_grad_norm")
 
 
 class GradNormCall(_TensorPlan):
@@ -803,6 +809,7 @@ class AdamwCall(_TensorPlan):
 
         super().__init__(grads, bits, ctype, fill)
         self.args = AdamwArgs()
+        self._args = ctypes.byref(self.args)
         self._keep = (params, grads, m, v, m_scale, v_scale, copies)
 
     def grad_norm(self, max_norm: float = float("inf"), grad_scale: float = 1.0):
@@ -822,8 +829,8 @@ class AdamwCall(_TensorPlan):
         a = self.args
         a.lr, a.beta1, a.beta2, a.eps, a.grad_scale = lr, beta1, beta2, eps, grad_scale
         a.seed, a.step = seed & (2**64 - 1), step
-        _check(lib().sparcml_adamw(ctypes.byref(self.plan), ctypes.byref(a), _ptr(clip), _stream_ptr(self.dev)),
-               "sparcml_adamw")
+        _check(lib().sparcml_adamw(self._plan, self._args, None if clip is None else clip.data_ptr(),
+                                   _stream_ptr(self.dev)), "sparcml_adamw")
 
 
 class _LogitsCall:
@@ -842,6 +849,9 @@ class _LogitsCall:
         self.ws = alloc_workspace(workspace_size(op, pairs, self.rows, self.vocab), self.dev)
         self.logp = torch.empty(self.rows, dtype=torch.float32, device=self.dev)
         self._keep = [logits, labels]
+        # what every run passes
+        self._in, self._logp = ctypes.byref(self.logits), self.logp.data_ptr()
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
 
     def _per_row(self, t, name):
         if t is not None:
@@ -867,6 +877,7 @@ class _LogitsCall:
             self._ldd = 0
         self.dlogits = dlogits
         self.stats = torch.empty(4, dtype=torch.float32, device=self.dev)
+        self._outs = (self._logp, self.stats.data_ptr(), _ptr(dlogits), self._ldd, *self._ws)
 
 
 class TokenLogprobCall(_LogitsCall):
@@ -877,10 +888,10 @@ class TokenLogprobCall(_LogitsCall):
     def __init__(self, logits, labels, scale: float = 1.0):
         super().__init__(logits, labels, scale, OP_LOGPROB)
         self.lse = _torch().empty_like(self.logp)
+        self._outs = (self._logp, self.lse.data_ptr(), *self._ws)
 
     def run(self) -> None:
-        _check(lib().sparcml_token_logprob(ctypes.byref(self.logits), _ptr(self.logp), _ptr(self.lse), _ptr(self.ws),
-                                           self.ws.numel(), _stream_ptr(self.dev)), "sparcml_token_logprob")
+        _check(lib().sparcml_token_logprob(self._in, *self._outs, _stream_ptr(self.dev)), "sparcml_token_logprob")
 
 
 def token_logprob(logits, labels, scale: float = 1.0):
@@ -905,12 +916,12 @@ class PolicyLossCall(_LogitsCall):
             raise ValueError("old, adv and weight must be given")
         self.args = PolicyArgs(self._per_row(old, "old"), self._per_row(ref, "ref"), self._per_row(adv, "adv"),
                                self._per_row(weight, "weight"), clip_lo, clip_hi, kl, grad_scale)
+        self._args = ctypes.byref(self.args)
         self._gradient(dlogits)
 
     def run(self) -> None:
-        _check(lib().sparcml_policy_loss(ctypes.byref(self.logits), ctypes.byref(self.args), _ptr(self.logp),
-                                         _ptr(self.stats), _ptr(self.dlogits), self._ldd, _ptr(self.ws),
-                                         self.ws.numel(), _stream_ptr(self.dev)), "sparcml_policy_loss")
+        _check(lib().sparcml_policy_loss(self._in, self._args, *self._outs, _stream_ptr(self.dev)),
+               "sparcml_policy_loss")
 
 
 def policy_loss(logits, labels, old, adv, weight, **more):
@@ -942,10 +953,8 @@ class PreferenceLossCall(_LogitsCall):
         self._gradient(dlogits)
 
     def run(self) -> None:
-        _check(lib().sparcml_preference_loss(ctypes.byref(self.logits), self.pairs, self.bounds, self.ref, *self.rates,
-                                             _ptr(self.logp), _ptr(self.stats), _ptr(self.dlogits), self._ldd,
-                                             _ptr(self.ws), self.ws.numel(), _stream_ptr(self.dev)),
-               "sparcml_preference_loss")
+        _check(lib().sparcml_preference_loss(self._in, self.pairs, self.bounds, self.ref, *self.rates, *self._outs,
+                                             _stream_ptr(self.dev)), "sparcml_preference_loss")
 
 
 def preference_loss(logits, labels, bounds, **more):
