@@ -269,7 +269,7 @@ struct TensorTab {
     double* partial;   // [kNormParts]
     uint32_t* ticket;  // [kTickets * kTicketStride], 0 between calls
 };
-constexpr uint32_t kNormParts = 2048;
+constexpr uint32_t kNormParts = 1024;
 // Counters of a norm's finished workgroups: kTickets - 1 groups', and the
 // groups' own; a 128-byte line each.
 constexpr uint32_t kTickets = 33, kTicketStride = 32;

@@ -270,7 +270,7 @@ struct Own {
 // read once more (mostly from the cache), the singles one a thread.  Writes
 // the log probability, lse and part where wanted, and with GRAD the gradient
 // of the policy loss.
-template <int TYPE, int THREADS, int NV, bool GRAD>
+template <int TYPE, int THREADS, int NV, bool GRAD, bool KEEP>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
 k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, float* at_label, uint32_t* ticket,
       PolicyTerms* terms, void* dlogits, uint64_t ldd)
@@ -300,7 +300,7 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         x[j].none();
-        if (tid + step * j < r.full) x[j].w = load_vec<u32x4>(row + r.piece(tid + step * j));
+        if (tid + step * j < r.full) x[j].w = load_vec<u32x4, KEEP>(row + r.piece(tid + step * j));
     }
     const float single = tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
     if (tid == 0) s_x = (float)row[label];
@@ -310,7 +310,7 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             y[u].none();
-            if (j + step * u < r.full) y[u].w = load_keep<u32x4>(row + r.piece(j + step * u));
+            if (j + step * u < r.full) y[u].w = load_vec<u32x4, true>(row + r.piece(j + step * u));
         }
         own.add(y, U, c);
     }
@@ -377,7 +377,7 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
 // Slice s of a row: pieces [s W, (s + 1) W); slice 0 takes the singles too.
 // (M, Z) of every slice of every row in use, the token's logit beside them;
 // with one slice a row its log probability (lse, terms) at once.
-template <int TYPE>
+template <int TYPE, bool KEEP>
 __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, uint32_t S, uint32_t W, float c,
                                                 Part* part, float* at_label, float* logp, float* lse, PolicyArgs a,
                                                 PolicyTerms* terms, uint32_t* ticket)
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, 
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 x[u].none();
-                if (j + 256 * u < end) x[u].w = load_vec<u32x4>(row + r.piece(j + 256 * u));
+                if (j + 256 * u < end) x[u].w = load_vec<u32x4, KEEP>(row + r.piece(j + 256 * u));
             }
             own.add(x, 4, c);
         }
@@ -631,8 +631,17 @@ __global__ void __launch_bounds__(256) k_preference_grad(Logits in, PreferenceAr
 
 // ---------------------------------------------------------------- host
 
-// How a call's rows are taken: cut into S slices of W pieces for the sums, G
-// slices for a gradient pass; `row`: log probabilities by a workgroup a row.
+// How a call's rows are taken.  `row`: log probabilities by a workgroup a
+// row (k_row), else by S slices of W pieces (k_slices), joined by groups of g
+// lanes; `many`: a policy loss and its gradient by a workgroup a row; G: slices
+// of a gradient pass.  The rules follow from (us, bf16, rows x vocabulary):
+//   row, rows of up to 4096 pieces (32768 16-bit logits): 8 x 32000 5.2 against
+//     6.1 by slices, 256 x 32000 6.4 / 8.3, 1000 x 32000 14.5 / 14.5; beyond,
+//     slices: 8 x 65000 7.3 / 6.1, 1000 x 65000 28.3 / 24.1
+//   many, from 128 rows on: 256 x 32000 13.3 against 18.6 in two passes, 256 x
+//     131072 34 / 46; 128 x 131072 26 / 28; 64 x 131072 25 / 18
+//   slices of few rows: about 1024 workgroups together (300 x 131072 19 with as
+//     many, 23 with four times as many), none of less than 512 pieces
 struct Cut {
     uint32_t S, W, g, G;
     uint64_t pieces;  // of a row at most
@@ -648,10 +657,8 @@ Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
     Cut r;
     r.pieces = vocab / (type == kF32 ? 4 : 8) + 1;
     r.G = (uint32_t)((r.pieces + 256 * kGradU - 1) / (256 * kGradU));
-    r.many = rows >= kManyRows && rows <= kMaxRows;
-    r.row = rows <= kMaxRows && r.pieces <= 512 * kHold;
-    // enough workgroups for the chip when there are few rows, none of less
-    // than 512 pieces
+    r.many = rows >= kManyRows;
+    r.row = r.pieces <= 512 * kHold;
     const uint64_t most = std::min<uint64_t>(64, (r.pieces + 511) / 512), want = 1024 / std::min<uint64_t>(rows, 1024);
     const uint64_t S = r.row ? 1 : std::max<uint64_t>(1, std::min(most, want));
     r.W = (uint32_t)((r.pieces + S - 1) / S);
@@ -705,26 +712,52 @@ void by_type(uint32_t type, F f)
         f(std::integral_constant<int, kF16>());
 }
 
-template <bool GRAD>
-void launch_row(const Cut& cut, const Logits& in, const PolicyArgs& a, float c, float* logp, float* lse, const Space& sp,
-                PolicyTerms* terms, void* dlogits, uint64_t ldd, hipStream_t s)
+// Of 1024 threads only where rows are longer than those can hold (8192 x 50000
+// bf16: 302 us with 1024, 279 with 512).
+template <bool GRAD, bool KEEP>
+void launch_row(const Cut& cut, Logits in, PolicyArgs a, float* logp, float* lse, const Space& sp, PolicyTerms* terms,
+                void* dlogits, uint64_t ldd, hipStream_t s)
 {
+    const float c = in.scale * kLog2e;
+    const uint64_t most = cut.pieces <= 1024 * kHold ? 512 : 1024;
+    const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kHold * 64 - 1) / (kHold * 64) * 64);
+    const uint64_t rows = in.rows, size = in.type == kF32 ? 4 : 2;
+    Part* part = GRAD ? nullptr : sp.part;
+    float* at_label = sp.at_label;
     by_type(in.type, [&](auto ty) {
         constexpr int TY = decltype(ty)::value;
-        auto go = [&](auto kern, uint64_t most) {
-            const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kHold * 64 - 1) / (kHold * 64) * 64);
-            hipLaunchKernelGGL(kern, dim3((uint32_t)in.rows), dim3((uint32_t)std::min(threads, most)), 0, s, in, a, c,
-                               logp, lse, GRAD ? nullptr : sp.part, sp.at_label, sp.ticket, terms, dlogits, ldd);
-        };
-        if (cut.pieces <= 1024 * kHold)
-            go(k_row<TY, 512, kHold, GRAD>, 512);
-        else
-            go(k_row<TY, 1024, kHold, GRAD>, 1024);
+        for (uint64_t r0 = 0; r0 < rows; r0 += kMaxRows) {
+            const dim3 grid((uint32_t)std::min(rows - r0, kMaxRows)), block((uint32_t)std::min(threads, most));
+            if (most == 512)
+                hipLaunchKernelGGL((k_row<TY, 512, kHold, GRAD, KEEP>), grid, block, 0, s, in, a, c, logp, lse, part,
+                                   at_label, sp.ticket, terms, dlogits, ldd);
+            else
+                hipLaunchKernelGGL((k_row<TY, 1024, kHold, GRAD, KEEP>), grid, block, 0, s, in, a, c, logp, lse, part,
+                                   at_label, sp.ticket, terms, dlogits, ldd);
+            // the next rows
+            auto on = [](auto*& p, uint64_t n) {
+                if (p) p += n;
+            };
+            in.x = static_cast<const uint8_t*>(in.x) + grid.x * in.ld * size;
+            if (dlogits) dlogits = static_cast<uint8_t*>(dlogits) + grid.x * ldd * size;
+            on(in.label, grid.x);
+            on(a.old_logp, grid.x);
+            on(a.ref_logp, grid.x);
+            on(a.adv, grid.x);
+            on(a.weight, grid.x);
+            on(logp, grid.x);
+            on(lse, grid.x);
+            on(part, grid.x);
+            on(at_label, grid.x);
+            on(terms, grid.x);
+        }
     });
 }
 
 // The rows in use: log probabilities (where S is 1, or a workgroup takes a
 // row), else the parts for who joins them.
+// KEEP: the logits are read again soon.
+template <bool KEEP>
 hipError_t rows_run(const Cut& cut, const Logits& in, const PolicyArgs* policy, const Space& sp, float* logp,
                     float* lse, hipStream_t s)
 {
@@ -733,11 +766,11 @@ hipError_t rows_run(const Cut& cut, const Logits& in, const PolicyArgs* policy, 
     PolicyTerms* terms = policy ? sp.terms : nullptr;
     timer_begin(kTLossRows, s);
     if (cut.row) {
-        launch_row<false>(cut, in, a, c, logp, lse, sp, terms, nullptr, 0, s);
+        launch_row<false, KEEP>(cut, in, a, logp, lse, sp, terms, nullptr, 0, s);
     } else {
         const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kMaxGrid);
         by_type(in.type, [&](auto ty) {
-            hipLaunchKernelGGL((k_slices<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a.weight, cut.S, cut.W,
+            hipLaunchKernelGGL((k_slices<decltype(ty)::value, KEEP>), dim3(grid), dim3(256), 0, s, in, a.weight, cut.S, cut.W,
                                c, sp.part, sp.at_label, logp, lse, a, terms, sp.ticket);
         });
     }
@@ -755,7 +788,7 @@ hipError_t logprob_run(const Logits& in, float* logp, float* lse, void* ws, hipS
 {
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
     const Space sp = carve(ws, in.rows, cut.S, 0, nullptr);
-    hipError_t e = rows_run(cut, in, nullptr, sp, logp, lse, s);
+    hipError_t e = rows_run<false>(cut, in, nullptr, sp, logp, lse, s);
     if (e != hipSuccess || cut.S == 1) return e;
     const uint32_t grid = (uint32_t)((in.rows * cut.g + 255) / 256);
     hipLaunchKernelGGL(k_join, dim3(grid), dim3(256), 0, s, in, (const float*)nullptr, cut.S, cut.g,
@@ -772,10 +805,10 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
     const bool fused = dlogits && cut.many;
     if (fused) {
         timer_begin(kTLossRows, s);
-        launch_row<true>(cut, in, a, c, logp, nullptr, sp, sp.terms, dlogits, ldd, s);
+        launch_row<true, false>(cut, in, a, logp, nullptr, sp, sp.terms, dlogits, ldd, s);
         timer_end(kTLossRows, s);
     } else {
-        hipError_t e = rows_run(cut, in, &a, sp, logp, nullptr, s);
+        hipError_t e = rows_run<false>(cut, in, &a, sp, logp, nullptr, s);
         if (e != hipSuccess) return e;
     }
     if (fused || (!dlogits && cut.S == 1))
@@ -799,7 +832,11 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
     const Space sp = carve(ws, in.rows, cut.S, pairs, nullptr);
     const float c = in.scale * kLog2e;
-    hipError_t e = rows_run(cut, in, nullptr, sp, logp, nullptr, s);
+    // logits that fit the 256 MB cache are found there by the gradient pass (1000
+    // rows of 131072 bf16: 132 -> 127 us; of 4000: 498 -> 522, so not those)
+    const bool fits = in.rows * in.ld * (in.type == kF32 ? 4 : 2) <= (256u << 20);
+    hipError_t e = dlogits && fits ? rows_run<true>(cut, in, nullptr, sp, logp, nullptr, s)
+                                   : rows_run<false>(cut, in, nullptr, sp, logp, nullptr, s);
     if (e != hipSuccess) return e;
     const size_t words = 2 * (size_t)pairs + 1;
     FewBounds few = {};

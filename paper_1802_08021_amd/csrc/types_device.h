@@ -42,19 +42,14 @@ __device__ __forceinline__ float unpack(u32x4 w, int i)
 }
 
 // A vector from p on, at any element-aligned address (one access: gfx950 takes
-// unaligned vector accesses to global memory), streamed: marked nontemporal.
-template <class V, class E>
+// unaligned vector accesses to global memory); streamed, marked nontemporal,
+// unless it is read once more soon (KEEP).
+template <class V, bool KEEP = false, class E>
 __device__ __forceinline__ V load_vec(const E* p)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
-    return __builtin_nontemporal_load(reinterpret_cast<const U*>(p));
-}
-// The same for data that is read once more soon.
-template <class V, class E>
-__device__ __forceinline__ V load_keep(const E* p)
-{
-    typedef V U __attribute__((aligned(sizeof(E))));
-    return *reinterpret_cast<const U*>(p);
+    const U* q = reinterpret_cast<const U*>(p);
+    return KEEP ? *q : __builtin_nontemporal_load(q);
 }
 template <class V, class E>
 __device__ __forceinline__ void store_vec(E* p, V v)

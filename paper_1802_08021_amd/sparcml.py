@@ -12,6 +12,8 @@ from __future__ import annotations
 import ctypes
 import os
 
+import numpy as np
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "libsparcml.so")
 
@@ -41,6 +43,11 @@ class Tensor(ctypes.Structure):
         ("decay", ctypes.c_float),
         ("lr_scale", ctypes.c_float),
     ]
+
+
+# The same for an array of them, to be filled by columns.
+_TENSOR_RECORD = np.dtype([(name, np.uint64) for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy", "n")]
+                          + [("decay", np.float32), ("lr_scale", np.float32)])
 
 
 class Tensors(ctypes.Structure):
@@ -707,30 +714,42 @@ def adamw_state(params, state_bits: int = 32):
     return codes(), codes(), scales(), scales()
 
 
-class _TensorPlan:
-    """A prepared plan of a model's tensors and its workspace."""
+def _pointers(tensors, name: str, dtypes, numels, index: int, what: str):
+    """Addresses of one list of a model's tensors, each checked."""
+    torch = _torch()
+    for t, (x, n) in enumerate(zip(tensors, numels)):
+        if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous():
+            raise ValueError(f"{name}[{t}] must be a contiguous CUDA (HIP) tensor")
+        if x.dtype not in dtypes or x.numel() != n or x.get_device() != index:
+            raise ValueError(f"{name}[{t}] must hold {n} {what} on the gradients' device")
+    return [x.data_ptr() for x in tensors]
 
-    def __init__(self, grads, state_bits=0, copy_type=BF16, fill=None):
+
+class _TensorPlan:
+    """A prepared plan of a model's tensors and its workspace.  ``columns``
+    (from the sizes and the device's index): the descriptors' other fields."""
+
+    def __init__(self, grads, state_bits=0, copy_type=BF16, columns=None):
         torch = _torch()
         if not grads:
             raise ValueError("no tensors")
+        _require_cuda(grads[0], "grads[0]")
         self.dev = grads[0].device
         gtype = _type_id(grads[0], "grads[0]")
-        arr = (Tensor * len(grads))()
-        total = 0
-        for t, g in enumerate(grads):
-            _require_cuda(g, f"grads[{t}]")
-            if g.dtype != grads[0].dtype or g.device != self.dev:
-                raise ValueError(f"grads[{t}] must have the type and device of grads[0]")
-            arr[t].grad, arr[t].n, arr[t].lr_scale = _ptr(g), g.numel(), 1.0
-            total += g.numel()
-            if fill:
-                fill(arr[t], t, g.numel())
+        sizes = [g.numel() for g in grads]
+        fields = {"grad": _pointers(grads, "grads", (grads[0].dtype,), sizes, grads[0].get_device(),
+                                    f"{grads[0].dtype} gradients"), "n": sizes}
+        if columns:
+            fields.update(columns(sizes, grads[0].get_device()))
+        # filled by columns: setting fields one by one takes a microsecond a tensor
+        arr = np.zeros(len(grads), dtype=_TENSOR_RECORD)
+        for name, column in fields.items():
+            arr[name] = column
         self.plan = Tensors()
-        self.ws = alloc_workspace(workspace_size(OP_TENSORS, len(grads), total, 0), self.dev)
-        _check(lib().sparcml_tensors_prepare(len(grads), arr, gtype, copy_type, state_bits, ctypes.byref(self.plan),
-                                             _ptr(self.ws), self.ws.numel(), _stream_ptr(self.dev)),
-               "sparcml_tensors_prepare")
+        self.ws = alloc_workspace(workspace_size(OP_TENSORS, len(grads), sum(sizes), 0), self.dev)
+        _check(lib().sparcml_tensors_prepare(len(grads), arr.ctypes.data_as(ctypes.POINTER(Tensor)), gtype, copy_type,
+                                             state_bits, ctypes.byref(self.plan), _ptr(self.ws), self.ws.numel(),
+                                             _stream_ptr(self.dev)), "sparcml_tensors_prepare")
         self.out = torch.empty(2, dtype=torch.float32, device=self.dev)
         self._plan, self._out = ctypes.byref(self.plan), self.out.data_ptr()
 
@@ -781,33 +800,29 @@ class AdamwCall(_TensorPlan):
         decay, lr_scale = per(decay), per(lr_scale)
         if len(decay) != count or len(lr_scale) != count:
             raise ValueError(f"decay and lr_scale must hold {count} numbers")
-        dev = grads[0].device if count else None
         given = [c for c in copies or [] if c is not None]
         ctype = _type_id(given[0], "copies") if given else BF16
         if ctype == F32:
             raise ValueError("copies must be bfloat16 or float16")
 
-        def moment(x, name, n):
-            _require_cuda(x, name)
-            ok = x.dtype == torch.float32 if bits == 32 else x.dtype in (torch.uint8, torch.float8_e4m3fn)
-            if not ok or x.numel() != n or x.device != dev:
-                raise ValueError(f"{name} must hold {n} {'fp32 moments' if bits == 32 else 'E4M3 codes'} on {dev}")
-
-        def fill(a, t, n):
-            _require(params[t], f"params[{t}]", torch.float32, n, dev)
-            moment(m[t], f"m[{t}]", n)
-            moment(v[t], f"v[{t}]", n)
-            a.param, a.m, a.v = _ptr(params[t]), _ptr(m[t]), _ptr(v[t])
+        def columns(sizes, index):
+            moment = ((torch.float32,), "fp32 moments") if bits == 32 else (
+                (torch.uint8, torch.float8_e4m3fn), "E4M3 codes")
+            f = {"param": _pointers(params, "params", (torch.float32,), sizes, index, "fp32 weights"),
+                 "m": _pointers(m, "m", moment[0], sizes, index, moment[1]),
+                 "v": _pointers(v, "v", moment[0], sizes, index, moment[1]),
+                 "decay": decay, "lr_scale": lr_scale}
             if bits == 8:
-                for name, x in (("m_scale", m_scale[t]), ("v_scale", v_scale[t])):
-                    _require(x, f"{name}[{t}]", torch.float32, -(-n // STATE_BLOCK), dev)
-                a.m_scale, a.v_scale = _ptr(m_scale[t]), _ptr(v_scale[t])
-            if copies is not None and copies[t] is not None:
-                _require(copies[t], f"copies[{t}]", given[0].dtype, n, dev)
-                a.copy = _ptr(copies[t])
-            a.decay, a.lr_scale = decay[t], lr_scale[t]
+                blocks = [-(-n // STATE_BLOCK) for n in sizes]
+                f["m_scale"] = _pointers(m_scale, "m_scale", (torch.float32,), blocks, index, "scales")
+                f["v_scale"] = _pointers(v_scale, "v_scale", (torch.float32,), blocks, index, "scales")
+            if given:
+                at = iter(_pointers(given, "copies", (given[0].dtype,),
+                                    [n for n, c in zip(sizes, copies) if c is not None], index, f"{given[0].dtype} entries"))
+                f["copy"] = [0 if c is None else next(at) for c in copies]
+            return f
 
-        super().__init__(grads, bits, ctype, fill)
+        super().__init__(grads, bits, ctype, columns)
         self.args = AdamwArgs()
         self._args = ctypes.byref(self.args)
         self._keep = (params, grads, m, v, m_scale, v_scale, copies)

@@ -161,6 +161,67 @@ def test_policy_loss_and_gradient(T, V, kind):
             assert r["dlogits"].data_ptr() == x.data_ptr()
 
 
+def test_long_rows_and_more_rows_than_a_launch():
+    """Rows beyond a workgroup's registers (their rest is read again), with
+    starts off the 128-byte lines, and more rows than one launch takes, on the
+    GPU's own fp64."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    for T, V, kind, pad, shift in ((140, 131073, "float32", 2, 1), (133, 90001, "bfloat16", 0, 0),
+                                   (129, 70000, "float16", 5, 3), (2, 200003, "float32", 0, 0), ((1 << 21) + 70, 3, "bfloat16", 0, 0)):
+        say(f"[long] {T} {V} {kind}")
+        x, label, gen = make(T, V, kind, T + V, pad, shift)
+        a = policy_inputs(x, label, gen, 1.0, True, T)
+        a["weight"][T // 2] = 0.0
+        label[T - 1] = -1
+        r = S.policy_loss(x, label, **a, kl=0.05)
+        only = S.policy_loss(x, label, **a, kl=0.05, dlogits=None)
+        lp, lse = S.token_logprob(x, label)
+        pref = S.preference_loss(x, label, [0, T // 3, T], ref=a["ref"])
+        y = x.double()
+        has = label >= 0
+        safe = label.clamp(min=0).long()[:, None]
+        soft = torch.log_softmax(y, 1)
+        want = torch.where(has, soft.gather(1, safe)[:, 0], 0.0)
+        err = z_bound(V) + 4 * U * 64 + 1e-7
+        assert float((lp - want).abs().max()) <= err
+        assert float((lse - torch.where(has, torch.logsumexp(y, 1), 0.0)).abs().max()) <= err
+        used = has & (a["weight"] != 0)
+        assert float((r["logp"] - torch.where(used, want, 0.0)).abs().max()) <= err
+        assert float((only["logp"] - r["logp"]).abs().max()) <= 2 * err
+        # coefficients from the kernel's own log probabilities, so that what is
+        # left to compare is the softmax
+        for d, mine in ((r["dlogits"], r["logp"]), (pref["dlogits"], pref["logp"])):
+            q = mine.double()
+            if d is r["dlogits"]:
+                rho = (q - a["old"].double()).exp()
+                u = rho * a["adv"].double()
+                held = rho.clamp(float(np.float32(0.8)), float(np.float32(1.2))) * a["adv"].double()
+                coef = -float(np.float32(0.05)) * torch.expm1(a["ref"].double() - q) - torch.where(u <= held, u, 0.0)
+                # (the two terms of a coefficient cancel where they will: each is off by itself)
+                size = u.abs() + 0.05 * (torch.exp(a["ref"].double() - q) + 1)
+                size = torch.where(used, a["weight"].double() * size, 0.0)
+                coef = torch.where(used, a["weight"].double() * coef, 0.0)
+                edge = (u - held).abs() < 1e-5 * u.abs()
+                edge &= u != held
+            else:
+                ratio = torch.where(has, q - a["ref"].double(), 0.0)
+                h = float(np.float32(0.1)) * (ratio[:T // 3].sum() - ratio[T // 3:].sum())
+                c0 = -float(np.float32(0.1)) * torch.sigmoid(-h)
+                coef = torch.where(has, torch.where(torch.arange(T, device=dev) < T // 3, c0, -c0), 0.0)
+                edge = torch.zeros_like(has)
+                size = coef.abs()
+            g = -coef[:, None] * soft.exp()
+            g.scatter_add_(1, safe, coef[:, None])
+            lim = coef.abs()[:, None] * soft.exp() * (z_bound(V) + 4 * U * 64 + 8 * U) + g.abs() * (STEP[kind] + 64 * U)
+            lim = lim + coef.abs()[:, None] * 64 * U * (g.abs() > 0.5 * coef.abs()[:, None]) + LEAST[kind]
+            lim = lim + size[:, None] * 16 * U
+            off = (d.double() - g).abs()
+            off[edge] = 0
+            assert bool((off <= lim).all()), float((off - lim).max())
+        del y, soft, g, lim, off
+
+
 def test_policy_clip_sides():
     """All four sides of the clip: the gradient is that of the unclipped
     product where it is the smaller one, else nothing (and no KL)."""
