@@ -40,6 +40,19 @@ int hip_fail(hipError_t e, const char* where)
 }
 
 bool valid_n(uint64_t N) { return N >= 1 && N < (1ull << 32); }
+// No exception crosses the ABI.
+template <class F>
+int guarded(F f)
+{
+    try {
+        return f();
+    } catch (const std::exception& ex) {
+        return fail(SPARCML_EHIP, "host exception: %s", ex.what());
+    } catch (...) {
+        return fail(SPARCML_EHIP, "host exception");
+    }
+}
+
 bool valid_rows(uint64_t rows, uint64_t vocab)
 {
     return rows >= 1 && rows < (1ull << 31) && vocab >= 1 && vocab < (1ull << 31);
@@ -610,7 +623,7 @@ static uint64_t plan_check(const sparcml_tensors& p)
 int sparcml_tensors_prepare(int count, const sparcml_tensor* tensors, int grad_type, int copy_type, int state_bits,
                             sparcml_tensors* plan, void* ws, size_t ws_bytes, void* stream)
 {
-    try {
+    return guarded([&]() -> int {
         if (count < 1 || count > 65535) return fail(SPARCML_EINVAL, "count must be in [1, 65535]");
         if (!tensors || !plan) return fail(SPARCML_EINVAL, "NULL argument");
         if (grad_type < SPARCML_F32 || grad_type > SPARCML_F16) return fail(SPARCML_EINVAL, "unknown grad_type %d", grad_type);
@@ -657,52 +670,54 @@ int sparcml_tensors_prepare(int count, const sparcml_tensor* tensors, int grad_t
         p.check = plan_check(p);
         *plan = p;
         return SPARCML_OK;
-    } catch (const std::exception& ex) {
-        return fail(SPARCML_EHIP, "host exception: %s", ex.what());
-    }
+    });
 }
 
 int sparcml_grad_norm(const sparcml_tensors* plan, double grad_scale, double max_norm, float* out, void* stream)
 {
-    if (!plan || plan->check != plan_check(*plan)) return fail(SPARCML_EINVAL, "no plan of sparcml_tensors_prepare");
-    if (!out) return fail(SPARCML_EINVAL, "out is NULL");
-    if (!(grad_scale > 0.0) || !isfinite(grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be positive and finite");
-    if (!(max_norm > 0.0)) return fail(SPARCML_EINVAL, "max_norm must be positive");
-    hipError_t e = grad_norm_run(plan->count, plan->chunks, plan->grad_type, grad_scale, max_norm, out, plan->ws,
-                                 (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(e, "grad_norm");
-    return SPARCML_OK;
+    return guarded([&]() -> int {
+        if (!plan || plan->check != plan_check(*plan)) return fail(SPARCML_EINVAL, "no plan of sparcml_tensors_prepare");
+        if (!out) return fail(SPARCML_EINVAL, "out is NULL");
+        if (!(grad_scale > 0.0) || !isfinite(grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be positive and finite");
+        if (!(max_norm > 0.0)) return fail(SPARCML_EINVAL, "max_norm must be positive");
+        hipError_t e = grad_norm_run(plan->count, plan->chunks, plan->grad_type, grad_scale, max_norm, out, plan->ws,
+                                     (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "grad_norm");
+        return SPARCML_OK;
+    });
 }
 
 int sparcml_adamw(const sparcml_tensors* plan, const sparcml_adamw_args* args, const float* clip, void* stream)
 {
-    if (!plan || plan->check != plan_check(*plan)) return fail(SPARCML_EINVAL, "no plan of sparcml_tensors_prepare");
-    if (!args) return fail(SPARCML_EINVAL, "args is NULL");
-    if (!plan->state_bits) return fail(SPARCML_EINVAL, "the plan holds gradients only");
-    const sparcml_adamw_args& a = *args;
-    if (!(a.lr >= 0.0) || !isfinite(a.lr)) return fail(SPARCML_EINVAL, "lr must be finite and not negative");
-    if (!(a.beta1 >= 0.0 && a.beta1 < 1.0 && a.beta2 >= 0.0 && a.beta2 < 1.0))
-        return fail(SPARCML_EINVAL, "betas must be in [0, 1)");
-    if (!((float)a.eps > 0.0f) || !isfinite((float)a.eps)) return fail(SPARCML_EINVAL, "eps must be positive and finite");
-    if (!isfinite((float)a.grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be finite");
-    if (a.step < 1) return fail(SPARCML_EINVAL, "step must be at least 1");
-    AdamwStep s;
-    s.lr = a.lr;
-    s.rate = a.lr / (1.0 - pow(a.beta1, (double)a.step));
-    s.b1 = (float)a.beta1;
-    s.omb1 = (float)(1.0 - a.beta1);
-    s.b2 = (float)a.beta2;
-    s.omb2 = (float)(1.0 - a.beta2);
-    s.ibc2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)a.step)));
-    s.eps = (float)a.eps;
-    s.gs = (float)a.grad_scale;
-    s.step = a.step;
-    s.key0 = (uint32_t)a.seed;
-    s.key1 = (uint32_t)(a.seed >> 32);
-    hipError_t e = adamw_run(plan->count, plan->chunks, plan->grad_type, plan->copy_type, plan->state_bits, s, clip,
-                             plan->ws, (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(e, "adamw");
-    return SPARCML_OK;
+    return guarded([&]() -> int {
+        if (!plan || plan->check != plan_check(*plan)) return fail(SPARCML_EINVAL, "no plan of sparcml_tensors_prepare");
+        if (!args) return fail(SPARCML_EINVAL, "args is NULL");
+        if (!plan->state_bits) return fail(SPARCML_EINVAL, "the plan holds gradients only");
+        const sparcml_adamw_args& a = *args;
+        if (!(a.lr >= 0.0) || !isfinite(a.lr)) return fail(SPARCML_EINVAL, "lr must be finite and not negative");
+        if (!(a.beta1 >= 0.0 && a.beta1 < 1.0 && a.beta2 >= 0.0 && a.beta2 < 1.0))
+            return fail(SPARCML_EINVAL, "betas must be in [0, 1)");
+        if (!((float)a.eps > 0.0f) || !isfinite((float)a.eps)) return fail(SPARCML_EINVAL, "eps must be positive and finite");
+        if (!isfinite((float)a.grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be finite");
+        if (a.step < 1) return fail(SPARCML_EINVAL, "step must be at least 1");
+        AdamwStep s;
+        s.lr = a.lr;
+        s.rate = a.lr / (1.0 - pow(a.beta1, (double)a.step));
+        s.b1 = (float)a.beta1;
+        s.omb1 = (float)(1.0 - a.beta1);
+        s.b2 = (float)a.beta2;
+        s.omb2 = (float)(1.0 - a.beta2);
+        s.ibc2 = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)a.step)));
+        s.eps = (float)a.eps;
+        s.gs = (float)a.grad_scale;
+        s.step = a.step;
+        s.key0 = (uint32_t)a.seed;
+        s.key1 = (uint32_t)(a.seed >> 32);
+        hipError_t e = adamw_run(plan->count, plan->chunks, plan->grad_type, plan->copy_type, plan->state_bits, s, clip,
+                                 plan->ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "adamw");
+        return SPARCML_OK;
+    });
 }
 
 // Shared argument checks of the losses.
@@ -733,44 +748,48 @@ static int gradient_validate(const sparcml_logits* in, const void* d, uint64_t l
 
 int sparcml_token_logprob(const sparcml_logits* in, float* logp, float* lse, void* ws, size_t ws_bytes, void* stream)
 {
-    Logits l;
-    int rc = logits_validate(in, &l);
-    if (rc != SPARCML_OK) return rc;
-    if (!logp) return fail(SPARCML_EINVAL, "logp is NULL");
-    const size_t need = logprob_workspace(l.rows, l.vocab);
-    if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
-    hipError_t e = logprob_run(l, logp, lse, ws, (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(e, "token_logprob");
-    return SPARCML_OK;
+    return guarded([&]() -> int {
+        Logits l;
+        int rc = logits_validate(in, &l);
+        if (rc != SPARCML_OK) return rc;
+        if (!logp) return fail(SPARCML_EINVAL, "logp is NULL");
+        const size_t need = logprob_workspace(l.rows, l.vocab);
+        if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+        hipError_t e = logprob_run(l, logp, lse, ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "token_logprob");
+        return SPARCML_OK;
+    });
 }
 
 int sparcml_policy_loss(const sparcml_logits* in, const sparcml_policy_args* args, float* logp, float* stats,
                         void* dlogits, uint64_t ld_d, void* ws, size_t ws_bytes, void* stream)
 {
-    Logits l;
-    int rc = logits_validate(in, &l);
-    if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
-    if (rc != SPARCML_OK) return rc;
-    if (!args || !args->old_logp || !args->adv || !args->weight || !logp || !stats)
-        return fail(SPARCML_EINVAL, "NULL argument");
-    if (!(args->clip_lo >= 0.0f && args->clip_lo <= 1.0f)) return fail(SPARCML_EINVAL, "clip_lo must be in [0, 1]");
-    if (!(args->clip_hi >= 0.0f)) return fail(SPARCML_EINVAL, "clip_hi must not be negative");
-    if (!isfinite(args->grad_scale) || (args->ref_logp && !isfinite(args->kl)))
-        return fail(SPARCML_EINVAL, "kl and grad_scale must be finite");
-    const size_t need = policy_workspace(l.rows, l.vocab);
-    if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
-    const PolicyArgs a{args->old_logp, args->ref_logp, args->adv, args->weight, (float)(1.0 - (double)args->clip_lo),
-                       (float)(1.0 + (double)args->clip_hi), args->kl, args->grad_scale};
-    hipError_t e = policy_run(l, a, logp, stats, dlogits, ld_d, ws, (hipStream_t)stream);
-    if (e != hipSuccess) return hip_fail(e, "policy_loss");
-    return SPARCML_OK;
+    return guarded([&]() -> int {
+        Logits l;
+        int rc = logits_validate(in, &l);
+        if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
+        if (rc != SPARCML_OK) return rc;
+        if (!args || !args->old_logp || !args->adv || !args->weight || !logp || !stats)
+            return fail(SPARCML_EINVAL, "NULL argument");
+        if (!(args->clip_lo >= 0.0f && args->clip_lo <= 1.0f)) return fail(SPARCML_EINVAL, "clip_lo must be in [0, 1]");
+        if (!(args->clip_hi >= 0.0f)) return fail(SPARCML_EINVAL, "clip_hi must not be negative");
+        if (!isfinite(args->grad_scale) || (args->ref_logp && !isfinite(args->kl)))
+            return fail(SPARCML_EINVAL, "kl and grad_scale must be finite");
+        const size_t need = policy_workspace(l.rows, l.vocab);
+        if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+        const PolicyArgs a{args->old_logp, args->ref_logp, args->adv, args->weight, (float)(1.0 - (double)args->clip_lo),
+                           (float)(1.0 + (double)args->clip_hi), args->kl, args->grad_scale};
+        hipError_t e = policy_run(l, a, logp, stats, dlogits, ld_d, ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "policy_loss");
+        return SPARCML_OK;
+    });
 }
 
 int sparcml_preference_loss(const sparcml_logits* in, int pairs, const uint64_t* bounds, const float* ref_logp,
                             float beta, float smoothing, float grad_scale, float* logp, float* stats, void* dlogits,
                             uint64_t ld_d, void* ws, size_t ws_bytes, void* stream)
 {
-    try {
+    return guarded([&]() -> int {
         Logits l;
         int rc = logits_validate(in, &l);
         if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
@@ -792,9 +811,7 @@ int sparcml_preference_loss(const sparcml_logits* in, int pairs, const uint64_t*
                                       b.data(), logp, stats, dlogits, ld_d, ws, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, "preference_loss");
         return SPARCML_OK;
-    } catch (const std::exception& ex) {
-        return fail(SPARCML_EHIP, "host exception: %s", ex.what());
-    }
+    });
 }
 
 }  // extern "C"

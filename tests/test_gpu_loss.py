@@ -222,6 +222,31 @@ def test_long_rows_and_more_rows_than_a_launch():
         del y, soft, g, lim, off
 
 
+def test_logits_beyond_32_bits():
+    """Rows past 2^32 elements: those at the end against 64 bits, in place."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    T, V, last = 34000, 131072, 3
+    x = torch.empty(T, V, device=dev, dtype=torch.bfloat16)
+    block = torch.randn(500, V, device=dev, dtype=torch.bfloat16)
+    for i in range(0, T, 500):
+        x[i:i + 500] = block
+    gen = torch.Generator(device=dev).manual_seed(3)
+    x[-last:] = torch.randn(last, V, device=dev, generator=gen) * 2
+    label = torch.full((T,), -1, dtype=torch.int32, device=dev)
+    label[-last:] = torch.randint(0, V, (last,), device=dev, generator=gen).int()
+    h, l = x[-last:].double().cpu().numpy(), label[-last:].cpu().numpy()
+    lp, _ = S.token_logprob(x, label)
+    want = R.rows(h, l, 1.0)[0]
+    err = lp_bound(h, l, 1.0, V)
+    assert np.all(np.abs(to_np(lp)[-last:] - want) <= err) and not bool(lp[:-last].any())
+    one = torch.ones(T, device=dev)
+    r = S.policy_loss(x, label, lp, one, one, dlogits="inplace")
+    _, _, d, coef = R.policy(h, l, to_np(lp)[-last:], np.ones(last), np.ones(last))
+    check_gradient(r["dlogits"][-last:].double().cpu().numpy(), d, np.abs(coef), h, 1.0, V, "bfloat16", err + 16 * U)
+    assert not bool(r["dlogits"][:500].any()) and not bool(r["dlogits"][T // 2:-last].any())
+
+
 def test_policy_clip_sides():
     """All four sides of the clip: the gradient is that of the unclipped
     product where it is the smaller one, else nothing (and no KL)."""

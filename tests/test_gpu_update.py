@@ -257,6 +257,38 @@ def test_norm_and_step_replay_in_a_graph():
             assert float(ca.out[0]) == float(cb.out[0])
 
 
+def test_a_tensor_beyond_32_bits():
+    """Elements past 2^32 of one tensor: the last blocks move as specified,
+    with the draws of their own place."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    n, tail = 2**32 + 1234, 4000
+    p = torch.zeros(n, device=dev)
+    g = torch.zeros(n, device=dev, dtype=torch.bfloat16)
+    gen = torch.Generator(device=dev).manual_seed(1)
+    p[-tail:] = torch.randn(tail, device=dev, generator=gen)
+    g[-tail:] = torch.randn(tail, device=dev, generator=gen).to(g.dtype)
+    m, v, ms, vs = S.adamw_state([p], 8)
+    before = [to_np(p[-tail:]).copy(), to_np(g[-tail:].float()).copy()]
+    call = S.AdamwCall([p], [g], m, v, m_scale=ms, v_scale=vs)
+    np.testing.assert_allclose(float(call.grad_norm()[0]), np.linalg.norm(before[1].astype(np.float64)), rtol=1e-6)
+    call.run(lr=1e-2, step=2, seed=77)
+    torch.cuda.synchronize()
+    zero = np.zeros(tail, F)
+    want, wm, wv, root = R.adamw(*before, zero, zero, lr=1e-2, step=2, bits=32)
+    np.testing.assert_array_equal(to_np(p[-tail:]), want)
+    first = -(-(n - tail) // 256) * 256  # the first whole block of the tail
+    k = first - (n - tail)
+    w = R.philox_words(n - first, 0, 2, 77, first)
+    codes, scale = R.encode(wm[k:], w & np.uint64(0xFFFF), False)
+    np.testing.assert_array_equal(to_np(m[0].view(torch.uint8)[first:]), codes)
+    np.testing.assert_array_equal(to_np(ms[0][first // 256:]), scale)
+    codes, scale = R.encode(root[k:], w >> np.uint64(16), True)
+    np.testing.assert_array_equal(to_np(v[0].view(torch.uint8)[first:]), codes)
+    np.testing.assert_array_equal(to_np(vs[0][first // 256:]), scale)
+    assert not bool(p[:1 << 20].any())
+
+
 def test_refusals_of_tensors():
     from paper_1802_08021_amd import sparcml as S
     torch, dev = torch_dev()

@@ -7,11 +7,11 @@ F = np.float32
 BLOCK = 256
 
 
-def philox_words(n, tensor, step, seed):
+def philox_words(n, tensor, step, seed, first=0):
     """Word j & 3 of the Philox4x32-10 block at counter (j >> 2, tensor,
-    step, 0), j < n (plain ten rounds on Python-sized integers)."""
+    step, 0), first <= j < first + n (plain ten rounds; first a multiple of 4)."""
     cnt = -(-n // 4)
-    c = [np.arange(cnt, dtype=np.uint64), np.full(cnt, tensor, np.uint64), np.full(cnt, step, np.uint64),
+    c = [np.arange(first // 4, first // 4 + cnt, dtype=np.uint64), np.full(cnt, tensor, np.uint64), np.full(cnt, step, np.uint64),
          np.zeros(cnt, np.uint64)]
     k = [np.uint64(seed & 0xFFFFFFFF), np.uint64(seed >> 32)]
     mask, s32 = np.uint64(0xFFFFFFFF), np.uint64(32)
