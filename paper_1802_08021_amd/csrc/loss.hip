@@ -23,7 +23,6 @@ namespace sparcml {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr float kLn2 = 0.693147180559945309f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -104,13 +103,26 @@ __device__ __forceinline__ Part join_slices(const Part* part, uint32_t S, uint32
     return Part{top, sum};
 }
 
-__device__ __forceinline__ float part_logp(Part p, float x, float c)
+// ln of a part's sum in fp64: its power of two and log2 of what is left of it,
+// in [sqrt(1/2), sqrt(2)), apart (fp32's log of a sum of thousands would be off
+// by 5e-7; exactly 0 for 1).
+__device__ __forceinline__ double part_ln(float sum)
 {
-    return p.sum == 0.0f ? -INFINITY : ((x - p.top) * c - log2f(p.sum)) * kLn2;
+    int e;
+    float m = frexpf(sum, &e);
+    if (m < 0.707106781f) {
+        m *= 2.0f;
+        --e;
+    }
+    return ((double)e + (double)__builtin_amdgcn_logf(m)) * 0.693147180559945309;
+}
+__device__ __forceinline__ double part_logp(Part p, float x, float scale)
+{
+    return p.sum == 0.0f ? (double)-INFINITY : ((double)x - (double)p.top) * (double)scale - part_ln(p.sum);
 }
 __device__ __forceinline__ float part_lse(Part p, float scale)
 {
-    return p.sum == 0.0f ? -INFINITY : p.top * scale + log2f(p.sum) * kLn2;
+    return p.sum == 0.0f ? -INFINITY : (float)((double)p.top * (double)scale + part_ln(p.sum));
 }
 
 // One gradient entry before the label's own term.
@@ -155,10 +167,10 @@ struct PolicyRow {
 struct PolicyTerms {
     float gain, k, clipped, coef;
 };
-__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const PolicyRow& q, float lp)
+__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const PolicyRow& q, double lp)
 {
     PolicyTerms r;
-    const float rho = expf(lp - q.old);
+    const float rho = exp2_fast((float)((lp - (double)q.old) * 1.44269504088896341));
     const float u = rho * q.adv, held = fminf(fmaxf(rho, a.lo), a.hi) * q.adv;
     const bool clipped = u > held;
     r.gain = q.w * (clipped ? held : u);  // (a NaN of u comes through)
@@ -166,7 +178,7 @@ __device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const P
     r.k = 0.0f;
     r.coef = clipped ? 0.0f : -u;
     if (a.ref_logp) {
-        const float far = q.ref - lp, em = expm1f(far);
+        const float far = (float)((double)q.ref - lp), em = expm1f(far);
         r.k = q.w * (em - far);
         r.coef = r.coef - a.kl * em;
     }
@@ -276,7 +288,7 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
       PolicyTerms* terms, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
-    constexpr int N = Piece<TYPE>::N, U = 2;
+    constexpr int N = Piece<TYPE>::N, U = 1;
     __shared__ float s_top[THREADS / 64], s_sum[THREADS / 64], s_x, s_coef;
     if (!GRAD && blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;  // for k_policy_grad
     const uint64_t t = blockIdx.x;
@@ -319,8 +331,8 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
     if (top == -INFINITY) top = 0.0f;
     const Part p = {top, join_waves<true>(own.sum * exp2_fast((own.top - top) * c), s_sum)};
     if (tid == 0) {
-        const float lp = part_logp(p, s_x, c);
-        logp[t] = lp;
+        const double lp = part_logp(p, s_x, in.scale);
+        logp[t] = (float)lp;
         if (lse) lse[t] = part_lse(p, in.scale);
         if (part) {
             part[t] = p;
@@ -419,8 +431,8 @@ __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, 
             part[b] = p;
             if (s == 0) at_label[t] = at;
             if (S == 1) {
-                const float lp = part_logp(p, at, c);
-                logp[t] = lp;
+                const double lp = part_logp(p, at, in.scale);
+                logp[t] = (float)lp;
                 if (lse) lse[t] = part_lse(p, in.scale);
                 if (terms) terms[t] = policy_terms(a, PolicyRow(a, t), lp);
             }
@@ -443,7 +455,7 @@ __device__ __forceinline__ void each_joined(const Logits& in, const float* weigh
         const float at = at_label[in_range];
         const bool use = t < end && in_use(in, weight, in_range);
         const Part p = join_slices(part + in_range * S, S, g, c);
-        if (t < end && (threadIdx.x & (g - 1)) == 0) f(t, use, use ? part_logp(p, at, c) : 0.0f, p);
+        if (t < end && (threadIdx.x & (g - 1)) == 0) f(t, use, use ? part_logp(p, at, in.scale) : 0.0, p);
     }
 }
 
@@ -454,8 +466,8 @@ __global__ void __launch_bounds__(256) k_join(Logits in, const float* weight, ui
     const uint32_t rows = 256 / g;
     for (uint64_t t0 = (uint64_t)blockIdx.x * rows; t0 < in.rows; t0 += (uint64_t)gridDim.x * rows)
         each_joined(in, weight, t0, min(t0 + rows, in.rows), S, g, c, part, at_label,
-                    [&](uint64_t t, bool use, float lp, Part p) {
-                        logp[t] = lp;
+                    [&](uint64_t t, bool use, double lp, Part p) {
+                        logp[t] = (float)lp;
                         if (lse) lse[t] = use ? part_lse(p, in.scale) : 0.0f;
                     });
 }
@@ -528,16 +540,16 @@ __global__ void __launch_bounds__(256) k_policy_grad(Logits in, PolicyArgs a, ui
         GradSlice<TYPE> slice(static_cast<const E*>(in.x) + t * in.ld, dlogits ? (uint32_t)in.vocab : 0, s, use);
         Part p = {0.0f, 0.0f};
         PolicyTerms m = {0.0f, 0.0f, 0.0f, 0.0f};
-        float lp = 0.0f;
+        double lp = 0.0;
         if (use) {
             const PolicyRow q(a, t);
             const float at = at_label[t];
             p = join_slices(part + t * S, S, g, c);
-            lp = part_logp(p, at, c);
+            lp = part_logp(p, at, in.scale);
             m = policy_terms(a, q, lp);
         }
         if (s == 0 && threadIdx.x == 0) {
-            logp[t] = lp;
+            logp[t] = (float)lp;
             // (device-scope accesses, each done before the next)
             float* w = &terms[t].gain;
             for (int i = 0; i < 3; ++i)
@@ -578,9 +590,9 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
     const uint32_t lo = many ? many[2 * b] : few.words[2 * b], mid = many ? many[2 * b + 1] : few.words[2 * b + 1];
     const uint32_t end = many ? many[2 * b + 2] : few.words[2 * b + 2];
     double x[2] = {0.0, 0.0};
-    auto add = [&](uint64_t t, bool use, float lp, Part) {
-        if (S > 1) logp[t] = lp;
-        if (use) x[t < mid ? 0 : 1] += (double)lp - (a.ref_logp ? (double)a.ref_logp[t] : 0.0);
+    auto add = [&](uint64_t t, bool use, double lp, Part) {
+        if (S > 1) logp[t] = (float)lp;
+        if (use) x[t < mid ? 0 : 1] += lp - (a.ref_logp ? (double)a.ref_logp[t] : 0.0);
     };
     if (S > 1)
         each_joined(in, nullptr, lo, end, S, g, c, part, at_label, add);
@@ -600,31 +612,38 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
                             good, bad}};
 }
 
-// Workgroup 0: the sums over pairs; the others a slice of the gradient each.
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_preference_grad(Logits in, PreferenceArgs a, uint32_t pairs, uint32_t S,
-                                                         uint32_t g, uint32_t G, float c, const Part* part,
-                                                         const float* coef, const PairSums* sums, float* stats,
-                                                         void* dlogits, uint64_t ldd)
+// The gradient by slices from coefficients that are there: of a policy loss
+// whose rows are one slice each (its terms), or of pairs (coef).  Workgroup 0:
+// the sums over tokens or pairs.
+template <int TYPE, bool POLICY>
+__global__ void __launch_bounds__(256) k_grad(Logits in, PolicyArgs a, const PolicyTerms* terms, uint32_t pairs,
+                                              const float* coef, const PairSums* sums, float factor, uint32_t S,
+                                              uint32_t g, uint32_t G, float c, const Part* part, float* stats,
+                                              void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     __shared__ double s_w[4][4];
     if (blockIdx.x == 0) {
         double x[4] = {0.0, 0.0, 0.0, 0.0};
-        for (uint32_t i = threadIdx.x; i < pairs; i += 256)
-            for (int q = 0; q < 4; ++q) x[q] += sums[i].x[q];
-        block_sum(x, s_w, 4);
-        if (threadIdx.x == 0)
-            for (int q = 0; q < 4; ++q) stats[q] = (float)(x[q] / pairs);
+        if (POLICY) {
+            for (uint64_t t = threadIdx.x; t < in.rows; t += 256) add_terms(terms[t], x);
+            put_policy_stats(a, x, s_w, stats);
+        } else {
+            for (uint32_t i = threadIdx.x; i < pairs; i += 256)
+                for (int q = 0; q < 4; ++q) x[q] += sums[i].x[q];
+            block_sum(x, s_w, 4);
+            if (threadIdx.x == 0)
+                for (int q = 0; q < 4; ++q) stats[q] = (float)(x[q] / pairs);
+        }
         return;
     }
     for (uint64_t b = blockIdx.x - 1; b < in.rows * G; b += gridDim.x - 1) {
         const uint64_t t = b / G;
-        const bool use = has_token(in, t);
+        const bool use = in_use(in, POLICY ? a.weight : nullptr, t);
         GradSlice<TYPE> slice(static_cast<const E*>(in.x) + t * in.ld, (uint32_t)in.vocab, (uint32_t)(b % G), use);
-        const float q = a.grad_scale * in.scale * coef[t];
+        const float q = factor * (POLICY ? terms[t].coef : coef[t]);
         Part p = {0.0f, 0.0f};
-        if (use) p = join_slices(part + t * S, S, g, c);
+        if (use) p = POLICY ? part[t] : join_slices(part + t * S, S, g, c);
         slice.write(static_cast<E*>(dlogits) + t * ldd, (uint32_t)in.label[t], q, p, c);
     }
 }
@@ -811,18 +830,24 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
         hipError_t e = rows_run<false>(cut, in, &a, sp, logp, nullptr, s);
         if (e != hipSuccess) return e;
     }
-    if (fused || (!dlogits && cut.S == 1))
+    if (fused || (!dlogits && cut.S == 1)) {
         hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, in.rows, a, sp.terms, stats);
-    else {
-        const uint32_t G = dlogits ? cut.G : 1;
-        const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * G, kMaxGrid);
-        timer_begin(kTLossGrad, s);
-        by_type(in.type, [&](auto ty) {
-            hipLaunchKernelGGL((k_policy_grad<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a, cut.S, cut.g,
-                               G, c, sp.part, sp.at_label, logp, sp.terms, sp.ticket, stats, dlogits, ldd);
-        });
-        timer_end(kTLossGrad, s);
+        return hipGetLastError();
     }
+    const uint32_t G = dlogits ? cut.G : 1;
+    const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * G, kMaxGrid);
+    timer_begin(kTLossGrad, s);
+    by_type(in.type, [&](auto ty) {
+        constexpr int TY = decltype(ty)::value;
+        if (cut.S == 1)
+            hipLaunchKernelGGL((k_grad<TY, true>), dim3(grid + 1), dim3(256), 0, s, in, a, sp.terms, 0u,
+                               (const float*)nullptr, (const PairSums*)nullptr, a.grad_scale * in.scale, 1u, 1u, G, c,
+                               sp.part, stats, dlogits, ldd);
+        else
+            hipLaunchKernelGGL((k_policy_grad<TY>), dim3(grid), dim3(256), 0, s, in, a, cut.S, cut.g, G, c, sp.part,
+                               sp.at_label, logp, sp.terms, sp.ticket, stats, dlogits, ldd);
+    });
+    timer_end(kTLossGrad, s);
     return hipGetLastError();
 }
 
@@ -853,8 +878,9 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
     const uint32_t grid = dlogits ? (uint32_t)std::min<uint64_t>(in.rows * cut.G, kMaxGrid) + 1 : 1;
     timer_begin(kTLossGrad, s);
     by_type(in.type, [&](auto ty) {
-        hipLaunchKernelGGL((k_preference_grad<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a, pairs, cut.S,
-                           cut.g, cut.G, c, sp.part, sp.coef, sp.sums, stats, dlogits, ldd);
+        hipLaunchKernelGGL((k_grad<decltype(ty)::value, false>), dim3(grid), dim3(256), 0, s, in, PolicyArgs{},
+                           (const PolicyTerms*)nullptr, pairs, sp.coef, sp.sums, a.grad_scale * in.scale, cut.S, cut.g,
+                           cut.G, c, sp.part, stats, dlogits, ldd);
     });
     timer_end(kTLossGrad, s);
     return hipGetLastError();

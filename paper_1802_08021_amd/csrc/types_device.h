@@ -32,6 +32,15 @@ struct Elem<kF16> {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// A pointer known to be to global memory (one read from a table would be taken
+// for a generic one, whose accesses wait for LDS too).
+#define SPARCML_GLOBAL __attribute__((address_space(1)))
+template <class T>
+__device__ __forceinline__ SPARCML_GLOBAL T* as_global(T* p)
+{
+    return (SPARCML_GLOBAL T*)p;
+}
+
 // Element i of 16 bytes of a type, as fp32.
 template <int TYPE>
 __device__ __forceinline__ float unpack(u32x4 w, int i)
@@ -48,14 +57,14 @@ template <class V, bool KEEP = false, class E>
 __device__ __forceinline__ V load_vec(const E* p)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
-    const U* q = reinterpret_cast<const U*>(p);
+    const SPARCML_GLOBAL U* q = as_global(reinterpret_cast<const U*>(p));
     return KEEP ? *q : __builtin_nontemporal_load(q);
 }
 template <class V, class E>
 __device__ __forceinline__ void store_vec(E* p, V v)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
-    __builtin_nontemporal_store(v, reinterpret_cast<U*>(p));
+    __builtin_nontemporal_store(v, as_global(reinterpret_cast<U*>(p)));
 }
 
 // Sum and maximum of the 64 lanes' values, in every lane: shifts within rows

@@ -25,18 +25,26 @@ __global__ void k_tensor_map(const TensorDesc* desc, const uint32_t* first, uint
     for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) map[first[t] + i] = make_uint2(t, i);
 }
 
-// Elements e .. e + 3 of an array of n as fp32, zeros outside it (e may lie
-// before the array: below zero, as a large number).
+// Element e of an array of n as fp32, zero outside it (e may lie before the
+// array: below zero, as a large number).  Without a branch, so that the loads
+// of a tensor's ends are under way together; n > 0.
+template <class E>
+__device__ __forceinline__ float get1(const E* p, uint64_t e, uint64_t n)
+{
+    const float x = (float)as_global(p)[e < n ? e : 0];
+    return e < n ? x : 0.0f;
+}
+
+// Elements e .. e + 3 of an array of n, likewise.
 template <int TYPE>
 __device__ __forceinline__ f32x4 get4(const void* p, uint64_t e, uint64_t n)
 {
     typedef typename Elem<TYPE>::type E;
-    const E* q = static_cast<const E*>(p) + e;
-    if (e < n && e + 4 <= n) return __builtin_convertvector(load_vec<typename Elem<TYPE>::vec4>(q), f32x4);
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    const E* q = static_cast<const E*>(p);
+    if (e < n && e + 4 <= n) return __builtin_convertvector(load_vec<typename Elem<TYPE>::vec4>(q + e), f32x4);
+    f32x4 x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (e + i < n) x[i] = (float)q[i];
+    for (int i = 0; i < 4; ++i) x[i] = get1(q, e + i, n);
     return x;
 }
 
@@ -51,19 +59,21 @@ __device__ __forceinline__ void put4(void* p, uint64_t e, uint64_t n, f32x4 x)
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (e + i < n) q[i] = (E)x[i];
+            if (e + i < n) as_global(q)[i] = (E)x[i];
     }
 }
 
 // Four codes as bytes of a word, zeros past the end.
 __device__ __forceinline__ uint32_t get_codes(const void* p, uint64_t e, uint64_t n)
 {
-    const uint8_t* q = static_cast<const uint8_t*>(p) + e;
-    if (e + 4 <= n) return load_vec<uint32_t>(q);
+    const uint8_t* q = static_cast<const uint8_t*>(p);
+    if (e + 4 <= n) return load_vec<uint32_t>(q + e);
     uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (e + i < n) w |= (uint32_t)q[i] << (8 * i);
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t x = as_global(q)[e + i < n ? e + i : 0];
+        w |= (e + i < n ? x : 0u) << (8 * i);
+    }
     return w;
 }
 
@@ -75,7 +85,7 @@ __device__ __forceinline__ void put_codes(void* p, uint64_t e, uint64_t n, uint3
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (e + i < n) q[i] = (uint8_t)(w >> (8 * i));
+            if (e + i < n) as_global(q)[i] = (uint8_t)(w >> (8 * i));
     }
 }
 
@@ -144,8 +154,8 @@ __global__ void __launch_bounds__(256) k_adamw(const TensorDesc* __restrict__ de
                 m = get4<kF32>(d.m, e, d.n);
                 v = get4<kF32>(d.v, e, d.n);
             } else {
-                m = decode4(get_codes(d.m, e, d.n), d.m_scale[b / kStateBlock]);
-                v = decode4(get_codes(d.v, e, d.n), d.v_scale[b / kStateBlock]);
+                m = decode4(get_codes(d.m, e, d.n), as_global(d.m_scale)[b / kStateBlock]);
+                v = decode4(get_codes(d.v, e, d.n), as_global(d.v_scale)[b / kStateBlock]);
                 v = v * v;
             }
             m = a.b1 * m + a.omb1 * g;
@@ -173,8 +183,8 @@ __global__ void __launch_bounds__(256) k_adamw(const TensorDesc* __restrict__ de
                 put_codes(d.v, e, d.n,
                           encode4(yr, z.x & 0xFFFF0000u, z.y & 0xFFFF0000u, z.z & 0xFFFF0000u, z.w & 0xFFFF0000u));
                 if (lane == 0) {
-                    d.m_scale[b / kStateBlock] = __uint_as_float(em << 23);
-                    d.v_scale[b / kStateBlock] = __uint_as_float(er << 23);
+                    as_global(d.m_scale)[b / kStateBlock] = __uint_as_float(em << 23);
+                    as_global(d.v_scale)[b / kStateBlock] = __uint_as_float(er << 23);
                 }
             }
         }
@@ -209,11 +219,10 @@ __global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ des
         const uint2 at = map[c];
         const E* grad = static_cast<const E*>(desc[at.x].grad);
         const uint64_t n = desc[at.x].n, e0 = (uint64_t)at.y * kTensorChunk - desc[at.x].shift;
-        const uint64_t e = e0 + (uint64_t)threadIdx.x * N;
         if (e0 < n && e0 + kTensorChunk <= n) {  // a whole piece
             u32x4 w[R];
 #pragma unroll
-            for (int u = 0; u < R; ++u) w[u] = load_vec<u32x4>(grad + e + u * (256 * N));
+            for (int u = 0; u < R; ++u) w[u] = load_vec<u32x4>(grad + e0 + (threadIdx.x + u * 256) * N);
 #pragma unroll
             for (int u = 0; u < R; ++u) {
                 float x[N];
@@ -222,11 +231,12 @@ __global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ des
                 add(x, N);
             }
         } else {
-            for (int u = 0; u < R * N / 4; ++u) {
-                const f32x4 x = get4<GT>(grad, e0 + (uint64_t)threadIdx.x * 4 + (uint32_t)u * 1024, n);
-                const float y[4] = {x[0], x[1], x[2], x[3]};
-                add(y, 4);
+            float x[kTensorChunk / 256];
+#pragma unroll
+            for (int i = 0; i < (int)kTensorChunk / 256; ++i) {
+                x[i] = get1(grad, e0 + threadIdx.x + i * 256, n);
             }
+            add(x, kTensorChunk / 256);
         }
     }
     const double sum = block_sum(acc[0] + acc[1], s_w);

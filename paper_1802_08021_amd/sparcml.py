@@ -716,12 +716,14 @@ def adamw_state(params, state_bits: int = 32):
 
 def _pointers(tensors, name: str, dtypes, numels, index: int, what: str):
     """Addresses of one list of a model's tensors, each checked."""
+    # whole lists at once: a large model has a thousand tensors
     torch = _torch()
-    for t, (x, n) in enumerate(zip(tensors, numels)):
-        if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous():
-            raise ValueError(f"{name}[{t}] must be a contiguous CUDA (HIP) tensor")
-        if x.dtype not in dtypes or x.numel() != n or x.get_device() != index:
-            raise ValueError(f"{name}[{t}] must hold {n} {what} on the gradients' device")
+    fine = (all(isinstance(x, torch.Tensor) for x in tensors) and {x.dtype for x in tensors} <= set(dtypes)
+            and {x.get_device() for x in tensors} == {index} and all([x.is_contiguous() for x in tensors]))
+    if not fine or [x.numel() for x in tensors] != numels:
+        t = next((t for t, (x, n) in enumerate(zip(tensors, numels)) if not isinstance(x, torch.Tensor)
+                  or x.dtype not in dtypes or x.get_device() != index or not x.is_contiguous() or x.numel() != n), 0)
+        raise ValueError(f"{name}[{t}] must be a contiguous tensor of {numels[t]} {what} on the gradients' device")
     return [x.data_ptr() for x in tensors]
 
 
