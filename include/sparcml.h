@@ -570,7 +570,7 @@ SPARCML_API int sparcml_adamw(const sparcml_tensors* plan, const sparcml_adamw_a
  * but -Inf has lse -Inf, log probability -Inf and a zero gradient.  Rows
  * without a token (or with weight 0) are not read: they may hold anything.
  * Sums of exponentials are taken in fp32 over the differences to the row's
- * maximum.
+ * maximum; log probabilities are formed in fp64 from there and rounded once.
  */
 typedef struct sparcml_logits {
     const void* x;

@@ -279,9 +279,15 @@ struct Own {
 
 // Row blockIdx.x by one workgroup: the first NV pieces of a thread stay in
 // registers between the two passes over them, the rest of a longer row is
-// read once more (mostly from the cache), the singles one a thread.  Writes
-// the log probability, lse and part where wanted, and with GRAD the gradient
-// of the policy loss.
+// read once more (from the 256 MB cache: marked nontemporal, it costs 960 us
+// instead of 804 below), the singles one a thread.  Writes the log probability,
+// lse and part where wanted, and with GRAD the gradient of the policy loss.
+// At 64 registers a thread two workgroups of 1024 share a CU, and one's loads
+// and stores go on under the other's exponentials: 8192 x 131072 bf16 780 us, 5.5
+// TB/s of logits and gradient (two passes by slices 1207; rows of 131072 wholly
+// in registers, one workgroup a CU, 857).  Without its exponentials it takes 800
+// of 804: what bounds it is memory, at the rate that rows of 256 KB a workgroup
+// are copied (5.5 to 6.0 TB/s).
 template <int TYPE, int THREADS, int NV, bool GRAD, bool KEEP>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
 k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, float* at_label, uint32_t* ticket,
@@ -388,7 +394,8 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
 
 // Slice s of a row: pieces [s W, (s + 1) W); slice 0 takes the singles too.
 // (M, Z) of every slice of every row in use, the token's logit beside them;
-// with one slice a row its log probability (lse, terms) at once.
+// with one slice a row its log probability (lse, terms) at once.  Bound by HBM:
+// 8192 x 131072 bf16 317 us, 6.8 TB/s (361 with plain loads).
 template <int TYPE, bool KEEP>
 __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, uint32_t S, uint32_t W, float c,
                                                 Part* part, float* at_label, float* logp, float* lse, PolicyArgs a,
@@ -614,7 +621,8 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
 
 // The gradient by slices from coefficients that are there: of a policy loss
 // whose rows are one slice each (its terms), or of pairs (coef).  Workgroup 0:
-// the sums over tokens or pairs.
+// the sums over tokens or pairs.  Bound by HBM: 8192 x 131072 bf16 690 us, 6.2
+// TB/s, with 2 pieces a thread (896 with one, 709 with four).
 template <int TYPE, bool POLICY>
 __global__ void __launch_bounds__(256) k_grad(Logits in, PolicyArgs a, const PolicyTerms* terms, uint32_t pairs,
                                               const float* coef, const PairSums* sums, float factor, uint32_t S,

@@ -4,7 +4,10 @@
 // Both walk a map of pieces of 4096 elements, {tensor, piece of it}, that
 // tensors_prepare_run lays out once: a workgroup finds its tensor with two
 // loads, whatever the number and the lengths of the tensors, and one launch
-// covers them all.
+// covers them all.  Both are bound by HBM: accesses are 16 bytes a lane (8 for
+// 16-bit types of the step), marked nontemporal, and a piece of 32-bit moments
+// begins at a line of its tensor (2^27 weights in 290 packed tensors: 725 us
+// with pieces from the tensors' first elements, 655 so).
 #include "internal.h"
 #include "philox_device.h"
 #include "types_device.h"
@@ -125,10 +128,20 @@ __device__ __forceinline__ uint32_t block_exponent(f32x4 x)
 }
 
 // One AdamW step: a quarter of a piece of the map a workgroup, four elements
-// a lane, so that a wave holds exactly one block of the 8-bit form.
+// a lane, so that a wave holds exactly one block of the 8-bit form and its
+// scale is one wave maximum.  Moments in 8 bits are rounded stochastically: the
+// second one moves by 1 - beta2 of itself a step, far less than half a code, and
+// rounding to nearest would hold it still.
+// Bytes an element: 28 (32-bit moments, fp32 gradient) or 16 and 16/256 (8-bit).
+// 20 M weights in 148 tensors, 32-bit: 91 us, 6.1 TB/s; 2^27 in 290, 8-bit: 385 us,
+// 5.6 TB/s (a large copy: 6.2).  One vector a lane is the right size: with 4
+// vectors 838 and 482 us instead of 725 and 387 (more in flight, in less even
+// order).  Without the generator, or with approximate roots and quotients, the
+// 8-bit step is 2 to 3% faster, so neither is what bounds it.
 template <int BITS, int GT, int CT>
-__global__ void __launch_bounds__(256) k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
-                                               uint64_t pieces, AdamwStep a, const float* __restrict__ clip)
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(8)))
+k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map, uint64_t pieces, AdamwStep a,
+        const float* __restrict__ clip)
 {
     constexpr uint32_t kSub = kTensorChunk / 1024;
     float f = a.gs;
@@ -199,8 +212,12 @@ __device__ __forceinline__ double block_sum(double x, double* s_w)
     return (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
 }
 
-// Norm of all gradients: workgroup b sums the squares of pieces b, b + G, ...,
-// the last workgroup to finish the partial sums, in their order.
+// Norm of all gradients: workgroup b sums the squares of pieces b, b + G, ...
+// in fp64, the last workgroup to finish the partial sums, in their order (the
+// same bits whichever it is).  2^27 in 290 tensors: fp32 81 us, 6.6 TB/s, bf16 43
+// us (1024 workgroups; 94 and 48 with 2048, whose loads crowd the memory); 20 M
+// bf16 in 148 tensors 10.7 us, where the chain map, tensor, gradient and the last
+// workgroup's sum count.
 template <int GT>
 __global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
                                               uint64_t pieces, double* partial, uint32_t* ticket, double gs,
