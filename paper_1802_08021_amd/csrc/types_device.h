@@ -57,14 +57,14 @@ template <class V, bool KEEP = false, class E>
 __device__ __forceinline__ V load_vec(const E* p)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
-    const SPARCML_GLOBAL U* q = as_global(reinterpret_cast<const U*>(p));
+    const SPARCML_GLOBAL U* q = (const SPARCML_GLOBAL U*)p;
     return KEEP ? *q : __builtin_nontemporal_load(q);
 }
 template <class V, class E>
 __device__ __forceinline__ void store_vec(E* p, V v)
 {
     typedef V U __attribute__((aligned(sizeof(E))));
-    __builtin_nontemporal_store(v, as_global(reinterpret_cast<U*>(p)));
+    __builtin_nontemporal_store(v, (SPARCML_GLOBAL U*)p);
 }
 
 // Sum and maximum of the 64 lanes' values, in every lane: shifts within rows
