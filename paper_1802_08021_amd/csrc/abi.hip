@@ -648,7 +648,8 @@ int sparcml_tensors_prepare(int count, const sparcml_tensor* tensors, int grad_t
             const uintptr_t at = (uintptr_t)(state_bits ? (const void*)a.param : a.grad);
             const uint32_t size = state_bits || grad_type == SPARCML_F32 ? 4 : 2;
             const uint32_t shift = state_bits == 8 ? 0 : (uint32_t)(at % 128 / size);
-            d[t] = TensorDesc{a.param, a.grad, a.m, a.v, a.m_scale, a.v_scale, a.copy, a.n, a.decay, a.lr_scale, shift, 0};
+            d[t] = TensorDesc{a.param, a.grad, a.m, a.v, a.m_scale, a.v_scale, a.copy, a.n, a.decay, a.lr_scale, shift,
+                              (uint32_t)chunks};
             total += a.n;
             chunks += tensor_chunks(a.n, shift);
         }

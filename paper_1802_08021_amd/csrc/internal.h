@@ -245,7 +245,7 @@ enum ElemType : uint32_t { kF32 = 0, kBf16 = 1, kF16 = 2 };
 constexpr uint32_t kStateBlock = 256;    // elements that share a scale (8-bit moments)
 constexpr uint32_t kTensorChunk = 4096;  // elements of a tensor that the work map lists as one piece
 
-// Device copy of one tensor descriptor (80 bytes).
+// Device copy of one tensor descriptor.
 struct TensorDesc {
     float* param;
     const void* grad;
@@ -258,16 +258,24 @@ struct TensorDesc {
     float decay, lr_scale;
     // Pieces of work begin this many elements before the tensor, so that each
     // begins at a line of its weights (32-bit moments) or of its gradient.
-    uint32_t shift, pad;
+    uint32_t shift;
+    uint32_t first;  // the tensor's first piece
+};
+
+// One piece of work: its tensor with all that a workgroup needs of it (one
+// load, not a chain of two), and which piece of which tensor it is.
+struct TensorPiece {
+    TensorDesc d;
+    uint32_t tensor, index;
+    uint32_t pad[2];
 };
 
 // What a prepared workspace holds; the same carving for every call on it.
 struct TensorTab {
-    TensorDesc* desc;  // [count]
-    uint32_t* first;   // [count] a tensor's first chunk
-    uint2* map;        // [chunks] {tensor, chunk of it}
-    double* partial;   // [kNormParts]
-    uint32_t* ticket;  // [kTickets * kTicketStride], 0 between calls
+    TensorDesc* desc;    // [count]
+    TensorPiece* piece;  // [chunks]
+    double* partial;     // [kNormParts]
+    uint32_t* ticket;    // [kTickets * kTicketStride], 0 between calls
 };
 constexpr uint32_t kNormParts = 1024;
 // Counters of a norm's finished workgroups: kTickets - 1 groups', and the

@@ -1,10 +1,10 @@
 // The update of Alg. 1 on gfx950: norm of a model's gradients, AdamW step
 // over all its tensors, moments in 32 or in 8 bits.
 //
-// Both walk a map of pieces of 4096 elements, {tensor, piece of it}, that
-// tensors_prepare_run lays out once: a workgroup finds its tensor with two
-// loads, whatever the number and the lengths of the tensors, and one launch
-// covers them all.  Both are bound by HBM: accesses are 16 bytes a lane (8 for
+// Both walk a list of pieces of 4096 elements that tensors_prepare_run lays out
+// once, each with its tensor's addresses and rates: a workgroup knows what to do
+// after one load, whatever the number and the lengths of the tensors, and one
+// launch covers them all.  Both are bound by HBM: accesses are 16 bytes a lane (8 for
 // 16-bit types of the step), marked nontemporal, and a piece of 32-bit moments
 // begins at a line of its tensor (2^27 weights in 290 packed tensors: 725 us
 // with pieces from the tensors' first elements, 655 so).
@@ -13,19 +13,21 @@
 #include "types_device.h"
 
 #include <algorithm>
-#include <vector>
 
 namespace sparcml {
 namespace {
 
-// map[first[t] + i] = {t, i} for the pieces i of tensor t.
-__global__ void k_tensor_map(const TensorDesc* desc, const uint32_t* first, uint2* map, uint32_t* ticket)
+// The pieces of tensor blockIdx.x.
+__global__ void k_tensor_pieces(const TensorDesc* desc, TensorPiece* piece, uint32_t* ticket)
 {
     const uint32_t t = blockIdx.x;
     if (t == 0 && threadIdx.x < kTickets) ticket[threadIdx.x * kTicketStride] = 0;
-    const TensorDesc d = desc[t];
-    const uint32_t pieces = d.n ? (uint32_t)((d.n + d.shift + kTensorChunk - 1) / kTensorChunk) : 0;
-    for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) map[first[t] + i] = make_uint2(t, i);
+    TensorPiece p;
+    p.d = desc[t];
+    p.tensor = t;
+    p.pad[0] = p.pad[1] = 0;
+    const uint32_t pieces = p.d.n ? (uint32_t)((p.d.n + p.d.shift + kTensorChunk - 1) / kTensorChunk) : 0;
+    for (p.index = threadIdx.x; p.index < pieces; p.index += blockDim.x) piece[p.d.first + p.index] = p;
 }
 
 // Element e of an array of n as fp32, zero outside it (e may lie before the
@@ -127,7 +129,7 @@ __device__ __forceinline__ uint32_t block_exponent(f32x4 x)
     return max(e, 35u) - 8u;
 }
 
-// One AdamW step: a quarter of a piece of the map a workgroup, four elements
+// One AdamW step: a quarter of a piece a workgroup, four elements
 // a lane, so that a wave holds exactly one block of the 8-bit form and its
 // scale is one wave maximum.  Moments in 8 bits are rounded stochastically: the
 // second one moves by 1 - beta2 of itself a step, far less than half a code, and
@@ -140,8 +142,7 @@ __device__ __forceinline__ uint32_t block_exponent(f32x4 x)
 // 8-bit step is 2 to 3% faster, so neither is what bounds it.
 template <int BITS, int GT, int CT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(8)))
-k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map, uint64_t pieces, AdamwStep a,
-        const float* __restrict__ clip)
+k_adamw(const TensorPiece* __restrict__ piece, uint64_t pieces, AdamwStep a, const float* __restrict__ clip)
 {
     constexpr uint32_t kSub = kTensorChunk / 1024;
     float f = a.gs;
@@ -152,12 +153,12 @@ k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map, uint
     }
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
     for (uint64_t w = blockIdx.x; w < pieces * kSub; w += gridDim.x) {
-        const uint2 at = map[w / kSub];
-        const TensorDesc d = desc[at.x];
+        const TensorPiece at = piece[w / kSub];
+        const TensorDesc& d = at.d;
         const float keep = (float)(1.0 - a.lr * (double)d.lr_scale * (double)d.decay);
         const float rate = (float)(a.rate * (double)d.lr_scale);
         // the wave's first element and the lane's (below zero: before the tensor)
-        const uint64_t b = (uint64_t)at.y * kTensorChunk + (uint32_t)(w % kSub) * 1024 + (uint32_t)wv * 256 - d.shift;
+        const uint64_t b = (uint64_t)at.index * kTensorChunk + (uint32_t)(w % kSub) * 1024 + (uint32_t)wv * 256 - d.shift;
         const uint64_t e = b + (uint32_t)lane * 4;
         if ((int64_t)b < (int64_t)d.n) {
             f32x4 p = get4<kF32>(d.param, e, d.n);
@@ -186,7 +187,7 @@ k_adamw(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map, uint
                 put4<kF32>(d.v, e, d.n, v);
             } else {
                 // lanes past the end hold zeros (of weights and states alike)
-                const uint4 z = philox(make_uint4((uint32_t)(e >> 2), at.x, a.step, 0u), a.key0, a.key1);
+                const uint4 z = philox(make_uint4((uint32_t)(e >> 2), at.tensor, a.step, 0u), a.key0, a.key1);
                 const uint32_t em = block_exponent(m), er = block_exponent(r);
                 const f32x4 ym = m * __uint_as_float((254u - em) << 23);
                 f32x4 yr = r * __uint_as_float((254u - er) << 23);
@@ -214,14 +215,13 @@ __device__ __forceinline__ double block_sum(double x, double* s_w)
 
 // Norm of all gradients: workgroup b sums the squares of pieces b, b + G, ...
 // in fp64, the last workgroup to finish the partial sums, in their order (the
-// same bits whichever it is).  2^27 in 290 tensors: fp32 81 us, 6.6 TB/s, bf16 43
+// same bits whichever it is).  2^27 in 290 tensors: fp32 81 us, 6.6 TB/s, bf16 44
 // us (1024 workgroups; 94 and 48 with 2048, whose loads crowd the memory); 20 M
-// bf16 in 148 tensors 10.7 us, where the chain map, tensor, gradient and the last
+// bf16 in 148 tensors 10.4 us, where the chain piece, gradient and the last
 // workgroup's sum count.
 template <int GT>
-__global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ desc, const uint2* __restrict__ map,
-                                              uint64_t pieces, double* partial, uint32_t* ticket, double gs,
-                                              double max_norm, float* out)
+__global__ void __launch_bounds__(256) k_norm(const TensorPiece* __restrict__ piece, uint64_t pieces, double* partial,
+                                              uint32_t* ticket, double gs, double max_norm, float* out)
 {
     __shared__ double s_w[4], s_end[4];
     __shared__ uint32_t s_last;
@@ -233,9 +233,9 @@ __global__ void __launch_bounds__(256) k_norm(const TensorDesc* __restrict__ des
     constexpr int N = GT == kF32 ? 4 : 8, R = kTensorChunk / (256 * N);  // elements of 16 bytes; accesses a piece
     typedef typename Elem<GT>::type E;
     for (uint64_t c = blockIdx.x; c < pieces; c += gridDim.x) {
-        const uint2 at = map[c];
-        const E* grad = static_cast<const E*>(desc[at.x].grad);
-        const uint64_t n = desc[at.x].n, e0 = (uint64_t)at.y * kTensorChunk - desc[at.x].shift;
+        const TensorPiece& at = piece[c];
+        const E* grad = static_cast<const E*>(at.d.grad);
+        const uint64_t n = at.d.n, e0 = (uint64_t)at.index * kTensorChunk - at.d.shift;
         if (e0 < n && e0 + kTensorChunk <= n) {  // a whole piece
             u32x4 w[R];
 #pragma unroll
@@ -295,7 +295,7 @@ template <int BITS, int GT, int CT>
 void launch_adamw(const TensorTab& t, uint64_t pieces, const AdamwStep& a, const float* clip, hipStream_t s)
 {
     const uint64_t grid = std::min<uint64_t>(pieces * (kTensorChunk / 1024), 1u << 22);
-    hipLaunchKernelGGL((k_adamw<BITS, GT, CT>), dim3((uint32_t)grid), dim3(256), 0, s, t.desc, t.map, pieces, a, clip);
+    hipLaunchKernelGGL((k_adamw<BITS, GT, CT>), dim3((uint32_t)grid), dim3(256), 0, s, t.piece, pieces, a, clip);
 }
 
 template <int BITS, int GT>
@@ -327,8 +327,7 @@ TensorTab tensors_carve(void* ws, uint32_t count, uint64_t chunks, size_t* bytes
     Carve c(ws);
     TensorTab t;
     t.desc = c.take<TensorDesc>(count);
-    t.first = c.take<uint32_t>(count);
-    t.map = c.take<uint2>(chunks);
+    t.piece = c.take<TensorPiece>(chunks);
     t.partial = c.take<double>(kNormParts);
     t.ticket = c.take<uint32_t>(kTickets * kTicketStride);
     if (bytes) *bytes = c.used;
@@ -338,16 +337,9 @@ TensorTab tensors_carve(void* ws, uint32_t count, uint64_t chunks, size_t* bytes
 hipError_t tensors_prepare_run(uint32_t count, const TensorDesc* host, uint64_t chunks, void* ws, hipStream_t s)
 {
     const TensorTab t = tensors_carve(ws, count, chunks, nullptr);
-    std::vector<uint32_t> first(count);
-    uint64_t at = 0;
-    for (uint32_t i = 0; i < count; ++i) {
-        first[i] = (uint32_t)at;
-        at += tensor_chunks(host[i].n, host[i].shift);
-    }
     hipError_t e = upload(t.desc, host, count * sizeof(TensorDesc), s);
-    if (e == hipSuccess) e = upload(t.first, first.data(), count * sizeof(uint32_t), s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_tensor_map, dim3(count), dim3(256), 0, s, t.desc, t.first, t.map, t.ticket);
+    hipLaunchKernelGGL(k_tensor_pieces, dim3(count), dim3(256), 0, s, t.desc, t.piece, t.ticket);
     return hipGetLastError();
 }
 
@@ -358,7 +350,7 @@ hipError_t grad_norm_run(uint32_t count, uint64_t chunks, uint32_t gtype, double
     const uint32_t parts = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(chunks, kNormParts));
     timer_begin(kTGradNorm, s);
     auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3(parts), dim3(256), 0, s, t.desc, t.map, chunks, t.partial, t.ticket, grad_scale,
+        hipLaunchKernelGGL(kern, dim3(parts), dim3(256), 0, s, t.piece, chunks, t.partial, t.ticket, grad_scale,
                            max_norm, out);
     };
     if (gtype == kF32)
