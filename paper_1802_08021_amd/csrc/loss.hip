@@ -218,19 +218,19 @@ __device__ __forceinline__ void put_policy_stats(const PolicyArgs& a, double* x,
     }
 }
 
-// The sums over tokens of their terms (four rows a thread in flight).
+// The sums over tokens of their terms (eight rows a thread in flight).
 __global__ void __launch_bounds__(1024) k_policy_stats(uint64_t rows, PolicyArgs a, const PolicyTerms* terms,
                                                        float* stats)
 {
     __shared__ double s_w[16][4];
     double x[3] = {0.0, 0.0, 0.0};
-    for (uint64_t t = threadIdx.x; t < rows; t += 4096) {
-        PolicyTerms r[4] = {};
+    for (uint64_t t = threadIdx.x; t < rows; t += 8192) {
+        PolicyTerms r[8] = {};
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
             if (t + 1024 * i < rows) r[i] = terms[t + 1024 * i];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) add_terms(r[i], x);
+        for (int i = 0; i < 8; ++i) add_terms(r[i], x);
     }
     put_policy_stats(a, x, s_w, stats);
 }
@@ -278,24 +278,27 @@ struct Own {
 };
 
 // Row blockIdx.x by one workgroup: the first NV pieces of a thread stay in
-// registers between the two passes over them, the rest of a longer row is
-// read once more (from the 256 MB cache: marked nontemporal, it costs 960 us
-// instead of 804 below), the singles one a thread.  Writes the log probability,
-// lse and part where wanted, and with GRAD the gradient of the policy loss.
+// registers between the two passes over them, LP more in LDS, the rest of a
+// longer row is read once more (GRAD; from the 256 MB cache: marked nontemporal,
+// it costs 960 us instead of 804 below), the singles one a thread.  Writes the log
+// probability, lse and part where wanted, and with GRAD the gradient of the
+// policy loss.
 // At 64 registers a thread two workgroups of 1024 share a CU, and one's loads
-// and stores go on under the other's exponentials: 8192 x 131072 bf16 780 us, 5.5
+// and stores go on under the other's exponentials: 8192 x 131072 bf16 770 us, 5.6
 // TB/s of logits and gradient (two passes by slices 1207; rows of 131072 wholly
-// in registers, one workgroup a CU, 857).  Without its exponentials it takes 800
-// of 804: what bounds it is memory, at the rate that rows of 256 KB a workgroup
-// are copied (5.5 to 6.0 TB/s).
-template <int TYPE, int THREADS, int NV, bool GRAD, bool KEEP>
+// in registers, one workgroup a CU, 857; nothing in LDS 799; 1024 rows 103, with
+// nothing in LDS 114).  Without its exponentials it takes 800 of 804: what
+// bounds it is memory, at the rate that rows of 256 KB a workgroup are copied
+// (5.5 to 6.0 TB/s).
+template <int TYPE, int THREADS, int NV, int LP, bool GRAD, bool KEEP>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
 k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, float* at_label, uint32_t* ticket,
       PolicyTerms* terms, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
-    constexpr int N = Piece<TYPE>::N, U = 1;
+    constexpr int N = Piece<TYPE>::N;
     __shared__ float s_top[THREADS / 64], s_sum[THREADS / 64], s_x, s_coef;
+    __shared__ u32x4 s_keep[LP ? LP * THREADS : 1];
     if (!GRAD && blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;  // for k_policy_grad
     const uint64_t t = blockIdx.x;
     const uint32_t V = (uint32_t)in.vocab, label = (uint32_t)in.label[t], tid = threadIdx.x, step = blockDim.x;
@@ -323,14 +326,12 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
     const float single = tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
     if (tid == 0) s_x = (float)row[label];
     Own own = {single, single == -INFINITY ? 0.0f : 1.0f};
-    for (uint32_t j = tid + step * NV; j < r.full; j += step * U) {
-        Piece<TYPE> y[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            y[u].none();
-            if (j + step * u < r.full) y[u].w = load_vec<u32x4, true>(row + r.piece(j + step * u));
-        }
-        own.add(y, U, c);
+    // (a thread's slots in LDS are its own: no barrier between the passes)
+    for (uint32_t j = tid + step * NV, slot = tid; GRAD && j < r.full; j += step, slot += step) {
+        Piece<TYPE> y[1];
+        y[0].w = load_vec<u32x4, true>(row + r.piece(j));
+        own.add(y, 1, c);
+        if (LP && slot < LP * step) s_keep[slot] = y[0].w;
     }
     own.add(x, used, c);
     float top = join_waves<false>(own.top, s_top);
@@ -351,11 +352,10 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
         }
     }
     if (!GRAD) return;
-    uint32_t j = tid + step * NV;
-    Piece<TYPE> next[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (j + step * u < r.full) next[u].w = load_vec<u32x4>(row + r.piece(j + step * u));
+    // (the first piece that is read again is under way over the barrier)
+    uint32_t j = tid + step * (NV + LP);
+    Piece<TYPE> next;
+    if (j < r.full) next.w = load_vec<u32x4>(row + r.piece(j));
     __syncthreads();
     const float coef = s_coef, xl = s_x;
     const float k = coef == 0.0f ? 0.0f : -coef / p.sum;
@@ -372,16 +372,15 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
         if (i >= used) break;
         write(x[i], tid + step * i);
     }
-    while (j < r.full) {
-        Piece<TYPE> now[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            now[u] = next[u];
-            if (j + step * (U + u) < r.full) next[u].w = load_vec<u32x4>(row + r.piece(j + step * (U + u)));
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) write(now[u], j + step * u);
-        j += step * U;
+    for (uint32_t i = 0; i < (uint32_t)LP && tid + step * (NV + i) < r.full; ++i) {
+        Piece<TYPE> now;
+        now.w = s_keep[tid + step * i];
+        write(now, tid + step * (NV + i));
+    }
+    for (; j < r.full; j += step) {
+        Piece<TYPE> now = next;
+        if (j + step < r.full) next.w = load_vec<u32x4>(row + r.piece(j + step));
+        write(now, j);
     }
     if (tid < r.singles) out[r.single(tid)] = (E)entry(single, c, top, k);
     // the label's own entry once more, by the thread that has just written it
@@ -750,7 +749,8 @@ struct Cut {
 constexpr uint64_t kManyRows = 128;
 constexpr uint64_t kMaxRows = 1u << 21;  // of a launch with a workgroup a row (fewer than 2^32 threads)
 constexpr uint32_t kMaxGrid = 1u << 22;
-constexpr uint32_t kHold = 8;  // pieces a thread of k_row holds
+constexpr uint32_t kHold = 8;     // pieces a thread of k_row holds in registers,
+constexpr uint32_t kHoldLds = 4;  // and one of 1024 in LDS (64 KB: two workgroups a CU)
 
 Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
 {
@@ -828,12 +828,14 @@ void launch_row(const Cut& cut, Logits in, PolicyArgs a, float* logp, float* lse
         constexpr int TY = decltype(ty)::value;
         for (uint64_t r0 = 0; r0 < rows; r0 += kMaxRows) {
             const dim3 grid((uint32_t)std::min(rows - r0, kMaxRows)), block((uint32_t)std::min(threads, most));
-            if (most == 512)
-                hipLaunchKernelGGL((k_row<TY, 512, kHold, GRAD, KEEP>), grid, block, 0, s, in, a, c, logp, lse, part,
-                                   at_label, sp.ticket, terms, dlogits, ldd);
+            auto go = [&](auto kern) {
+                hipLaunchKernelGGL(kern, grid, block, 0, s, in, a, c, logp, lse, part, at_label, sp.ticket, terms, dlogits,
+                                   ldd);
+            };
+            if (!GRAD || most == 512)  // (cut.row: 512 threads hold the row)
+                go(k_row<TY, 512, kHold, 0, GRAD, KEEP>);
             else
-                hipLaunchKernelGGL((k_row<TY, 1024, kHold, GRAD, KEEP>), grid, block, 0, s, in, a, c, logp, lse, part,
-                                   at_label, sp.ticket, terms, dlogits, ldd);
+                go(k_row<TY, 1024, kHold, kHoldLds, true, false>);
             // the next rows
             auto on = [](auto*& p, uint64_t n) {
                 if (p) p += n;
