@@ -567,8 +567,8 @@ SPARCML_API int sparcml_adamw(const sparcml_tensors* plan, const sparcml_adamw_a
  *   scale    inverse temperature, > 0: the distribution of row t is the
  *            softmax of scale * x[t].
  * Logits may be -Inf (a token that cannot come).  A row that holds nothing
- * but -Inf has lse -Inf, log probability -Inf and a zero gradient.  Rows
- * without a token (or with weight 0) are not read: they may hold anything.
+ * but -Inf has lse -Inf and log probability -Inf.  Rows without a token (or
+ * with weight 0) are not read: they may hold anything.
  * Sums of exponentials are taken in fp32 over the differences to the row's
  * maximum; log probabilities are formed in fp64 from there and rounded once.
  */
@@ -603,6 +603,12 @@ SPARCML_API int sparcml_token_logprob(const sparcml_logits* in, float* logp, flo
  *   dlogits[t][v] = grad_scale * scale * coef * ([v == label] - softmax_v)
  * Rows without a token or with w == 0 add nothing, have logp 0 and a zero
  * gradient.  Sums over rows are taken in fp64 in a fixed order.
+ * A row that holds nothing but -Inf adds nothing.  A token whose own logit is
+ * -Inf adds what the formulas give (without old or ref of -Inf too, a ratio of
+ * 0 and a k of +Inf).  Both have logp -Inf whatever the row's other logits
+ * are, and so a zero gradient.  In the formulas old or ref that is the same
+ * infinity as lp is 0 away from it, and 0 times an infinity (an advantage or
+ * kl of 0) is 0.
  *   old, adv, weight  device float[rows];  ref: the same, or NULL (then kl
  *            is not read).
  *   clip_lo in [0, 1], clip_hi >= 0, kl finite, grad_scale finite.

@@ -162,27 +162,37 @@ struct PolicyRow {
     }
 };
 
+// Log probabilities are -Inf where a token cannot come: two that are the same
+// infinity are 0 apart, and a factor of 0 takes an infinity away (NaN stays).
+__device__ __forceinline__ double apart(double x, double y) { return x == y ? 0.0 : x - y; }
+template <class T>
+__device__ __forceinline__ T times(T a, T x)
+{
+    return a == (T)0 && fabs(x) == (T)INFINITY ? (T)0 : a * x;
+}
+
 // Its terms and the loss' derivative by its log probability, all with the
-// weight.
+// weight.  A row that holds nothing but -Inf has none; a log probability of
+// -Inf does not move with the row's logits.
 struct PolicyTerms {
     float gain, k, clipped, coef;
 };
-__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const PolicyRow& q, double lp)
+__device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const PolicyRow& q, const Part& p, double lp)
 {
-    PolicyTerms r;
-    const float rho = exp2_fast((float)((lp - (double)q.old) * 1.44269504088896341));
-    const float u = rho * q.adv, held = fminf(fmaxf(rho, a.lo), a.hi) * q.adv;
+    PolicyTerms r = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (p.sum == 0.0f) return r;
+    const float rho = exp2_fast((float)(apart(lp, (double)q.old) * 1.44269504088896341));
+    const float u = times(q.adv, rho), held = times(q.adv, fminf(fmaxf(rho, a.lo), a.hi));
     const bool clipped = u > held;
     r.gain = q.w * (clipped ? held : u);  // (a NaN of u comes through)
     r.clipped = clipped ? q.w : 0.0f;
-    r.k = 0.0f;
     r.coef = clipped ? 0.0f : -u;
     if (a.ref_logp) {
-        const float far = (float)((double)q.ref - lp), em = expm1f(far);
-        r.k = q.w * (em - far);
-        r.coef = r.coef - a.kl * em;
+        const float far = (float)apart((double)q.ref, lp), em = expm1f(far);
+        r.k = q.w * (far == INFINITY ? far : em - far);
+        r.coef = r.coef - times(a.kl, em);
     }
-    r.coef = q.w * r.coef;
+    r.coef = lp == -INFINITY ? 0.0f : q.w * r.coef;
     return r;
 }
 
@@ -211,7 +221,7 @@ __device__ __forceinline__ void put_policy_stats(const PolicyArgs& a, double* x,
 {
     block_sum(x, s_w, 3);
     if (threadIdx.x == 0) {
-        stats[0] = (float)((a.ref_logp ? (double)a.kl * x[1] : 0.0) - x[0]);
+        stats[0] = (float)((a.ref_logp ? times((double)a.kl, x[1]) : 0.0) - x[0]);
         stats[1] = (float)-x[0];
         stats[2] = (float)x[1];
         stats[3] = (float)x[2];
@@ -346,9 +356,9 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
             at_label[t] = s_x;
         }
         if (terms) {
-            const PolicyTerms m = policy_terms(a, q, lp);
+            const PolicyTerms m = policy_terms(a, q, p, lp);
             terms[t] = m;
-            if (GRAD) s_coef = p.sum == 0.0f ? 0.0f : a.grad_scale * in.scale * m.coef;
+            if (GRAD) s_coef = a.grad_scale * in.scale * m.coef;
         }
     }
     if (!GRAD) return;
@@ -440,7 +450,7 @@ __global__ void __launch_bounds__(256) k_slices(Logits in, const float* weight, 
                 const double lp = part_logp(p, at, in.scale);
                 logp[t] = (float)lp;
                 if (lse) lse[t] = part_lse(p, in.scale);
-                if (terms) terms[t] = policy_terms(a, PolicyRow(a, t), lp);
+                if (terms) terms[t] = policy_terms(a, PolicyRow(a, t), p, lp);
             }
         }
         __syncthreads();
@@ -552,7 +562,7 @@ __global__ void __launch_bounds__(256) k_policy_grad(Logits in, PolicyArgs a, ui
             const float at = at_label[t];
             p = join_slices(part + t * S, S, g, c);
             lp = part_logp(p, at, in.scale);
-            m = policy_terms(a, q, lp);
+            m = policy_terms(a, q, p, lp);
         }
         if (s == 0 && threadIdx.x == 0) {
             logp[t] = (float)lp;

@@ -1,0 +1,111 @@
+"""Losses over rows that hold nothing but -Inf and tokens whose own logit is
+-Inf, against 64 bits, in every path: such a row has no gradient and leaves the
+others as they are.  Bounds as derived in test_gpu_loss."""
+import numpy as np
+import pytest
+
+from gpu_util import say, to_np, torch_dev
+from test_gpu_loss import U, check_gradient, lp_bound, make
+
+pytestmark = pytest.mark.gpu
+INF = np.inf
+
+# rows x vocabulary: a workgroup a row with the gradient, 512 and 1024 threads;
+# the gradient by slices after a row a workgroup; slices of rows, joined; slices
+# that are whole rows (without a gradient, or for a preference loss).
+PATHS = [(130, 500, "float32"), (130, 70000, "bfloat16"), (9, 500, "float16"), (9, 40000, "float32"),
+         (600, 20000, "float32")]
+
+
+def apart(a, b):
+    return np.where(a == b, 0.0, a - np.where(a == b, 0.0, b))
+
+
+def log_probs(x, label, scale):
+    """(lp, softmax, empty) of each row in 64 bits."""
+    y = x * scale
+    top = y.max(1)
+    empty = top == -INF
+    e = np.exp(y - np.where(empty, 0.0, top)[:, None])
+    z = np.where(empty, 1.0, e.sum(1))
+    at = np.take_along_axis(y, label[:, None].astype(np.int64), 1)[:, 0]
+    return at - np.where(empty, 0.0, top) - np.log(z), e / z[:, None], empty
+
+
+def gradient(soft, label, coef, scale):
+    d = -coef[:, None] * scale * soft
+    d[np.arange(len(coef)), label] += coef * scale
+    return d
+
+
+def masked(T, V, kind, seed):
+    """Row 0 empty, row 1 with its own token masked, row 2 half masked."""
+    x, label, gen = make(T, V, kind, seed, pad=3)
+    x[0] = float("-inf")
+    label[1:3] = 1
+    x[1, 1] = float("-inf")
+    x[2, V // 2:] = float("-inf")
+    return x, label, gen
+
+
+@pytest.mark.parametrize("T,V,kind", PATHS)
+@pytest.mark.parametrize("same", [True, False])
+@pytest.mark.parametrize("kl", [None, 0.0, 0.05])
+def test_policy_loss(T, V, kind, same, kl):
+    """same: old and reference values come from token_logprob over the same
+    logits (-Inf where it is), else they are finite there.  kl None: without
+    reference values."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    say(f"[masked policy] {T} {V} {kind} {same} {kl}")
+    x, label, gen = masked(T, V, kind, T + V)
+    rnd = lambda s: torch.randn(T, device=dev, generator=gen) * s  # noqa: E731
+    lp, _ = S.token_logprob(x, label)
+    assert lp[0] == -INF and lp[1] == -INF and bool(torch.isfinite(lp[2:]).all())
+    old, ref = lp + rnd(0.3), lp + rnd(0.4)
+    if not same:
+        old[:2], ref[:2] = -1.0, -2.0
+    adv = rnd(1.0)
+    adv[1] = -0.5
+    adv[3], old[3] = 0.0, old[3] - 200.0  # a ratio beyond fp32 of no advantage
+    adv[4], old[4] = 2.0, float("-inf")   # clipped
+    weight = torch.rand(T, device=dev, generator=gen) + 0.1
+    h, l = x.double().cpu().numpy(), label.cpu().numpy()
+    n = [to_np(a).astype(np.float64) for a in (old, ref, adv, weight)]
+    with np.errstate(all="ignore"):
+        p, soft, empty = log_probs(h, l, 1.0)
+        rho = np.exp(apart(p, n[0]))
+        u = np.where(n[2] == 0, 0.0, rho * n[2])
+        held = np.clip(rho, np.float32(0.8), np.float32(1.2)) * n[2]
+        gain, cut = np.minimum(u, held), u > held
+        far = apart(n[1], p) if kl is not None else np.zeros(T)
+        k = np.where(far == INF, INF, np.expm1(far) - far)
+        beta = float(np.float32(kl)) if kl else 0.0
+        coef = -np.where(cut, 0.0, u) - (beta * np.expm1(far) if beta else 0.0)
+        use = ~empty
+        coef = np.where(p == -INF, 0.0, n[3] * coef)
+        w = n[3][use]
+        policy, kls = np.sum(w * -gain[use]), np.sum(w * k[use])
+        want = np.array([policy + (beta * kls if beta else 0.0), policy, kls, np.sum(w * cut[use])])
+        size = n[3] * (np.abs(np.where(cut, held, u)) + (np.exp(far) + 1 if kl is not None else 0))
+    fine = np.isfinite(p)
+    err = np.zeros(T)
+    err[fine] = lp_bound(h[fine], l[fine], 1.0, V)
+    total = np.sum((size * (err + 16 * U))[fine]) + 8 * U * np.abs(want[np.isfinite(want)]).max() + 1e-6
+    more = {} if kl is None else dict(ref=ref, kl=kl)
+    for where in ("new", None, "inplace"):
+        r = S.policy_loss(x, label, old, adv, weight, dlogits=where, **more)
+        got = to_np(r["stats"]).astype(np.float64)
+        assert np.array_equal(np.isfinite(got), np.isfinite(want)) and not np.isnan(got).any(), (got, want)
+        on = np.isfinite(want)
+        assert np.all(got[~on] == want[~on])
+        lim = 2 * total + np.array([0, 0, 0, 1e-5 * want[3]])
+        assert np.all(np.abs(got[on] - want[on]) <= lim[on]), (got, want, lim)
+        logp = to_np(r["logp"])
+        assert np.all(logp[:2] == -INF) and np.all(np.abs(logp[fine] - p[fine]) <= err[fine])
+        if where:
+            d = r["dlogits"].double().cpu().numpy()
+            assert not d[:2].any() and not d[2, V // 2:].any()
+            size_rel = np.where(coef != 0, size / np.maximum(np.abs(coef), 1e-30), 0) * (err + 16 * U)
+            check_gradient(d[fine], gradient(soft, l, coef, 1.0)[fine], np.abs(coef)[fine], h[fine], 1.0, V, kind,
+                           size_rel[fine])
