@@ -608,7 +608,8 @@ SPARCML_API int sparcml_token_logprob(const sparcml_logits* in, float* logp, flo
  * 0 and a k of +Inf).  Both have logp -Inf whatever the row's other logits
  * are, and so a zero gradient.  In the formulas old or ref that is the same
  * infinity as lp is 0 away from it, and 0 times an infinity (an advantage or
- * kl of 0) is 0.
+ * kl of 0) is 0.  coef, and its product with the scales, beyond fp32's range
+ * are held at its largest number.
  *   old, adv, weight  device float[rows];  ref: the same, or NULL (then kl
  *            is not read).
  *   clip_lo in [0, 1], clip_hi >= 0, kl finite, grad_scale finite.

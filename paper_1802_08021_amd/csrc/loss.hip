@@ -125,6 +125,10 @@ __device__ __forceinline__ float part_lse(Part p, float scale)
     return p.sum == 0.0f ? -INFINITY : (float)((double)p.top * (double)scale + part_ln(p.sum));
 }
 
+// A row's coefficient: beyond fp32, its largest number (an infinity would leave
+// NaN where the row has no probability).
+__device__ __forceinline__ float within(float x) { return fabsf(x) == INFINITY ? copysignf(3.402823466e38f, x) : x; }
+
 // One gradient entry before the label's own term.
 __device__ __forceinline__ float entry(float x, float c, float top, float k) { return k * exp2_fast((x - top) * c); }
 
@@ -192,7 +196,7 @@ __device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const P
         r.k = q.w * (far == INFINITY ? far : em - far);
         r.coef = r.coef - times(a.kl, em);
     }
-    r.coef = lp == -INFINITY ? 0.0f : q.w * r.coef;
+    r.coef = lp == -INFINITY ? 0.0f : within(q.w * r.coef);
     return r;
 }
 
@@ -358,7 +362,7 @@ k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, flo
         if (terms) {
             const PolicyTerms m = policy_terms(a, q, p, lp);
             terms[t] = m;
-            if (GRAD) s_coef = a.grad_scale * in.scale * m.coef;
+            if (GRAD) s_coef = within(a.grad_scale * in.scale * m.coef);
         }
     }
     if (!GRAD) return;
@@ -513,6 +517,7 @@ struct GradSlice {
     }
     __device__ __forceinline__ void write(E* out, uint32_t label, float coef, Part p, float c)
     {
+        coef = within(coef);
         const bool none = coef == 0.0f || p.sum == 0.0f;
         const float k = none ? 0.0f : -coef / p.sum;
 #pragma unroll

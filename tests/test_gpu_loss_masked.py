@@ -109,3 +109,28 @@ def test_policy_loss(T, V, kind, same, kl):
             size_rel = np.where(coef != 0, size / np.maximum(np.abs(coef), 1e-30), 0) * (err + 16 * U)
             check_gradient(d[fine], gradient(soft, l, coef, 1.0)[fine], np.abs(coef)[fine], h[fine], 1.0, V, kind,
                            size_rel[fine])
+
+
+@pytest.mark.parametrize("T,V,kind", PATHS[:4])
+def test_coefficients_beyond_fp32(T, V, kind):
+    """A ratio or a KL term that overflows: the gradient is as large as it can
+    be where the row has probability, and zero in masked places."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    x, label, _ = make(T, V, kind, 5, pad=3)
+    x[:, V // 2:] = float("-inf")
+    label.copy_(torch.arange(T, device=dev) % (V // 2))
+    lp, _ = S.token_logprob(x, label)
+    one = torch.ones(T, device=dev)
+    for old, adv, ref, sign in ((lp - 100, -one, None, 1), (lp - 100, -one, lp, 1), (lp, one, lp + 100, -1),
+                                (torch.full_like(lp, float("-inf")), -one, None, 1)):
+        for where in ("new", "inplace"):
+            r = S.policy_loss(x.clone(), label, old, adv, one, ref=ref, kl=0.5, dlogits=where)
+            d = r["dlogits"].float()
+            assert not bool(torch.isnan(d).any())
+            assert not d[:, V // 2:].any()
+            at = d.gather(1, label.long()[:, None])[:, 0] * sign
+            unsure = lp > -1e-3  # (a row that is all but sure of its token: nothing is left to move)
+            assert bool((at > (6e4 if kind == "float16" else 1e30))[~unsure].all())
+        still = S.policy_loss(x, label, old, adv, one, ref=ref, kl=0.5, grad_scale=0.0)["dlogits"]
+        assert not still.any()  # (NaN counts as any)
