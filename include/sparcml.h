@@ -643,7 +643,10 @@ SPARCML_API int sparcml_policy_loss(const sparcml_logits* in, const sparcml_poli
  * and the gradient with respect to the logits, scaled by grad_scale.  Rows
  * without a token add nothing, have logp 0 and a zero gradient; an empty
  * sequence has reward 0.  Sums over rows and pairs are taken in fp64 in a
- * fixed order.
+ * fixed order.  Rows that hold nothing but -Inf and tokens whose own logit is
+ * -Inf are taken as by sparcml_policy_loss: no gradient; the first add
+ * nothing, the others make a reward infinite unless ref is -Inf too.  Equal
+ * infinite rewards of a pair are 0 apart.
  *   pairs    1 <= pairs <= 65535.
  *   bounds   HOST array of 2 * pairs + 1: bounds[0] == 0, not decreasing,
  *            bounds[2 * pairs] == rows.

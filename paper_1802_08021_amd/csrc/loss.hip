@@ -604,20 +604,23 @@ struct PairLoss {
 };
 __device__ __forceinline__ PairLoss pair_loss(const PreferenceArgs& a, uint32_t pairs, double good, double bad)
 {
-    good *= (double)a.beta;
-    bad *= (double)a.beta;
-    const double h = good - bad, z = exp(-fabs(h)), soft = log1p(z);
+    good = times((double)a.beta, good);
+    bad = times((double)a.beta, bad);
+    const double h = apart(good, bad), z = exp(-fabs(h)), soft = log1p(z);
     const double up = h >= 0.0 ? 1.0 / (1.0 + z) : z / (1.0 + z);    // sigmoid(h)
     const double down = h >= 0.0 ? z / (1.0 + z) : 1.0 / (1.0 + z);  // sigmoid(-h)
     const double eps = (double)a.smoothing;
     PairLoss r;
-    r.sums = PairSums{{(1.0 - eps) * (soft - fmin(h, 0.0)) + eps * (soft + fmax(h, 0.0)), h > 0.0 ? 1.0 : 0.0, good, bad}};
+    r.sums = PairSums{{times(1.0 - eps, soft - fmin(h, 0.0)) + times(eps, soft + fmax(h, 0.0)), h > 0.0 ? 1.0 : 0.0, good, bad}};
     r.coef = (float)((double)a.beta * (eps * up - (1.0 - eps) * down) / (double)pairs);
     return r;
 }
-__device__ __forceinline__ double log_ratio(const PreferenceArgs& a, uint64_t t, double lp)
+// A token's log ratio; none in a row that holds nothing but -Inf (p: the row's
+// part, looked at where lp is -Inf).
+__device__ __forceinline__ double log_ratio(const PreferenceArgs& a, uint64_t t, double lp, const Part& p)
 {
-    return lp - (a.ref_logp ? (double)a.ref_logp[t] : 0.0);
+    if (lp == -INFINITY && p.sum == 0.0f) return 0.0;
+    return apart(lp, a.ref_logp ? (double)a.ref_logp[t] : 0.0);
 }
 
 constexpr uint32_t kFewPairs = 32;
@@ -637,18 +640,18 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
     const uint32_t lo = many ? many[2 * b] : few.words[2 * b], mid = many ? many[2 * b + 1] : few.words[2 * b + 1];
     const uint32_t end = many ? many[2 * b + 2] : few.words[2 * b + 2];
     double x[2] = {0.0, 0.0};
-    auto add = [&](uint64_t t, bool use, double lp, Part) {
+    auto add = [&](uint64_t t, bool use, double lp, const Part& p) {
         if (S > 1) logp[t] = (float)lp;
-        if (use) x[t < mid ? 0 : 1] += log_ratio(a, t, lp);
+        if (use) x[t < mid ? 0 : 1] += log_ratio(a, t, lp, p);
     };
     if (S > 1)
         each_joined(in, nullptr, lo, end, S, g, c, part, at_label, add);
     else
-        for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256) add(t, has_token(in, t), logp[t], Part{});
+        for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256) add(t, has_token(in, t), logp[t], part[t]);
     block_sum(x, s_w, 2);
     const PairLoss r = pair_loss(a, pairs, x[0], x[1]);
     for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256)
-        coef[t] = has_token(in, t) ? (t < mid ? r.coef : -r.coef) : 0.0f;
+        coef[t] = has_token(in, t) && logp[t] != -INFINITY ? (t < mid ? r.coef : -r.coef) : 0.0f;
     if (threadIdx.x == 0) sums[b] = r.sums;
 }
 
@@ -709,7 +712,7 @@ __global__ void __launch_bounds__(256) k_few_pairs(Logits in, PreferenceArgs a, 
     if (blockIdx.x == 0) {
         // a thread a sequence, from ratios that all threads have fetched
         for (uint32_t t = threadIdx.x; t < (uint32_t)in.rows; t += 256)
-            s_ratio[t] = has_token(in, t) ? log_ratio(a, t, (double)logp[t]) : 0.0;
+            s_ratio[t] = has_token(in, t) ? log_ratio(a, t, (double)logp[t], part[t]) : 0.0;
         __syncthreads();
         if (threadIdx.x < 2 * pairs) {
             double sum = 0.0;
@@ -735,10 +738,10 @@ __global__ void __launch_bounds__(256) k_few_pairs(Logits in, PreferenceArgs a, 
         p = part[t];
         double x[2] = {0.0, 0.0};
         for (uint32_t u = lo + threadIdx.x; u < end; u += 256)
-            if (has_token(in, u)) x[u < mid ? 0 : 1] += log_ratio(a, u, (double)logp[u]);
+            if (has_token(in, u)) x[u < mid ? 0 : 1] += log_ratio(a, u, (double)logp[u], part[u]);
         block_sum(x, s_w, 2);
         const float d = pair_loss(a, pairs, x[0], x[1]).coef;
-        q = a.grad_scale * in.scale * (t < mid ? d : -d);
+        q = logp[t] == -INFINITY ? 0.0f : a.grad_scale * in.scale * (t < mid ? d : -d);
     }
     slice.write(static_cast<E*>(dlogits) + t * ldd, (uint32_t)in.label[t], q, p, c);
 }

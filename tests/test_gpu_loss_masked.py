@@ -134,3 +134,73 @@ def test_coefficients_beyond_fp32(T, V, kind):
             assert bool((at > (6e4 if kind == "float16" else 1e30))[~unsure].all())
         still = S.policy_loss(x, label, old, adv, one, ref=ref, kl=0.5, grad_scale=0.0)["dlogits"]
         assert not still.any()  # (NaN counts as any)
+
+
+@pytest.mark.parametrize("T,V,kind,pairs", [(12, 500, "float32", 4), (12, 500, "bfloat16", 4), (300, 513, "float16", 5),
+                                            (300, 513, "float32", 40), (16, 40000, "float32", 4),
+                                            (96, 40000, "bfloat16", 40), (600, 20000, "float32", 6)])
+@pytest.mark.parametrize("source", ["same", "finite", "none"])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_preference_loss(T, V, kind, pairs, source, smoothing):
+    """An empty row in pair 0's preferred sequence; a masked token in pair 1's
+    other one, in pair 2's preferred one, and in both of pair 3."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    say(f"[masked preference] {T} {V} {kind} {pairs} {source} {smoothing}")
+    x, label, gen = make(T, V, kind, T + V + pairs, pad=3)
+    bounds = [0, 2, 4, 5, 7, 9, 10, 11, 12]
+    if pairs > 4:  # the rest in ragged pieces, empty ones among them
+        rng = np.random.default_rng(pairs)
+        bounds += sorted(rng.integers(12, T + 1, 2 * (pairs - 4) - 1).tolist()) + [T]
+    bounds[-1] = T
+    assert len(bounds) == 2 * pairs + 1
+    x[0] = float("-inf")
+    for t in (6, 8, 10, 11):
+        label[t] = 1
+        x[t, 1] = float("-inf")
+    label[3] = 2
+    x[3, V // 2:] = float("-inf")
+    lp, _ = S.token_logprob(x, label)
+    gone = [0, 6, 8, 10, 11]
+    assert torch.isinf(lp).nonzero()[:, 0].tolist() == gone
+    ref = lp + torch.randn(T, device=dev, generator=gen) * 0.5
+    if source == "finite":
+        ref[gone] = -2.0
+    h, l = x.double().cpu().numpy(), label.cpu().numpy()
+    p, soft, empty = log_probs(h, l, 1.0)
+    n = np.zeros(T) if source == "none" else to_np(ref).astype(np.float64)
+    beta, eps = float(np.float32(0.1)), float(np.float32(smoothing))
+    ratio = np.where(empty, 0.0, apart(p, n))
+    coef, out = np.zeros(T), np.zeros(4)
+    times = lambda a, b: 0.0 if a == 0 else a * b  # noqa: E731
+    for b in range(pairs):
+        lo, mid, end = bounds[2 * b:2 * b + 3]
+        good, bad = beta * ratio[lo:mid].sum(), beta * ratio[mid:end].sum()
+        d = float(apart(np.float64(good), np.float64(bad)))
+        out += np.array([times(1 - eps, np.logaddexp(0, -d)) + times(eps, np.logaddexp(0, d)), d > 0, good, bad]) / pairs
+        with np.errstate(over="ignore"):
+            q = beta * (eps / (1 + np.exp(-d)) - (1 - eps) / (1 + np.exp(d))) / pairs
+        coef[lo:mid], coef[mid:end] = q, -q
+    coef[gone] = 0.0
+    if source == "none":
+        assert np.isinf(out[3]) and np.isinf(out[2])
+    fine = np.isfinite(p)
+    err = np.zeros(T)
+    err[fine] = lp_bound(h[fine], l[fine], 1.0, V)
+    worst = max(np.sum(err[bounds[2 * b]:bounds[2 * b + 2]]) for b in range(pairs)) * beta
+    rel = worst * beta / pairs / 4 / np.maximum(np.abs(coef), 1e-30) if smoothing else worst
+    rel = np.where(coef != 0, rel, 0) + 8 * U
+    for where in ("new", None, "inplace"):
+        r = S.preference_loss(x, label, bounds, ref=None if source == "none" else ref, beta=0.1, smoothing=smoothing,
+                              dlogits=where)
+        got = to_np(r["stats"]).astype(np.float64)
+        on = np.isfinite(out)
+        assert np.all(got[~on] == out[~on]), (got, out)
+        lim = worst + 2 * U * np.abs(out) + 1e-7 + np.array([0, 1e-6, 0, 0])
+        assert np.all(np.abs(got[on] - out[on]) <= lim[on]), (got, out, lim)
+        logp = to_np(r["logp"])
+        assert np.all(logp[gone] == -INF) and np.all(np.abs(logp[fine] - p[fine]) <= err[fine])
+        if where:
+            d = r["dlogits"].double().cpu().numpy()
+            assert not d[gone].any() and not d[3, V // 2:].any()
+            check_gradient(d[fine], gradient(soft, l, coef, 1.0)[fine], np.abs(coef)[fine], h[fine], 1.0, V, kind, rel[fine])
