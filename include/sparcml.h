@@ -136,7 +136,8 @@ typedef struct sparcml_stream {
  *            input stream nnz; LOGPROB, POLICY, PREFERENCE: vocabulary;
  *            DENSIFY, QUANTIZE_BUCKETED, CONCAT, VALIDATE, TENSORS: ignored.
  *   delta    REDUCE only (switch threshold as a fraction of N).
- * A workspace sized with max_nnz >= the actual largest nnz is sufficient.
+ * A workspace sized with max_nnz >= the actual largest nnz is sufficient;
+ * LOGPROB, POLICY, PREFERENCE: with P, N and max_nnz of at least the call's.
  * Returns SPARCML_OK and *bytes, or SPARCML_EINVAL.
  */
 SPARCML_API int sparcml_workspace_size(int op, int P, uint64_t N, uint64_t max_nnz, double delta,

@@ -770,6 +770,11 @@ constexpr uint32_t kMaxGrid = 1u << 22;
 constexpr uint32_t kHold = 8;     // pieces a thread of k_row holds in registers,
 constexpr uint32_t kHoldLds = 4;  // and one of 1024 in LDS (64 KB: two workgroups a CU)
 
+constexpr uint64_t kMaxSlices = 1024;  // of few rows together
+
+// Slices of a row at most.
+uint64_t most_slices(uint64_t pieces) { return std::min<uint64_t>(64, (pieces + 511) / 512); }
+
 Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
 {
     Cut r;
@@ -777,8 +782,8 @@ Cut cut_rows(uint64_t rows, uint64_t vocab, uint32_t type)
     r.G = (uint32_t)((r.pieces + 256 * kGradU - 1) / (256 * kGradU));
     r.many = rows >= kManyRows;
     r.row = r.pieces <= 512 * kHold;
-    const uint64_t most = std::min<uint64_t>(64, (r.pieces + 511) / 512), want = 1024 / std::min<uint64_t>(rows, 1024);
-    const uint64_t S = r.row ? 1 : std::max<uint64_t>(1, std::min(most, want));
+    const uint64_t want = kMaxSlices / std::min(rows, kMaxSlices);
+    const uint64_t S = r.row ? 1 : std::max<uint64_t>(1, std::min(most_slices(r.pieces), want));
     r.W = (uint32_t)((r.pieces + S - 1) / S);
     r.S = (uint32_t)((r.pieces + r.W - 1) / r.W);
     for (r.g = 1; r.g < r.S;) r.g *= 2;
@@ -793,30 +798,30 @@ struct Space {
     PairSums* sums;
     uint32_t* bounds;
 };
-Space carve(void* ws, uint64_t rows, uint32_t S, uint32_t pairs, size_t* bytes)
+enum class Use { logprob, policy, preference };
+Space carve(void* ws, Use use, uint64_t rows, uint64_t parts, uint32_t pairs, size_t* bytes)
 {
     Carve c(ws);
     Space r;
-    r.part = c.take<Part>(rows * S);
-    r.terms = c.take<PolicyTerms>(pairs ? 0 : rows);
+    r.part = c.take<Part>(parts);
+    r.terms = c.take<PolicyTerms>(use == Use::policy ? rows : 0);
     r.ticket = c.take<uint32_t>(1);
     r.at_label = c.take<float>(rows);
-    r.coef = c.take<float>(pairs ? rows : 0);
+    r.coef = c.take<float>(use == Use::preference ? rows : 0);
     r.sums = c.take<PairSums>(pairs);
     r.bounds = c.take<uint32_t>(pairs ? 2 * (uint64_t)pairs + 1 : 0);
     if (bytes) *bytes = c.used;
     return r;
 }
-// Enough for every element type.
-size_t workspace(uint32_t pairs, uint64_t rows, uint64_t vocab)
+// Enough for every element type (fp32 has the most pieces) and for every call
+// of fewer rows or a smaller vocabulary: rows * S falls where S does, so the
+// parts are counted by what bounds it, which does not.
+size_t workspace(Use use, uint32_t pairs, uint64_t rows, uint64_t vocab)
 {
-    size_t most = 0;
-    for (uint32_t type : {(uint32_t)kF32, (uint32_t)kBf16}) {
-        size_t b = 0;
-        carve(nullptr, rows, cut_rows(rows, vocab, type).S, pairs, &b);
-        most = std::max(most, b);
-    }
-    return most;
+    const uint64_t pieces = cut_rows(rows, vocab, kF32).pieces;
+    size_t b = 0;
+    carve(nullptr, use, rows, std::max(rows, std::min(kMaxSlices, rows * most_slices(pieces))), pairs, &b);
+    return b;
 }
 
 template <class F>
@@ -900,14 +905,17 @@ hipError_t rows_run(const Cut& cut, const Logits& in, const PolicyArgs* policy, 
 
 }  // namespace
 
-size_t logprob_workspace(uint64_t rows, uint64_t vocab) { return workspace(0, rows, vocab); }
-size_t policy_workspace(uint64_t rows, uint64_t vocab) { return workspace(0, rows, vocab); }
-size_t preference_workspace(uint32_t pairs, uint64_t rows, uint64_t vocab) { return workspace(pairs, rows, vocab); }
+size_t logprob_workspace(uint64_t rows, uint64_t vocab) { return workspace(Use::logprob, 0, rows, vocab); }
+size_t policy_workspace(uint64_t rows, uint64_t vocab) { return workspace(Use::policy, 0, rows, vocab); }
+size_t preference_workspace(uint32_t pairs, uint64_t rows, uint64_t vocab)
+{
+    return workspace(Use::preference, pairs, rows, vocab);
+}
 
 hipError_t logprob_run(const Logits& in, float* logp, float* lse, void* ws, hipStream_t s)
 {
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
-    const Space sp = carve(ws, in.rows, cut.S, 0, nullptr);
+    const Space sp = carve(ws, Use::logprob, in.rows, in.rows * cut.S, 0, nullptr);
     hipError_t e = rows_run<false>(cut, in, nullptr, sp, logp, lse, s);
     if (e != hipSuccess || cut.S == 1) return e;
     const uint32_t grid = (uint32_t)((in.rows * cut.g + 255) / 256);
@@ -920,7 +928,7 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
                       void* ws, hipStream_t s)
 {
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
-    const Space sp = carve(ws, in.rows, cut.S, 0, nullptr);
+    const Space sp = carve(ws, Use::policy, in.rows, in.rows * cut.S, 0, nullptr);
     const float c = in.scale * kLog2e;
     const bool fused = dlogits && cut.many;
     if (fused) {
@@ -956,7 +964,7 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
                           float* logp, float* stats, void* dlogits, uint64_t ldd, void* ws, hipStream_t s)
 {
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
-    const Space sp = carve(ws, in.rows, cut.S, pairs, nullptr);
+    const Space sp = carve(ws, Use::preference, in.rows, in.rows * cut.S, pairs, nullptr);
     const float c = in.scale * kLog2e;
     // logits that fit the 256 MB cache are found there by the gradient pass (1000
     // rows of 131072 bf16: 132 -> 127 us; of 4000: 498 -> 522, so not those)
