@@ -9,10 +9,10 @@ Index tensors are int32 holding the uint32 bit patterns of the ABI.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
-
-import numpy as np
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_lib", "libsparcml.so")
@@ -45,9 +45,9 @@ class Tensor(ctypes.Structure):
     ]
 
 
-# The same for an array of them, to be filled by columns.
-_TENSOR_RECORD = np.dtype([(name, np.uint64) for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy", "n")]
-                          + [("decay", np.float32), ("lr_scale", np.float32)])
+# The same as bytes, for an array of them from their columns.
+_TENSOR_COLUMNS = ("param", "grad", "m", "v", "m_scale", "v_scale", "copy", "n", "decay", "lr_scale")
+_pack_tensor = struct.Struct("8Q2f").pack
 
 
 class Tensors(ctypes.Structure):
@@ -743,13 +743,13 @@ class _TensorPlan:
                                     f"{grads[0].dtype} gradients"), "n": sizes}
         if columns:
             fields.update(columns(sizes, grads[0].get_device()))
-        # filled by columns: setting fields one by one takes a microsecond a tensor
-        arr = np.zeros(len(grads), dtype=_TENSOR_RECORD)
-        for name, column in fields.items():
-            arr[name] = column
+        # packed from columns: setting fields one by one takes a microsecond a tensor
+        none = [0] * len(grads)
+        rates = (array.array("f", fields.pop(name, none)) for name in _TENSOR_COLUMNS[8:])
+        arr = ctypes.c_char_p(b"".join(map(_pack_tensor, *(fields.get(name, none) for name in _TENSOR_COLUMNS[:8]), *rates)))
         self.plan = Tensors()
         self.ws = alloc_workspace(workspace_size(OP_TENSORS, len(grads), sum(sizes), 0), self.dev)
-        _check(lib().sparcml_tensors_prepare(len(grads), arr.ctypes.data_as(ctypes.POINTER(Tensor)), gtype, copy_type,
+        _check(lib().sparcml_tensors_prepare(len(grads), ctypes.cast(arr, ctypes.POINTER(Tensor)), gtype, copy_type,
                                              state_bits, ctypes.byref(self.plan), _ptr(self.ws), self.ws.numel(),
                                              _stream_ptr(self.dev)), "sparcml_tensors_prepare")
         self.out = torch.empty(2, dtype=torch.float32, device=self.dev)
