@@ -690,7 +690,8 @@ SPARCML_API int sparcml_preference_loss(const sparcml_logits* in, int pairs, con
 #define SPARCML_TIMER_GRAD_NORM 11    /* gradient norm */
 #define SPARCML_TIMER_ADAMW 12        /* AdamW step */
 #define SPARCML_TIMER_LOSS_ROWS 13    /* losses: the pass over the logits' rows */
-#define SPARCML_TIMER_LOSS_GRAD 14    /* losses: the gradient pass, where it is one of its own */
+#define SPARCML_TIMER_LOSS_GRAD 14    /* losses: what follows it (joined slices, sums over tokens and pairs, the
+                                         gradient where it is a pass of its own) */
 SPARCML_API int sparcml_timing_enable(int on);
 SPARCML_API int sparcml_timing_read(int group, float* ms);
 

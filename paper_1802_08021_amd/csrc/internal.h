@@ -54,7 +54,7 @@ enum TimerSlot {
     kTGradNorm = 11,    // gradient norm
     kTAdamw = 12,       // AdamW step
     kTLossRows = 13,    // losses: the pass over the logits' rows
-    kTLossGrad = 14,    // losses: the gradient pass
+    kTLossGrad = 14,    // losses: what follows it (sums, the gradient pass)
     kTSlots = 15
 };
 void timer_begin(int slot, hipStream_t s);

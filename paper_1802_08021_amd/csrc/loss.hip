@@ -919,8 +919,10 @@ hipError_t logprob_run(const Logits& in, float* logp, float* lse, void* ws, hipS
     hipError_t e = rows_run<false>(cut, in, nullptr, sp, logp, lse, s);
     if (e != hipSuccess || cut.S == 1) return e;
     const uint32_t grid = (uint32_t)((in.rows * cut.g + 255) / 256);
+    timer_begin(kTLossGrad, s);
     hipLaunchKernelGGL(k_join, dim3(grid), dim3(256), 0, s, in, (const float*)nullptr, cut.S, cut.g,
                        in.scale * kLog2e, sp.part, sp.at_label, logp, lse);
+    timer_end(kTLossGrad, s);
     return hipGetLastError();
 }
 
@@ -940,7 +942,9 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
         if (e != hipSuccess) return e;
     }
     if (fused || (!dlogits && cut.S == 1)) {
+        timer_begin(kTLossGrad, s);
         hipLaunchKernelGGL(k_policy_stats, dim3(1), dim3(1024), 0, s, in.rows, a, sp.terms, stats);
+        timer_end(kTLossGrad, s);
         return hipGetLastError();
     }
     const uint32_t G = dlogits ? cut.G : 1;
@@ -992,9 +996,9 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
         if (e != hipSuccess) return e;
         many = sp.bounds;
     }
+    timer_begin(kTLossGrad, s);
     hipLaunchKernelGGL(k_pairs, dim3(pairs), dim3(256), 0, s, in, a, pairs, few, many, cut.S, cut.g, c, sp.part,
                        sp.at_label, logp, sp.coef, sp.sums);
-    timer_begin(kTLossGrad, s);
     by_type(in.type, [&](auto ty) {
         hipLaunchKernelGGL((k_grad<decltype(ty)::value, false>), dim3(grid), dim3(256), 0, s, in, PolicyArgs{},
                            (const PolicyTerms*)nullptr, pairs, sp.coef, sp.sums, a.grad_scale * in.scale, cut.S, cut.g,
