@@ -183,17 +183,18 @@ struct PolicyTerms {
 };
 __device__ __forceinline__ PolicyTerms policy_terms(const PolicyArgs& a, const PolicyRow& q, const Part& p, double lp)
 {
-    PolicyTerms r = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (p.sum == 0.0f) return r;
+    PolicyTerms r;
+    const bool none = p.sum == 0.0f;
     const float rho = exp2_fast((float)(apart(lp, (double)q.old) * 1.44269504088896341));
     const float u = times(q.adv, rho), held = times(q.adv, fminf(fmaxf(rho, a.lo), a.hi));
     const bool clipped = u > held;
-    r.gain = q.w * (clipped ? held : u);  // (a NaN of u comes through)
-    r.clipped = clipped ? q.w : 0.0f;
+    r.gain = none ? 0.0f : q.w * (clipped ? held : u);  // (a NaN of u comes through)
+    r.clipped = clipped && !none ? q.w : 0.0f;
+    r.k = 0.0f;
     r.coef = clipped ? 0.0f : -u;
     if (a.ref_logp) {
         const float far = (float)apart((double)q.ref, lp), em = expm1f(far);
-        r.k = q.w * (far == INFINITY ? far : em - far);
+        r.k = none ? 0.0f : q.w * (far == INFINITY ? far : em - far);
         r.coef = r.coef - times(a.kl, em);
     }
     r.coef = lp == -INFINITY ? 0.0f : within(q.w * r.coef);
@@ -615,12 +616,12 @@ __device__ __forceinline__ PairLoss pair_loss(const PreferenceArgs& a, uint32_t 
     r.coef = (float)((double)a.beta * (eps * up - (1.0 - eps) * down) / (double)pairs);
     return r;
 }
-// A token's log ratio; none in a row that holds nothing but -Inf (p: the row's
-// part, looked at where lp is -Inf).
-__device__ __forceinline__ double log_ratio(const PreferenceArgs& a, uint64_t t, double lp, const Part& p)
+// A token's log ratio; none in a row that holds nothing but -Inf.  (Without a
+// branch, so that the loads are under way together.)
+__device__ __forceinline__ double log_ratio(const PreferenceArgs& a, uint64_t t, double lp, Part p)
 {
-    if (lp == -INFINITY && p.sum == 0.0f) return 0.0;
-    return apart(lp, a.ref_logp ? (double)a.ref_logp[t] : 0.0);
+    const double x = apart(lp, a.ref_logp ? (double)a.ref_logp[t] : 0.0);
+    return p.sum == 0.0f ? 0.0 : x;
 }
 
 constexpr uint32_t kFewPairs = 32;
@@ -640,7 +641,7 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
     const uint32_t lo = many ? many[2 * b] : few.words[2 * b], mid = many ? many[2 * b + 1] : few.words[2 * b + 1];
     const uint32_t end = many ? many[2 * b + 2] : few.words[2 * b + 2];
     double x[2] = {0.0, 0.0};
-    auto add = [&](uint64_t t, bool use, double lp, const Part& p) {
+    auto add = [&](uint64_t t, bool use, double lp, Part p) {
         if (S > 1) logp[t] = (float)lp;
         if (use) x[t < mid ? 0 : 1] += log_ratio(a, t, lp, p);
     };
@@ -650,8 +651,11 @@ __global__ void __launch_bounds__(256) k_pairs(Logits in, PreferenceArgs a, uint
         for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256) add(t, has_token(in, t), logp[t], part[t]);
     block_sum(x, s_w, 2);
     const PairLoss r = pair_loss(a, pairs, x[0], x[1]);
-    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256)
-        coef[t] = has_token(in, t) && logp[t] != -INFINITY ? (t < mid ? r.coef : -r.coef) : 0.0f;
+    for (uint64_t t = (uint64_t)lo + threadIdx.x; t < end; t += 256) {
+        // (a token whose own logit is -Inf: its log probability does not move)
+        const float at = at_label[t];
+        coef[t] = has_token(in, t) && at != -INFINITY ? (t < mid ? r.coef : -r.coef) : 0.0f;
+    }
     if (threadIdx.x == 0) sums[b] = r.sums;
 }
 
@@ -704,8 +708,8 @@ __global__ void __launch_bounds__(256) k_grad(Logits in, PolicyArgs a, const Pol
 constexpr uint32_t kPairRows = 256;
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_few_pairs(Logits in, PreferenceArgs a, uint32_t pairs, FewBounds bounds,
-                                                   uint32_t G, float c, const Part* part, const float* logp,
-                                                   float* stats, void* dlogits, uint64_t ldd)
+                                                   uint32_t G, float c, const Part* part, const float* at_label,
+                                                   const float* logp, float* stats, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     __shared__ double s_w[4][4], s_ratio[kPairRows], s_seq[2 * kFewPairs];
@@ -741,7 +745,7 @@ __global__ void __launch_bounds__(256) k_few_pairs(Logits in, PreferenceArgs a, 
             if (has_token(in, u)) x[u < mid ? 0 : 1] += log_ratio(a, u, (double)logp[u], part[u]);
         block_sum(x, s_w, 2);
         const float d = pair_loss(a, pairs, x[0], x[1]).coef;
-        q = logp[t] == -INFINITY ? 0.0f : a.grad_scale * in.scale * (t < mid ? d : -d);
+        q = at_label[t] == -INFINITY ? 0.0f : a.grad_scale * in.scale * (t < mid ? d : -d);
     }
     slice.write(static_cast<E*>(dlogits) + t * ldd, (uint32_t)in.label[t], q, p, c);
 }
@@ -986,7 +990,7 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
             timer_begin(kTLossGrad, s);
             by_type(in.type, [&](auto ty) {
                 hipLaunchKernelGGL((k_few_pairs<decltype(ty)::value>), dim3(grid), dim3(256), 0, s, in, a, pairs, few,
-                                   cut.G, c, sp.part, logp, stats, dlogits, ldd);
+                                   cut.G, c, sp.part, sp.at_label, logp, stats, dlogits, ldd);
             });
             timer_end(kTLossGrad, s);
             return hipGetLastError();
