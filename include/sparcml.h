@@ -622,7 +622,8 @@ SPARCML_API int sparcml_token_logprob(const sparcml_logits* in, float* logp, flo
  *   dlogits  NULL (forward only), or device, of in->type, element (t, v) at
  *            dlogits[t * ld_d + v]; every v < vocab of every row is
  *            written.  May be in->x itself (ld_d == in->ld), else it must
- *            not overlap it.
+ *            not overlap it (from the first row's start to the last one's
+ *            end: rows between the other's rows are refused).
  *   ws       sparcml_workspace_size(SPARCML_OP_POLICY, 1, rows, vocab, ...)
  * Does not synchronize.  Errors: EINVAL, EWORKSPACE, EHIP.
  */

@@ -233,7 +233,9 @@ __device__ __forceinline__ void put_policy_stats(const PolicyArgs& a, double* x,
     }
 }
 
-// The sums over tokens of their terms (eight rows a thread in flight).
+// The sums over tokens of their terms (eight rows a thread in flight).  8192
+// rows: 6.4 us after a pass over short rows, 8.7 after one over 2 GB, when the
+// terms come from HBM.
 __global__ void __launch_bounds__(1024) k_policy_stats(uint64_t rows, PolicyArgs a, const PolicyTerms* terms,
                                                        float* stats)
 {
@@ -294,17 +296,17 @@ struct Own {
 
 // Row blockIdx.x by one workgroup: the first NV pieces of a thread stay in
 // registers between the two passes over them, LP more in LDS, the rest of a
-// longer row is read once more (GRAD; from the 256 MB cache: marked nontemporal,
-// it costs 960 us instead of 804 below), the singles one a thread.  Writes the log
-// probability, lse and part where wanted, and with GRAD the gradient of the
-// policy loss.
+// longer row is read once more (GRAD; from the 256 MB cache, so its first read
+// is not marked nontemporal: 8192 x 131072 bf16 871 us with the mark, 770
+// without), the singles one a thread.  Writes the log probability, lse and
+// part where wanted, and with GRAD the gradient of the policy loss.
 // At 64 registers a thread two workgroups of 1024 share a CU, and one's loads
 // and stores go on under the other's exponentials: 8192 x 131072 bf16 770 us, 5.6
-// TB/s of logits and gradient (two passes by slices 1207; rows of 131072 wholly
-// in registers, one workgroup a CU, 857; nothing in LDS 799; 1024 rows 103, with
-// nothing in LDS 114).  Without its exponentials it takes 800 of 804: what
-// bounds it is memory, at the rate that rows of 256 KB a workgroup are copied
-// (5.5 to 6.0 TB/s).
+// TB/s of logits and gradient (two passes by slices 996; nothing in LDS 790;
+// rows of 131072 wholly in registers, one workgroup a CU, 857), 1024 rows 108
+// (131, 114), of fp32 222, 4.8 TB/s (250, 228).  Without its exponentials it
+// takes as long: what bounds it is memory, at the rate that rows of 256 KB a
+// workgroup are copied (5.5 to 6.0 TB/s).
 template <int TYPE, int THREADS, int NV, int LP, bool GRAD, bool KEEP>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
 k_row(Logits in, PolicyArgs a, float c, float* logp, float* lse, Part* part, float* at_label, uint32_t* ticket,
@@ -668,8 +670,9 @@ __device__ __forceinline__ void put_pair_stats(double* x, double (*s_w)[4], uint
 
 // The gradient by slices from coefficients that are there: of a policy loss
 // whose rows are one slice each (its terms), or of pairs (coef).  Workgroup 0:
-// the sums over tokens or pairs.  Bound by HBM: 8192 x 131072 bf16 690 us, 6.2
-// TB/s, with 2 pieces a thread (896 with one, 709 with four).
+// the sums over tokens or pairs.  Bound by HBM: 8192 x 131072 bf16 680 us of
+// a policy loss, 750 of pairs, 5.7 to 6.3 TB/s, with 2 pieces a thread (with one
+// 896, with four 709 where two took 690).
 template <int TYPE, bool POLICY>
 __global__ void __launch_bounds__(256) k_grad(Logits in, PolicyArgs a, const PolicyTerms* terms, uint32_t pairs,
                                               const float* coef, const PairSums* sums, float factor, uint32_t S,
@@ -703,8 +706,11 @@ __global__ void __launch_bounds__(256) k_grad(Logits in, PolicyArgs a, const Pol
 
 // The gradient of a preference loss of few pairs and rows without a launch for
 // the pairs: every workgroup sums its own row's pair (the logits are under way
-// meanwhile), workgroup 0 all of them.  Up to 256 rows: 64 x 8000 bf16 9.1 us
-// against 12.3 with that launch, 256 x 32000 16.6 / 18.1, 400 x 8000 16.8 / 13.8.
+// meanwhile), workgroup 0 all of them.  Up to 256 rows (us, bf16, without / with
+// that launch): one pair of 64 x 8000 9.3 / 12.7, 128 x 1000 9.5 / 12.4, 256 x
+// 1000 11.9 / 12.8, 256 x 32000 17.6 / 17.2, 512 x 1000 17.9 / 12.9, 512 x 32000
+// 27.5 / 25.4; eight pairs of 256 x 8000 10.4 / 12.8, 512 x 8000 12.9 / 14.1, 512 x
+// 32000 25.5 / 24.3 (the rows of a pair count, but the crossing is near 256).
 constexpr uint32_t kPairRows = 256;
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_few_pairs(Logits in, PreferenceArgs a, uint32_t pairs, FewBounds bounds,
@@ -755,12 +761,18 @@ __global__ void __launch_bounds__(256) k_few_pairs(Logits in, PreferenceArgs a, 
 // How a call's rows are taken.  `row`: log probabilities by a workgroup a
 // row (k_row), else by S slices of W pieces (k_slices), joined by groups of g
 // lanes; `many`: a policy loss and its gradient by a workgroup a row; G: slices
-// of a gradient pass.  The rules follow from (us, bf16, rows x vocabulary):
+// of a gradient pass.  The rules follow from (us, bf16 unless it says fp32, rows
+// x vocabulary):
 //   row, rows of up to 4096 pieces (32768 16-bit logits): 8 x 32000 5.2 against
 //     6.1 by slices, 256 x 32000 6.4 / 8.3, 1000 x 32000 14.5 / 14.5; beyond,
 //     slices: 8 x 65000 7.3 / 6.1, 1000 x 65000 28.3 / 24.1
-//   many, from 128 rows on: 256 x 32000 13.3 against 18.6 in two passes, 256 x
-//     131072 34 / 46; 128 x 131072 26 / 28; 64 x 131072 25 / 18
+//   many, from 128 rows on (one pass / two, inputs out of cache):
+//      64 x 32000 12.6 / 10.2, fp32 15.9 / 13.3; 64 x 131072 26 / 20, fp32 37 / 27
+//     128 x 32000 12.9 / 12.5, fp32 16.8 / 18.3; 128 x 131072 28 / 29, fp32 42 / 45
+//     256 x 32000 14.1 / 16.0, fp32 21 / 30; 256 x 131072 35 / 48, fp32 63 / 81
+//     512 x 32000 18 / 24, fp32 29 / 50; 512 x 131072 58 / 86, fp32 109 / 151
+//     (shorter rows are launches: 128 x 1000 8.5 / 8.3, 256 x 8000 10.5 / 8.8, 512
+//     x 1000 9.2 / 8.3, 512 x 8000 12.3 / 12.0, fp32 12.6 / 14.8)
 //   slices of few rows: about 1024 workgroups together (300 x 131072 19 with as
 //     many, 23 with four times as many), none of less than 512 pieces
 struct Cut {
@@ -839,8 +851,8 @@ void by_type(uint32_t type, F f)
         f(std::integral_constant<int, kF16>());
 }
 
-// Of 1024 threads only where rows are longer than those can hold (8192 x 50000
-// bf16: 302 us with 1024, 279 with 512).
+// Of 512 threads up to twice the pieces that they hold (8192 x 50000 bf16: 280
+// us, 302 with 1024), of 1024 beyond.
 template <bool GRAD, bool KEEP>
 void launch_row(const Cut& cut, Logits in, PolicyArgs a, float* logp, float* lse, const Space& sp, PolicyTerms* terms,
                 void* dlogits, uint64_t ldd, hipStream_t s)
@@ -975,7 +987,7 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
     const Space sp = carve(ws, Use::preference, in.rows, in.rows * cut.S, pairs, nullptr);
     const float c = in.scale * kLog2e;
     // logits that fit the 256 MB cache are found there by the gradient pass (1000
-    // rows of 131072 bf16: 132 -> 127 us; of 4000: 498 -> 522, so not those)
+    // rows of 131072 bf16: 132 -> 127 us; 4000 rows: 498 -> 522, so not those)
     const bool fits = in.rows * in.ld * (in.type == kF32 ? 4 : 2) <= (256u << 20);
     hipError_t e = dlogits && fits ? rows_run<true>(cut, in, nullptr, sp, logp, nullptr, s)
                                    : rows_run<false>(cut, in, nullptr, sp, logp, nullptr, s);

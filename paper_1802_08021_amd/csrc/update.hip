@@ -7,7 +7,7 @@
 // launch covers them all.  Both are bound by HBM: accesses are 16 bytes a lane (8 for
 // 16-bit types of the step), marked nontemporal, and a piece of 32-bit moments
 // begins at a line of its tensor (2^27 weights in 290 packed tensors: 725 us
-// with pieces from the tensors' first elements, 655 so).
+// with pieces from the tensors' first elements, 655 to 667 so).
 #include "internal.h"
 #include "philox_device.h"
 #include "types_device.h"
@@ -135,10 +135,10 @@ __device__ __forceinline__ uint32_t block_exponent(f32x4 x)
 // second one moves by 1 - beta2 of itself a step, far less than half a code, and
 // rounding to nearest would hold it still.
 // Bytes an element: 28 (32-bit moments, fp32 gradient) or 16 and 16/256 (8-bit).
-// 20 M weights in 148 tensors, 32-bit: 91 us, 6.1 TB/s; 2^27 in 290, 8-bit: 385 us,
-// 5.6 TB/s (a large copy: 6.2).  One vector a lane is the right size: with 4
-// vectors 838 and 482 us instead of 725 and 387 (more in flight, in less even
-// order).  Without the generator, or with approximate roots and quotients, the
+// 20 M weights in 148 tensors, 32-bit: 91 to 95 us, 5.9 to 6.2 TB/s; 2^27 in 290, 8-bit:
+// 387 to 395 us, 5.5 TB/s (a large copy: 6.2).  One vector a lane is the right size: with
+// 4 vectors, before pieces began at lines, 2^27 took 838 us in 32 bits where one took
+// 725, and 482 in 8 bits where one took 387 (more in flight, in less even order).  Without the generator, or with approximate roots and quotients, the
 // 8-bit step is 2 to 3% faster, so neither is what bounds it.
 template <int BITS, int GT, int CT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(8)))
@@ -215,7 +215,7 @@ __device__ __forceinline__ double block_sum(double x, double* s_w)
 
 // Norm of all gradients: workgroup b sums the squares of pieces b, b + G, ...
 // in fp64, the last workgroup to finish the partial sums, in their order (the
-// same bits whichever it is).  2^27 in 290 tensors: fp32 81 us, 6.6 TB/s, bf16 44
+// same bits whichever it is).  2^27 in 290 tensors: fp32 81 us, 6.6 TB/s, bf16 43
 // us (1024 workgroups; 94 and 48 with 2048, whose loads crowd the memory); 20 M
 // bf16 in 148 tensors 10.4 us, where the chain piece, gradient and the last
 // workgroup's sum count.
