@@ -35,6 +35,11 @@
  *   sparcml_policy_loss    -- clipped policy loss with a KL term, and its
  *                             gradient
  *   sparcml_preference_loss -- loss of paired log ratios, and its gradient
+ *   sparcml_token_scores   -- the same with the rows' entropy and their most
+ *                             likely tokens
+ *   sparcml_token_scores_grad -- the gradient of a loss over these
+ *   sparcml_distill_loss   -- divergence from a teacher's listed tokens, and
+ *                             its gradient
  *   sparcml_tensors_prepare -- a model's tensors, laid out once for
  *   sparcml_grad_norm      -- the norm of all gradients, a clipping factor
  *   sparcml_adamw          -- one AdamW step over all tensors, moments in
@@ -95,6 +100,10 @@ extern "C" {
 #define SPARCML_OP_LOGPROB 9
 #define SPARCML_OP_POLICY 10
 #define SPARCML_OP_PREFERENCE 11
+#define SPARCML_OP_SCORES 12
+#define SPARCML_OP_DISTILL 13
+
+#define SPARCML_MAX_TOP 256 /* tokens on a row's list at most */
 
 /* Element types of logits, gradients and weight copies. */
 #define SPARCML_F32 0
@@ -669,6 +678,127 @@ SPARCML_API int sparcml_preference_loss(const sparcml_logits* in, int pairs, con
                             size_t ws_bytes, void* stream);
 
 /*
+ * What rows of logits say.  For a row in use, p = softmax(scale x[t]):
+ *   logp[t]     log p of the row's token (only with labels)
+ *   lse[t]      log sum_v exp(scale x[t][v])
+ *   entropy[t]  -sum_v p_v log p_v
+ *   norm[t]     two numbers that sparcml_token_scores_grad takes: the largest
+ *               logit M, and log sum_v exp(scale (x[t][v] - M))
+ *   top_id[t], top_logp[t]  the `top` most likely tokens, the likeliest first
+ *               (equal logits: the lowest index first), and their log p.
+ *               Tokens of -Inf are on no list: where fewer are left, the other
+ *               entries are -1 and -Inf.
+ * in->label may be NULL: then every row is in use and logp must be NULL.  With
+ * labels, rows without a token are not in use: logp, lse, entropy and norm are
+ * 0 there, the list holds -1 and -Inf.  A row that holds nothing but -Inf has
+ * lse, log probability and norm[t][1] -Inf, norm[t][0] and entropy 0.  NaN or
+ * +Inf among a row's logits makes its numbers NaN; the list then holds the
+ * largest of the logits that are not NaN.
+ * Sums are taken in fp32 over the differences to the maximum, both terms of the
+ * entropy (log of the sum, mean difference) without cancellation.
+ *   logp, lse, entropy  device float[rows] or NULL; norm float[rows][2] or NULL.
+ *   top      0 <= top <= SPARCML_MAX_TOP, top <= vocab; top_id int32[rows][top]
+ *            and top_logp float[rows][top], NULL only where top is 0.
+ *   ws       sparcml_workspace_size(SPARCML_OP_SCORES, top, rows, vocab, ...)
+ * Does not synchronize.  Errors: EINVAL, EWORKSPACE, EHIP.
+ */
+typedef struct sparcml_scores {
+    float* logp;
+    float* lse;
+    float* entropy;
+    float* norm;
+    int32_t* top_id;
+    float* top_logp;
+    uint32_t top;
+    uint32_t reserved; /* 0 */
+} sparcml_scores;
+SPARCML_API int sparcml_token_scores(const sparcml_logits* in, const sparcml_scores* out, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/*
+ * Gradient with respect to the logits of a loss over the scores, from its
+ * derivatives by them.  With (M, l) = norm[t], p_v = exp(scale (x_v - M) - l):
+ *   dlogits[t][v] = scale (d_logp [v == label] + sum_i d_top_i [v == top_id_i]
+ *       + p_v (d_lse - d_logp - sum_i d_top_i - d_entropy (log p_v + entropy)))
+ * Rows that are not in use, rows of nothing but -Inf and rows whose derivatives
+ * are all 0 have a zero gradient and are not read; a token whose own logit is
+ * -Inf has no log probability that moves (its derivative is left out), and no
+ * gradient.  A derivative that is NULL is 0.  Entries of top_id outside
+ * [0, vocab) are none; a token that is there twice counts twice.
+ *   norm, entropy, top_id  as sparcml_token_scores wrote them for these logits
+ *            and this scale (entropy only with d_entropy, top_id with d_top).
+ *   d_logp, d_lse, d_entropy  device float[rows], d_top float[rows][top], or
+ *            NULL; d_logp needs labels.
+ *   dlogits, ld_d   as for sparcml_policy_loss, but not NULL.
+ * No workspace.  Does not synchronize.  Errors: EINVAL, EHIP.
+ */
+typedef struct sparcml_scores_grad {
+    const float* norm;
+    const float* entropy;
+    const int32_t* top_id;
+    const float* d_logp;
+    const float* d_lse;
+    const float* d_entropy;
+    const float* d_top;
+    uint32_t top;
+    uint32_t reserved; /* 0 */
+} sparcml_scores_grad;
+SPARCML_API int sparcml_token_scores_grad(const sparcml_logits* in, const sparcml_scores_grad* args, void* dlogits,
+                              uint64_t ld_d, void* stream);
+
+/*
+ * Distillation: divergence of the rows' distributions p = softmax(scale x[t])
+ * from a teacher's, of which `count` tokens and values a row are known, joined
+ * with the loss of given tokens; and its gradient.  Over the listed tokens i:
+ *   rest == 1: values are log probabilities (as sparcml_token_scores writes
+ *     them), q_i = exp(value_i).  All other tokens together are one more
+ *     outcome, with r = max(1 - sum q_i, 2^-24) and p_r = 1 - sum p_i.
+ *   rest == 0: the list stands for itself, q = softmax(teacher_scale value)
+ *     over it; values are logits, or log probabilities.  beta must be 0.
+ *   beta == 0: div = KL(q || p) = sum q (log q - log p)
+ *   beta == 1: div = KL(p || q)
+ *   between:   div = beta KL(q || m) + (1 - beta) KL(p || m), m = beta q + (1 - beta) p
+ *   loss = sum_t w_t ((1 - hard) div_t - hard log p[label_t])
+ *   dlogits = grad_scale * (its derivative by the logits)
+ * An entry is none where its id is outside [0, vocab), its value is -Inf, or
+ * its token is listed before; a row without entries has div 0.  A row of
+ * weight 0, or (with labels) without a token, is not in use: it is not read,
+ * has div 0 and a zero gradient.  A row that holds nothing but -Inf adds
+ * nothing.  A listed or given token whose own logit is -Inf adds what the
+ * formulas give (+Inf, where q > 0 and beta == 0), but its log probability does
+ * not move: it has no derivative.  Where all tokens that are left to the
+ * student are listed there is no rest, and its term is left out.  Factors
+ * beyond fp32's range are held at its largest number.  What is computed of a
+ * list is in fp64; sums over rows are taken in fp64 in a fixed order.
+ *   id       device int32, entry i of row t at id[t * ld + i]; value the same,
+ *            of `type` (SPARCML_F32 / BF16 / F16).  1 <= count <= SPARCML_MAX_TOP,
+ *            ld >= count.
+ *   weight   device float[rows], or NULL (1 everywhere).
+ *   in->label  may be NULL, if hard is 0.
+ *   beta, hard in [0, 1]; teacher_scale > 0 (read with rest == 0);
+ *            grad_scale finite.
+ *   div      device float[rows].
+ *   stats    device float[4]: the loss; sums over rows of w div, w (-log
+ *            p[label]) (0 without labels), and w (sum of p over the list).
+ *   dlogits, ld_d   as for sparcml_policy_loss.
+ *   ws       sparcml_workspace_size(SPARCML_OP_DISTILL, count, rows, vocab, ...)
+ * Does not synchronize.  Errors: EINVAL, EWORKSPACE, EHIP.
+ */
+typedef struct sparcml_distill_args {
+    const int32_t* id;
+    const void* value;
+    const float* weight;
+    uint64_t ld;
+    uint32_t count;
+    uint32_t type;
+    uint32_t rest;
+    float teacher_scale, beta, hard, grad_scale;
+    uint32_t reserved; /* 0 */
+} sparcml_distill_args;
+SPARCML_API int sparcml_distill_loss(const sparcml_logits* in, const sparcml_distill_args* args, float* div, float* stats,
+                         void* dlogits, uint64_t ld_d, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Kernel timing for benchmarks and profiling (off by default; per calling
  * thread).  While enabled, each call records a pair of HIP events on its
  * stream around each of its main kernels; sparcml_timing_read returns the
@@ -695,6 +825,8 @@ SPARCML_API int sparcml_preference_loss(const sparcml_logits* in, int pairs, con
 #define SPARCML_TIMER_LOSS_ROWS 13    /* losses: the pass over the logits' rows */
 #define SPARCML_TIMER_LOSS_GRAD 14    /* losses: what follows it (joined slices, sums over tokens and pairs, the
                                          gradient where it is a pass of its own) */
+#define SPARCML_TIMER_SCORES 15       /* token scores */
+#define SPARCML_TIMER_SCORES_GRAD 16  /* their gradient */
 SPARCML_API int sparcml_timing_enable(int on);
 SPARCML_API int sparcml_timing_read(int group, float* ms);
 

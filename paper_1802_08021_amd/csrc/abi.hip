@@ -361,6 +361,13 @@ int sparcml_workspace_size(int op, int P, uint64_t N, uint64_t max_nnz, double d
                  : op == SPARCML_OP_POLICY ? policy_workspace(N, max_nnz)
                                            : preference_workspace((uint32_t)P, N, max_nnz);
         return SPARCML_OK;
+    case SPARCML_OP_SCORES:
+    case SPARCML_OP_DISTILL:
+        if (P < (op == SPARCML_OP_DISTILL) || P > SPARCML_MAX_TOP || !valid_rows(N, max_nnz))
+            return fail(SPARCML_EINVAL, "bad sizes of logits or lists");
+        *bytes = op == SPARCML_OP_SCORES ? scores_workspace((uint32_t)P, N, max_nnz)
+                                         : distill_workspace((uint32_t)P, N, max_nnz);
+        return SPARCML_OK;
     default: return fail(SPARCML_EINVAL, "unknown op %d", op);
     }
 }
@@ -722,9 +729,9 @@ int sparcml_adamw(const sparcml_tensors* plan, const sparcml_adamw_args* args, c
 }
 
 // Shared argument checks of the losses.
-static int logits_validate(const sparcml_logits* in, Logits* l)
+static int logits_validate(const sparcml_logits* in, Logits* l, bool labels = true)
 {
-    if (!in || !in->x || !in->label) return fail(SPARCML_EINVAL, "NULL logits or labels");
+    if (!in || !in->x || (labels && !in->label)) return fail(SPARCML_EINVAL, "NULL logits or labels");
     if (!valid_rows(in->rows, in->vocab)) return fail(SPARCML_EINVAL, "rows and vocab must be in [1, 2^31)");
     if (in->ld < in->vocab || in->ld >= (1ull << 31)) return fail(SPARCML_EINVAL, "need vocab <= ld < 2^31");
     if (in->type > SPARCML_F16) return fail(SPARCML_EINVAL, "unknown type %u", in->type);
@@ -811,6 +818,78 @@ int sparcml_preference_loss(const sparcml_logits* in, int pairs, const uint64_t*
         hipError_t e = preference_run(l, PreferenceArgs{ref_logp, beta, smoothing, grad_scale}, (uint32_t)pairs,
                                       b.data(), logp, stats, dlogits, ld_d, ws, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, "preference_loss");
+        return SPARCML_OK;
+    });
+}
+
+static_assert(SPARCML_MAX_TOP == kMaxTop, "the kernels hold that many");
+
+int sparcml_token_scores(const sparcml_logits* in, const sparcml_scores* out, void* ws, size_t ws_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        Logits l;
+        int rc = logits_validate(in, &l, false);
+        if (rc != SPARCML_OK) return rc;
+        if (!out) return fail(SPARCML_EINVAL, "NULL argument");
+        if (out->logp && !l.label) return fail(SPARCML_EINVAL, "logp needs labels");
+        if (out->top > SPARCML_MAX_TOP || out->top > l.vocab) return fail(SPARCML_EINVAL, "top must be at most %d and vocab", SPARCML_MAX_TOP);
+        if (out->top && (!out->top_id || !out->top_logp)) return fail(SPARCML_EINVAL, "top_id or top_logp is NULL");
+        const size_t need = scores_workspace(out->top, l.rows, l.vocab);
+        if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+        const ScoresOut o{out->logp, out->lse, out->entropy, out->norm, out->top_id, out->top_logp, out->top};
+        hipError_t e = scores_run(l, o, ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "token_scores");
+        return SPARCML_OK;
+    });
+}
+
+int sparcml_token_scores_grad(const sparcml_logits* in, const sparcml_scores_grad* args, void* dlogits, uint64_t ld_d,
+                              void* stream)
+{
+    return guarded([&]() -> int {
+        Logits l;
+        int rc = logits_validate(in, &l, false);
+        if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
+        if (rc != SPARCML_OK) return rc;
+        if (!args || !args->norm || !dlogits) return fail(SPARCML_EINVAL, "NULL argument");
+        const sparcml_scores_grad& g = *args;
+        if (g.d_logp && !l.label) return fail(SPARCML_EINVAL, "d_logp needs labels");
+        if (g.d_entropy && !g.entropy) return fail(SPARCML_EINVAL, "d_entropy needs the entropy");
+        if (g.d_top && (!g.top_id || !g.top || g.top > SPARCML_MAX_TOP || g.top > l.vocab))
+            return fail(SPARCML_EINVAL, "d_top needs top_id, and top in [1, %d] and at most vocab", SPARCML_MAX_TOP);
+        const ScoresGrad a{g.norm, g.entropy, g.top_id, g.d_logp, g.d_lse, g.d_entropy, g.d_top, g.d_top ? g.top : 0};
+        hipError_t e = scores_grad_run(l, a, dlogits, ld_d, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "token_scores_grad");
+        return SPARCML_OK;
+    });
+}
+
+int sparcml_distill_loss(const sparcml_logits* in, const sparcml_distill_args* args, float* div, float* stats,
+                         void* dlogits, uint64_t ld_d, void* ws, size_t ws_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        Logits l;
+        int rc = logits_validate(in, &l, false);
+        if (rc == SPARCML_OK) rc = gradient_validate(in, dlogits, ld_d);
+        if (rc != SPARCML_OK) return rc;
+        if (!args || !args->id || !args->value || !div || !stats) return fail(SPARCML_EINVAL, "NULL argument");
+        const sparcml_distill_args& a = *args;
+        if (a.count < 1 || a.count > SPARCML_MAX_TOP || a.ld < a.count || a.ld >= (1ull << 31))
+            return fail(SPARCML_EINVAL, "need 1 <= count <= %d and count <= ld < 2^31", SPARCML_MAX_TOP);
+        if (a.type > SPARCML_F16) return fail(SPARCML_EINVAL, "unknown type %u of values", a.type);
+        if (a.rest > 1) return fail(SPARCML_EINVAL, "rest must be 0 or 1");
+        if (!(a.beta >= 0.0f && a.beta <= 1.0f) || !(a.hard >= 0.0f && a.hard <= 1.0f))
+            return fail(SPARCML_EINVAL, "beta and hard must be in [0, 1]");
+        if (!a.rest && a.beta != 0.0f) return fail(SPARCML_EINVAL, "without the rest, beta must be 0");
+        if (!a.rest && (!(a.teacher_scale > 0.0f) || !isfinite(a.teacher_scale)))
+            return fail(SPARCML_EINVAL, "teacher_scale must be positive and finite");
+        if (!isfinite(a.grad_scale)) return fail(SPARCML_EINVAL, "grad_scale must be finite");
+        if (a.hard != 0.0f && !l.label) return fail(SPARCML_EINVAL, "hard needs labels");
+        const size_t need = distill_workspace(a.count, l.rows, l.vocab);
+        if (!ws || ws_bytes < need) return fail(SPARCML_EWORKSPACE, "workspace %zu < %zu bytes", ws_bytes, need);
+        const DistillArgs d{a.id, a.value, a.weight, a.ld, a.count, a.type, a.rest, a.teacher_scale, a.beta, a.hard, a.grad_scale};
+        hipError_t e = distill_run(l, d, div, stats, dlogits, ld_d, ws, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, "distill_loss");
         return SPARCML_OK;
     });
 }

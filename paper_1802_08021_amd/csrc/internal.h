@@ -55,7 +55,9 @@ enum TimerSlot {
     kTAdamw = 12,       // AdamW step
     kTLossRows = 13,    // losses: the pass over the logits' rows
     kTLossGrad = 14,    // losses: what follows it (sums, the gradient pass)
-    kTSlots = 15
+    kTScores = 15,      // token scores
+    kTScoresGrad = 16,  // their gradient
+    kTSlots = 17
 };
 void timer_begin(int slot, hipStream_t s);
 void timer_end(int slot, hipStream_t s);
@@ -325,5 +327,37 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
 // bounds: host array of 2 * pairs + 1 row numbers (each below 2^31).
 hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pairs, const uint32_t* bounds,
                           float* logp, float* stats, void* dlogits, uint64_t ldd, void* ws, hipStream_t s);
+
+// ---------------------------------------------------------------- scores
+// (Logits without labels: every row is in use.)
+constexpr uint32_t kMaxTop = 256;  // tokens on a row's list
+struct ScoresOut {
+    float *logp, *lse, *entropy, *norm;
+    int32_t* top_id;
+    float* top_logp;
+    uint32_t top;
+};
+struct ScoresGrad {
+    const float *norm, *entropy;
+    const int32_t* top_id;
+    const float *d_logp, *d_lse, *d_entropy, *d_top;
+    uint32_t top;
+};
+size_t scores_workspace(uint32_t top, uint64_t rows, uint64_t vocab);
+hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_t s);
+hipError_t scores_grad_run(const Logits& in, const ScoresGrad& a, void* dlogits, uint64_t ldd, hipStream_t s);
+
+// ---------------------------------------------------------------- distillation
+struct DistillArgs {
+    const int32_t* id;
+    const void* value;
+    const float* weight;  // or nullptr: 1 everywhere
+    uint64_t ld;
+    uint32_t count, type, rest;
+    float teacher_scale, beta, hard, grad_scale;
+};
+size_t distill_workspace(uint32_t count, uint64_t rows, uint64_t vocab);
+hipError_t distill_run(const Logits& in, const DistillArgs& a, float* div, float* stats, void* dlogits, uint64_t ldd,
+                       void* ws, hipStream_t s);
 
 }  // namespace sparcml

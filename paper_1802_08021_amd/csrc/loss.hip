@@ -126,34 +126,6 @@ __global__ void __launch_bounds__(1024) k_policy_stats(uint64_t rows, PolicyArgs
 
 // ---------------------------------------------------------------- a workgroup a row
 
-// What a thread has of its row so far: the maximum and the sum against it.
-struct Own {
-    float top, sum;
-    // The first `used` of U pieces (the same in the whole wave).
-    template <int TYPE, int U>
-    __device__ __forceinline__ void add(Piece<TYPE> (&x)[U], int used, float c)
-    {
-        float high = top;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u >= used) break;
-#pragma unroll
-            for (int i = 0; i < Piece<TYPE>::N; ++i) high = fmaxf(high, x[u].get(i));
-        }
-        const float base = high == -INFINITY ? 0.0f : high;
-        float more[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u >= used) break;
-            x[u].repack();
-#pragma unroll
-            for (int i = 0; i < Piece<TYPE>::N; ++i) more[i & 3] += exp2_fast((x[u].get(i) - base) * c);
-        }
-        sum = sum * exp2_fast((top - base) * c) + ((more[0] + more[1]) + (more[2] + more[3]));
-        top = high;
-    }
-};
-
 // Row blockIdx.x by one workgroup: the first NV pieces of a thread stay in
 // registers between the two passes over them, LP more in LDS, the rest of a
 // longer row is read once more (GRAD; from the 256 MB cache, so its first read

@@ -150,6 +150,34 @@ __device__ __forceinline__ void block_sum(double* x, double (*s_w)[4], int count
     }
 }
 
+// What a thread has of its row so far: the maximum and the sum against it.
+struct Own {
+    float top, sum;
+    // The first `used` of U pieces (the same in the whole wave).
+    template <int TYPE, int U>
+    __device__ __forceinline__ void add(Piece<TYPE> (&x)[U], int used, float c)
+    {
+        float high = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u >= used) break;
+#pragma unroll
+            for (int i = 0; i < Piece<TYPE>::N; ++i) high = fmaxf(high, x[u].get(i));
+        }
+        const float base = high == -INFINITY ? 0.0f : high;
+        float more[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u >= used) break;
+            x[u].repack();
+#pragma unroll
+            for (int i = 0; i < Piece<TYPE>::N; ++i) more[i & 3] += exp2_fast((x[u].get(i) - base) * c);
+        }
+        sum = sum * exp2_fast((top - base) * c) + ((more[0] + more[1]) + (more[2] + more[3]));
+        top = high;
+    }
+};
+
 template <class F>
 void by_type(uint32_t type, F f)
 {

@@ -19,7 +19,8 @@ LIB_PATH = os.path.join(_HERE, "_lib", "libsparcml.so")
 
 OK, EINVAL, ECAPACITY, EWORKSPACE, EUNSORTED, EHIP = 0, -1, -2, -3, -4, -5
 OP_TOPK, OP_QUANTIZE, OP_REDUCE, OP_DENSIFY, OP_QUANTIZE_BUCKETED, OP_CONCAT, OP_VALIDATE = 1, 2, 3, 4, 5, 6, 7
-OP_TENSORS, OP_LOGPROB, OP_POLICY, OP_PREFERENCE = 8, 9, 10, 11
+OP_TENSORS, OP_LOGPROB, OP_POLICY, OP_PREFERENCE, OP_SCORES, OP_DISTILL = 8, 9, 10, 11, 12, 13
+MAX_TOP = 256  # tokens on a row's list
 F32, BF16, F16 = 0, 1, 2
 
 
@@ -90,6 +91,31 @@ class PolicyArgs(ctypes.Structure):
     """Mirror of ``sparcml_policy_args``."""
     _fields_ = [(name, ctypes.c_void_p) for name in ("old_logp", "ref_logp", "adv", "weight")] + [
         (name, ctypes.c_float) for name in ("clip_lo", "clip_hi", "kl", "grad_scale")]
+
+
+class Scores(ctypes.Structure):
+    """Mirror of ``sparcml_scores``."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("logp", "lse", "entropy", "norm", "top_id", "top_logp")] + [
+        ("top", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+    ]
+
+
+class ScoresGrad(ctypes.Structure):
+    """Mirror of ``sparcml_scores_grad``."""
+    _fields_ = [(name, ctypes.c_void_p)
+                for name in ("norm", "entropy", "top_id", "d_logp", "d_lse", "d_entropy", "d_top")] + [
+        ("top", ctypes.c_uint32),
+        ("reserved", ctypes.c_uint32),
+    ]
+
+
+class DistillArgs(ctypes.Structure):
+    """Mirror of ``sparcml_distill_args``."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("id", "value", "weight")] + [("ld", ctypes.c_uint64)] + [
+        (name, ctypes.c_uint32) for name in ("count", "type", "rest")] + [
+        (name, ctypes.c_float) for name in ("teacher_scale", "beta", "hard", "grad_scale")] + [
+        ("reserved", ctypes.c_uint32)]
 
 
 class SparcmlError(RuntimeError):
@@ -163,6 +189,12 @@ def lib() -> ctypes.CDLL:
     L.sparcml_preference_loss.argtypes = [ctypes.POINTER(Logits), i32, ctypes.POINTER(u64), vp, f32, f32, f32, vp, vp,
                                           vp, u64, vp, ctypes.c_size_t, vp]
     L.sparcml_preference_loss.restype = i32
+    L.sparcml_token_scores.argtypes = [vp, vp, vp, ctypes.c_size_t, vp]
+    L.sparcml_token_scores.restype = i32
+    L.sparcml_token_scores_grad.argtypes = [vp, vp, vp, u64, vp]
+    L.sparcml_token_scores_grad.restype = i32
+    L.sparcml_distill_loss.argtypes = [vp, vp, vp, vp, vp, u64, vp, ctypes.c_size_t, vp]
+    L.sparcml_distill_loss.restype = i32
     L.sparcml_timing_enable.argtypes = [i32]
     L.sparcml_timing_enable.restype = i32
     L.sparcml_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_float)]
@@ -179,6 +211,7 @@ TIMER_REDUCE_PASS, TIMER_REDUCE_WRITE, TIMER_REDUCE_SLOW = 0, 1, 2
 TIMER_QUANT_NORM, TIMER_QUANT_CODES, TIMER_TOPK_SELECT, TIMER_TOPK_WRITE, TIMER_DENSIFY = 3, 4, 5, 6, 7
 TIMER_CONCAT, TIMER_TOPK_BUCKETED, TIMER_REDUCE_MERGE = 8, 9, 10
 TIMER_GRAD_NORM, TIMER_ADAMW, TIMER_LOSS_ROWS, TIMER_LOSS_GRAD = 11, 12, 13, 14
+TIMER_SCORES, TIMER_SCORES_GRAD = 15, 16
 
 
 def timing_enable(on: bool) -> None:
@@ -851,6 +884,8 @@ class AdamwCall(_TensorPlan):
 
 
 class _LogitsCall:
+    # op None: a call without a workspace; labels may be None where the call
+    # allows it.
     def __init__(self, logits, labels, scale, op, pairs=1):
         torch = _torch()
         if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
@@ -860,15 +895,40 @@ class _LogitsCall:
         self.rows, self.vocab = logits.shape
         self.dev = logits.device
         ld = logits.stride(0) if self.rows > 1 else self.vocab
-        _require(labels, "labels", torch.int32, self.rows, self.dev)
+        if labels is not None or op in (OP_LOGPROB, OP_POLICY, OP_PREFERENCE):
+            _require(labels, "labels", torch.int32, self.rows, self.dev)
         self.logits = Logits(logits.data_ptr(), _ptr(labels), self.rows, self.vocab, ld, _type_id(logits, "logits"),
                              scale)
-        self.ws = alloc_workspace(workspace_size(op, pairs, self.rows, self.vocab), self.dev)
-        self.logp = torch.empty(self.rows, dtype=torch.float32, device=self.dev)
+        self.ws = alloc_workspace(0 if op is None else workspace_size(op, pairs, self.rows, self.vocab), self.dev)
+        self.logp = None
+        if op in (OP_LOGPROB, OP_POLICY, OP_PREFERENCE) or (op == OP_SCORES and labels is not None):
+            self.logp = torch.empty(self.rows, dtype=torch.float32, device=self.dev)
         self._keep = [logits, labels]
         # what every run passes
-        self._in, self._logp = ctypes.byref(self.logits), self.logp.data_ptr()
+        self._in, self._logp = ctypes.byref(self.logits), _ptr(self.logp)
         self._ws = (self.ws.data_ptr(), self.ws.numel())
+
+    def _launch(self, f, *args):
+        """The library's call on the tensors' device and its current stream."""
+        torch = _torch()
+        if torch.cuda.current_device() == self.dev.index:
+            rc = f(*args, _stream_ptr(self.dev))
+        else:
+            with torch.cuda.device(self.dev):
+                rc = f(*args, _stream_ptr(self.dev))
+        _check(rc, f.__name__)
+
+    def _list(self, t, name, dtypes, count=None):
+        """Row stride of a list of tokens or values a row."""
+        torch = _torch()
+        if not isinstance(t, torch.Tensor) or t.device != self.dev or t.dim() != 2 or t.shape[0] != self.rows \
+                or t.dtype not in dtypes or not t.shape[1] or (t.stride(1) != 1 and t.shape[1] > 1) \
+                or (count is not None and t.shape[1] != count):
+            raise ValueError(f"{name} must be a 2-D tensor of {self.rows} rows of "
+                             f"{'tokens' if count is None else count}, adjacent in a row, on {self.dev}, of a type "
+                             f"among {', '.join(map(str, dtypes))}")
+        self._keep.append(t)
+        return t.stride(0) if self.rows > 1 else t.shape[1]
 
     def _per_row(self, t, name):
         if t is not None:
@@ -980,3 +1040,121 @@ def preference_loss(logits, labels, bounds, **more):
     c = PreferenceLossCall(logits, labels, bounds, **more)
     c.run()
     return {"stats": c.stats, "logp": c.logp, "dlogits": c.dlogits}
+
+
+class TokenScoresCall(_LogitsCall):
+    """Repeated scores of rows of logits [T, V] (fp32, bf16 or fp16, rows at
+    any stride).  ``labels``: int32 [T] (outside [0, V): a row that is not in
+    use), or None: no tokens are given.  run() fills ``logp`` (None without
+    labels), ``lse``, ``entropy`` (fp32 [T]), ``norm`` (fp32 [T, 2], what the
+    gradient takes), and the ``top`` (up to 256) most likely tokens in order:
+    ``top_id`` (int32 [T, top]; -1 where there are none left) and ``top_logp``
+    (fp32)."""
+
+    def __init__(self, logits, labels=None, top: int = 0, scale: float = 1.0):
+        torch = _torch()
+        if not 0 <= top <= MAX_TOP:
+            raise ValueError(f"top must be in [0, {MAX_TOP}]")
+        super().__init__(logits, labels, scale, OP_SCORES, top)
+        new = lambda *shape: torch.empty(*shape, dtype=torch.float32, device=self.dev)  # noqa: E731
+        self.lse, self.entropy, self.norm = new(self.rows), new(self.rows), new(self.rows, 2)
+        self.top_id = torch.empty(self.rows, top, dtype=torch.int32, device=self.dev)
+        self.top_logp = new(self.rows, top)
+        self.out = Scores(self._logp, _ptr(self.lse), _ptr(self.entropy), _ptr(self.norm), _ptr(self.top_id),
+                          _ptr(self.top_logp), top)
+        self._outs = (ctypes.byref(self.out), *self._ws)
+
+    def run(self) -> None:
+        self._launch(lib().sparcml_token_scores, self._in, *self._outs)
+
+
+def token_scores(logits, labels=None, top: int = 0, scale: float = 1.0):
+    """What rows of logits say (see TokenScoresCall): dict(logp, lse, entropy,
+    norm, top_id, top_logp)."""
+    c = TokenScoresCall(logits, labels, top, scale)
+    c.run()
+    return {k: getattr(c, k) for k in ("logp", "lse", "entropy", "norm", "top_id", "top_logp")}
+
+
+class TokenScoresGradCall(_LogitsCall):
+    """Repeated gradient of a loss over the scores, from its derivatives by
+    them: ``d_logp`` (with ``labels``), ``d_lse``, ``d_entropy`` (with
+    ``entropy``) fp32 [T], ``d_top`` fp32 [T, top] (with ``top_id``), each or
+    None.  ``norm``, ``entropy``, ``top_id``: as TokenScoresCall filled them
+    for these logits and this scale.  run() fills ``dlogits`` (as
+    PolicyLossCall, but not None)."""
+
+    def __init__(self, logits, norm, labels=None, d_logp=None, d_lse=None, entropy=None, d_entropy=None, top_id=None,
+                 d_top=None, scale: float = 1.0, dlogits="new"):
+        torch = _torch()
+        super().__init__(logits, labels, scale, None)
+        _require(norm, "norm", torch.float32, 2 * self.rows, self.dev)
+        self._keep.append(norm)
+        if (d_entropy is not None and entropy is None) or (d_top is not None and top_id is None):
+            raise ValueError("d_entropy goes with entropy, d_top with top_id")
+        if dlogits is None:
+            raise ValueError("dlogits must be 'new', 'inplace' or a tensor")
+        top = 0
+        if d_top is not None:
+            self._list(top_id, "top_id", (torch.int32,))
+            top = top_id.shape[1]
+            _require(top_id, "top_id", torch.int32, self.rows * top, self.dev)
+            _require(d_top, "d_top", torch.float32, self.rows * top, self.dev)
+            self._keep.append(d_top)
+        per = self._per_row
+        self.args = ScoresGrad(_ptr(norm), per(entropy, "entropy"), _ptr(top_id) if top else 0, per(d_logp, "d_logp"),
+                               per(d_lse, "d_lse"), per(d_entropy, "d_entropy"), _ptr(d_top), top)
+        self._gradient(dlogits)
+        self._outs = (ctypes.byref(self.args), _ptr(self.dlogits), self._ldd)
+
+    def run(self) -> None:
+        self._launch(lib().sparcml_token_scores_grad, self._in, *self._outs)
+
+
+def token_scores_grad(logits, norm, **more):
+    """One gradient of a loss over scores (see TokenScoresGradCall)."""
+    c = TokenScoresGradCall(logits, norm, **more)
+    c.run()
+    return c.dlogits
+
+
+class DistillLossCall(_LogitsCall):
+    """Repeated divergence of the rows' distributions from a teacher's lists:
+    ``ids`` int32 [T, K] and ``values`` [T, K] (fp32, bf16 or fp16), K up to
+    256, rows at any stride; ids outside [0, V) are no entries.  ``rest`` True:
+    values are log probabilities (token_scores' ``top_logp``), and all other
+    tokens together are one more outcome; False: softmax(teacher_scale *
+    values) is all of the teacher's distribution (``beta`` 0 only).  ``beta``:
+    0 KL(teacher || student), 1 KL(student || teacher), between a mixture's.
+    ``hard``: share of the loss of given tokens (``labels``), -log p.
+    ``weight``: fp32 [T] (0: a row that is not read) or None.  run() fills
+    ``div`` (fp32 [T]), ``stats`` (loss; sums of weighted div, -log p of the
+    labels, probability of the listed tokens) and ``dlogits`` (as
+    PolicyLossCall)."""
+
+    def __init__(self, logits, ids, values, weight=None, labels=None, rest: bool = True, beta: float = 0.0,
+                 hard: float = 0.0, scale: float = 1.0, teacher_scale: float = 1.0, grad_scale: float = 1.0,
+                 dlogits="new"):
+        torch = _torch()
+        if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or not 1 <= ids.shape[1] <= MAX_TOP:
+            raise ValueError(f"ids must be a 2-D tensor of 1 to {MAX_TOP} tokens a row")
+        super().__init__(logits, labels, scale, OP_DISTILL, ids.shape[1])
+        ld = self._list(ids, "ids", (torch.int32,))
+        if self._list(values, "values", (torch.float32, torch.bfloat16, torch.float16), ids.shape[1]) != ld:
+            raise ValueError("ids and values must have the same row stride")
+        self.div = torch.empty(self.rows, dtype=torch.float32, device=self.dev)
+        self.args = DistillArgs(ids.data_ptr(), values.data_ptr(), self._per_row(weight, "weight"), ld, ids.shape[1],
+                                _type_id(values, "values"), int(bool(rest)), teacher_scale, beta, hard, grad_scale)
+        self._gradient(dlogits)
+        self._outs = (ctypes.byref(self.args), _ptr(self.div), _ptr(self.stats), _ptr(self.dlogits), self._ldd, *self._ws)
+
+    def run(self) -> None:
+        self._launch(lib().sparcml_distill_loss, self._in, *self._outs)
+
+
+def distill_loss(logits, ids, values, **more):
+    """One divergence from a teacher's lists and its gradient (see
+    DistillLossCall): dict(stats, div, dlogits)."""
+    c = DistillLossCall(logits, ids, values, **more)
+    c.run()
+    return {"stats": c.stats, "div": c.div, "dlogits": c.dlogits}
