@@ -53,6 +53,8 @@ struct RowCut {
         full = (V - head) / N;
         singles = V - full * N;
     }
+    // From its first element on.
+    __device__ __forceinline__ explicit RowCut(uint32_t V) : head(0), full(V / N), singles(V % N) {}
     __device__ __forceinline__ uint32_t piece(uint32_t j) const { return head + j * N; }
     __device__ __forceinline__ uint32_t single(uint32_t i) const { return i < head ? i : i + full * N; }
     __device__ __forceinline__ bool in_piece(uint32_t v) const { return v >= head && (v - head) / N < full; }
