@@ -48,13 +48,44 @@ __device__ __forceinline__ bool distilled(const Logits& in, const DistillArgs& a
     return !(in.label && !has_token(in, t)) && !(a.weight && a.weight[t] == 0.0f);
 }
 
-// What a row's gradient is made of, and its terms of the sums over rows.
-struct DistillRow {
-    double ln, off, far;  // ln S; what makes log probabilities of the list's values; F
-    float top, rest_top;  // M; the largest unlisted logit
-    float A, k, hard;     // coefficient off the list; scales; of the given token
+// A row's terms of the sums over rows.
+struct DistillTerms {
     float div, nll, covered;
 };
+// What its gradient is made of: off the list A 2^(c (x - top)); the given
+// token's part.
+struct DistillRow {
+    float A, top, given;
+};
+
+// e^x in fp64, within 10^-11 of itself: 2^n e^g with |g| <= ln 2 / 2, the
+// series of e^g up to g^9.  (The library's own, inlined where it is needed here,
+// takes 160 registers.)
+__device__ __forceinline__ double exp64(double x)
+{
+    const double n = rint(fmin(fmax(x, -2000.0), 2000.0) * 1.4426950408889634);
+    const double g = __builtin_fma(n, -0.6931471805599453, fmin(fmax(x, -2000.0), 2000.0));
+    double y = 1.0 / 362880.0;
+    const double series[9] = {1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+    for (int i = 0; i < 9; ++i) y = __builtin_fma(y, g, series[i]);
+    y = ldexp(y, (int)n);
+    return x != x ? x : x == -INFINITY ? 0.0 : y;
+}
+// ln x in fp64, as part_ln takes it: within 10^-7.
+__device__ __forceinline__ double ln64(double x)
+{
+    if (!(x > 0.0 && x < INFINITY)) return x == 0.0 ? -INFINITY : x;
+    int e;
+    double m = frexp(x, &e);
+    if (m < 0.7071067811865476) {
+        m *= 2.0;
+        --e;
+    }
+    // (what is left of the rounding to fp32 is its own logarithm's first term)
+    const float f = (float)m;
+    return ((double)e + (double)__builtin_amdgcn_logf(f)) * 0.6931471805599453 + (m - (double)f) / (double)f;
+}
 
 // One outcome's share of the divergence and its derivative by the student's
 // log probability (lq, lp: log probabilities; a probability of 0 takes an
@@ -65,7 +96,7 @@ struct Share {
 __device__ __forceinline__ double product(double p, double x) { return p == 0.0 ? 0.0 : p * x; }
 __device__ __forceinline__ Share share_of(float beta, double lq, double lp)
 {
-    const double q = exp(lq), p = exp(lp), b = (double)beta;
+    const double q = exp64(lq), p = exp64(lp), b = (double)beta;
     Share r;
     if (beta == 0.0f) {
         r.div = product(q, lq - lp);
@@ -73,7 +104,7 @@ __device__ __forceinline__ Share share_of(float beta, double lq, double lp)
     } else if (beta == 1.0f) {
         r.div = r.f = product(p, lp - lq);
     } else {
-        const double lm = log(b * q + (1.0 - b) * p);
+        const double lm = ln64(b * q + (1.0 - b) * p);
         r.f = (1.0 - b) * product(p, lp - lm);
         r.div = b * product(q, lq - lm) + r.f;
     }
@@ -81,13 +112,127 @@ __device__ __forceinline__ Share share_of(float beta, double lq, double lp)
     return r;
 }
 
-// A listed token's gradient.
-__device__ __forceinline__ float listed_entry(const DistillArgs& a, const DistillRow& w, float value, float x, float scale)
+__device__ __forceinline__ double wave_sum(double x)
 {
-    const double lp = ((double)x - (double)w.top) * (double)scale - w.ln;
-    const Share e = share_of(a.beta, (double)value * (a.rest ? 1.0 : (double)a.teacher_scale) - w.off, lp);
-    const double soft = 1.0 - (double)a.hard;
-    return within((float)((double)w.k * (soft * e.f + exp(lp) * ((double)w.hard - soft * w.far))));
+    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+// A list in LDS: its tokens, the teacher's values, the student's logits, and
+// from the row's terms on the tokens' gradients.
+struct List {
+    uint32_t id[kMaxTop], dup;
+    float value[kMaxTop], x[kMaxTop], grad[kMaxTop];
+    DistillRow row;
+    // Entries that repeat an earlier one (found by whoever sets dup) go; every
+    // thread of the workgroup takes part.
+    __device__ __forceinline__ void drop_repeats(uint32_t count)
+    {
+        if (!dup) return;
+        uint32_t again = 0;
+        for (uint32_t i = threadIdx.x, k = 0; i < count; i += blockDim.x, ++k)
+            for (uint32_t j = 0; j < i; ++j) again |= (uint32_t)(id[j] == id[i]) << k;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x, k = 0; i < count; i += blockDim.x, ++k)
+            if (again >> k & 1u) id[i] = 0xFFFFFFFFu;
+        __syncthreads();
+    }
+};
+
+// A row's terms and its list's gradients, by one wave: from the sum over the
+// unlisted tokens and the given token's logit.
+__device__ __forceinline__ DistillTerms list_terms(const Logits& in, const DistillArgs& a, uint64_t t, const Part& rest,
+                                                   float at, List& list)
+{
+    const uint32_t lane = threadIdx.x & 63, V = (uint32_t)in.vocab;
+    const double scale = (double)in.scale, ts = a.rest ? 1.0 : (double)a.teacher_scale;
+    float M = rest.sum == 0.0f ? -INFINITY : rest.top, best = -INFINITY;
+    for (uint32_t i = lane; i < a.count; i += 64)
+        if (list.id[i] < V) {
+            best = fmaxf(best, list.value[i]);
+            M = fmaxf(M, list.x[i]);
+        }
+    M = wave_join<false>(M);
+    best = a.rest ? 0.0f : wave_join<false>(best);
+    const float top = M == -INFINITY ? 0.0f : M;
+    double q = 0.0, near = 0.0;
+#pragma unroll 1
+    for (uint32_t i = lane; i < a.count; i += 64)
+        if (list.id[i] < V) {
+            q += exp64(((double)list.value[i] - (double)best) * ts);
+            near += exp64(((double)list.x[i] - (double)top) * scale);
+        }
+    q = wave_sum(q);
+    near = wave_sum(near);
+    // the teacher's log probabilities: value ts - off
+    const double off = !a.rest && q != 0.0 ? (double)best * ts + ln64(q) : 0.0;
+    const double far = ((double)rest.top - (double)top) * scale;
+    const double outside = rest.sum == 0.0f ? 0.0 : exp64(far) * (double)rest.sum;
+    const double total = outside + near, ln = ln64(total);
+    double div = 0.0, F = 0.0, covered = 0.0;
+#pragma unroll 1
+    for (uint32_t i = lane; i < a.count; i += 64)
+        if (list.id[i] < V) {
+            const double lp = ((double)list.x[i] - (double)top) * scale - ln;
+            const Share s = share_of(a.beta, (double)list.value[i] * ts - off, lp);
+            div += s.div;
+            F += s.f;
+            covered += exp64(lp);
+        }
+    div = wave_sum(div);
+    F = wave_sum(F);
+    covered = wave_sum(covered);
+    Share out = {0.0, 0.0};
+    if (a.rest && rest.sum != 0.0f)
+        out = share_of(a.beta, ln64(fmax(1.0 - q, 0x1p-24)), far + part_ln(rest.sum) - ln);
+    div += out.div;
+    F += out.f;
+    const bool some = total != 0.0;  // (a row of nothing but -Inf adds nothing)
+    const double soft = 1.0 - (double)a.hard, hard = in.label && at != -INFINITY ? (double)a.hard : 0.0;
+    const double k0 = (double)within((float)((a.weight ? (double)a.weight[t] : 1.0) * (double)a.grad_scale * scale));
+    const uint32_t label = in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu;
+    bool listed = false;
+#pragma unroll 1
+    for (uint32_t i = lane; i < a.count; i += 64)
+        if (list.id[i] < V) {
+            const double lp = ((double)list.x[i] - (double)top) * scale - ln;
+            const Share s = share_of(a.beta, (double)list.value[i] * ts - off, lp);
+            const bool given = list.id[i] == label;
+            const double g = soft * s.f + exp64(lp) * (hard - soft * F) - (given ? hard : 0.0);
+            list.grad[i] = some ? within((float)(k0 * g)) : 0.0f;
+            listed |= given;
+        }
+    listed = __any(listed);
+    if (lane == 0) {
+        const double A = rest.sum == 0.0f ? 0.0 : k0 * (soft * out.f / (double)rest.sum + (hard - soft * F) * exp64(far) / total);
+        const float A32 = within((float)A);
+        // (NaN where the token has its place on the list, or none)
+        const float given = listed || hard == 0.0
+                                ? __builtin_nanf("")
+                                : within((float)(A32 * exp64(((double)at - (double)rest.top) * scale) - k0 * hard));
+        list.row = some ? DistillRow{A32, rest.top, given} : DistillRow{0.0f, 0.0f, __builtin_nanf("")};
+    }
+    const double nll = in.label ? ln - ((double)at - (double)top) * scale : 0.0;
+    return some ? DistillTerms{(float)div, (float)nll, (float)covered} : DistillTerms{0.0f, 0.0f, 0.0f};
+}
+
+// Marks of a piece's elements (a bit each) and what is left of the piece
+// without them.
+template <int TYPE>
+__device__ __forceinline__ uint32_t marks_of(const uint32_t* marks, uint32_t j)
+{
+    constexpr uint32_t N = Piece<TYPE>::N;
+    return marks[j * N / 32] >> (j * N % 32) & ((1u << N) - 1);
+}
+template <int TYPE>
+__device__ __forceinline__ void hide(Piece<TYPE>& x, uint32_t marks)
+{
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t two = marks >> (i * Piece<TYPE>::N / 4);
+        const uint32_t m = TYPE == kF32 ? (two & 1u ? ~0u : 0u) : (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
+        x.w[i] = (x.w[i] & ~m) | (Piece<TYPE>::kNone & m);
+    }
 }
 
 // ---------------------------------------------------------------- sums
@@ -96,13 +241,15 @@ constexpr uint32_t kWindow = 4096;  // pieces whose marks lie in LDS at a time
 
 // Slice s of a row, as k_slices takes them: (M, Z) over the unlisted tokens.
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, uint32_t S, uint32_t W, float c, Part* part)
+__global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, uint32_t S, uint32_t W, float c, Part* part,
+                                                     float* at_list, float* at_label, uint32_t* ticket)
 {
     typedef typename Elem<TYPE>::type E;
     constexpr uint32_t N = Piece<TYPE>::N;
     __shared__ float s_top[4], s_sum[4];
     __shared__ uint32_t s_marks[kWindow * N / 32], s_single[4];
     const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
+    if (blockIdx.x == 0 && tid == 0) *ticket = 0;  // for k_distill_grad
     for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
         const uint64_t t = b / S;
         const uint32_t s = (uint32_t)(b % S);
@@ -112,6 +259,10 @@ __global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, u
         const uint32_t first = (uint32_t)min((uint64_t)r.full, (uint64_t)s * W);
         const uint32_t end = (uint32_t)min((uint64_t)r.full, (uint64_t)(s + 1) * W);
         const Entry mine(a, t, tid, V);
+        if (s == 0) {  // (in place, the gradient's slices find each other's logits gone)
+            if (tid < a.count) at_list[t * a.count + tid] = mine.v < V ? (float)row[mine.v] : -INFINITY;
+            if (tid == 0) at_label[t] = in.label ? (float)row[in.label[t]] : -INFINITY;
+        }
         if (tid < 4) s_single[tid] = 0;
         Own own = {-INFINITY, 0.0f};
         for (uint32_t at = first; at < end || at == first; at += kWindow) {
@@ -135,14 +286,8 @@ __global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, u
             for (uint32_t j = at + tid; j < stop; j += 256) {
                 Piece<TYPE> x[1];
                 x[0].w = load_vec<u32x4, true>(row + r.piece(j));
-                const uint32_t marks = s_marks[(j - at) * N / 32] >> ((j - at) * N % 32) & ((1u << N) - 1);
-                if (marks)
-                    for (uint32_t i = 0; i < 4; ++i) {
-                        const uint32_t two = marks >> (i * N / 4);
-                        const uint32_t m = N == 4 ? (two & 1u ? ~0u : 0u)
-                                                  : (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
-                        x[0].w[i] = (x[0].w[i] & ~m) | (Piece<TYPE>::kNone & m);
-                    }
+                const uint32_t marks = marks_of<TYPE>(s_marks, j - at);
+                if (marks) hide(x[0], marks);
                 own.add(x, 1, c);
             }
             __syncthreads();
@@ -155,231 +300,319 @@ __global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, u
     }
 }
 
-// ---------------------------------------------------------------- terms
+// ---------------------------------------------------------------- a workgroup a row
 
-// Row blockIdx.x: its terms from the slices' parts and its list, an entry a
-// thread.
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_distill_terms(Logits in, DistillArgs a, uint32_t S, float c, const Part* part,
-                                                       DistillRow* terms, float* div)
+// Row blockIdx.x by one workgroup, as k_row takes it (the first NV pieces of a
+// thread in registers between the passes, LP more in LDS, the rest read once
+// more): the marks of its list, the sum over the unlisted tokens, by the first
+// wave the list's terms (four entries a lane) and the row's coefficient, the
+// gradient, and behind it the listed and the given token's places once more.
+template <int TYPE, int THREADS, int NV, int LP, bool KEEP>
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
+k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
-    __shared__ double s_w[4][4], s_w2[4][4], s_w3[4][4];
-    __shared__ float s_top[4], s_value[4];
-    __shared__ uint32_t s_id[kMaxTop];
-    const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
-    for (uint64_t t = blockIdx.x; t < in.rows; t += gridDim.x) {
-        if (!distilled(in, a, t)) {
-            if (tid == 0) {
-                terms[t] = DistillRow{};
-                div[t] = 0.0f;
-            }
-            continue;
-        }
-        const E* row = static_cast<const E*>(in.x) + t * in.ld;
-        Entry e(a, t, tid, V);
-        // a token that is there twice counts by its first entry
-        s_id[tid] = e.v;
-        __syncthreads();
-        if (e.v < V)
-            for (uint32_t i = 0; i < tid; ++i)
-                if (s_id[i] == e.v) {
-                    e.v = 0xFFFFFFFFu;
-                    break;
-                }
-        const bool there = e.v < V;
-        const float x = there ? (float)row[e.v] : -INFINITY;
-        const float at = in.label ? (float)row[in.label[t]] : -INFINITY;
-        const Part rest = join_slices(part + t * S, S, 64, c);
-        // the teacher's log probabilities: value * scale - off
-        const double ts = a.rest ? 1.0 : (double)a.teacher_scale;
-        double off = 0.0, left = 0.0;
-        const float best = a.rest ? 0.0f : join_waves<false>(there ? e.value : -INFINITY, s_value);
-        const float top_x = join_waves<false>(x, s_top);
-        const float M = fmaxf(top_x, rest.sum == 0.0f ? -INFINITY : rest.top);
-        const float top = M == -INFINITY ? 0.0f : M;
-        const double near = ((double)x - (double)top) * (double)in.scale;
-        double sums[2] = {there ? exp(a.rest ? (double)e.value : ((double)e.value - (double)best) * ts) : 0.0,
-                          there ? exp(near) : 0.0};
-        block_sum(sums, s_w, 2);
-        if (a.rest)
-            left = fmax(1.0 - sums[0], 0x1p-24);
-        else if (sums[0] > 0.0)
-            off = (double)best * ts + log(sums[0]);
-        const double far = ((double)rest.top - (double)top) * (double)in.scale;
-        const double outside = rest.sum == 0.0f ? 0.0 : exp(far) * (double)rest.sum;
-        const double total = outside + sums[1], ln = log(total);
-        Share own = {0.0, 0.0};
-        double p = 0.0;
-        if (there) {
-            own = share_of(a.beta, (double)e.value * ts - off, near - ln);
-            p = exp(near - ln);
-        }
-        double all[3] = {own.div, own.f, p};
-        block_sum(all, s_w2, 3);
+    constexpr int N = Piece<TYPE>::N;
+    extern __shared__ uint32_t s_marks[];
+    __shared__ u32x4 s_keep[LP ? LP * THREADS : 1];
+    __shared__ Part s_part[THREADS / 64];
+    __shared__ uint32_t s_single[4];
+    __shared__ List s_list;
+    const uint64_t t = blockIdx.x;
+    const uint32_t V = (uint32_t)in.vocab, tid = threadIdx.x, step = blockDim.x, lane = tid & 63;
+    const E* row = static_cast<const E*>(in.x) + t * in.ld;
+    E* out = static_cast<E*>(dlogits) + t * ldd;
+    if (!distilled(in, a, t)) {
         if (tid == 0) {
-            DistillRow w = {};
-            if (total != 0.0) {
-                Share out = {0.0, 0.0};
-                if (a.rest && rest.sum != 0.0f) out = share_of(a.beta, log(left), far + part_ln(rest.sum) - ln);
-                const double F = all[1] + out.f, soft = 1.0 - (double)a.hard;
-                const double weight = a.weight ? (double)a.weight[t] : 1.0;
-                const bool given = in.label && at != -INFINITY;
-                w.ln = ln;
-                w.off = off;
-                w.far = F;
-                w.top = top;
-                w.rest_top = rest.top;
-                w.k = within((float)(weight * (double)a.grad_scale * (double)in.scale));
-                w.hard = given ? a.hard : 0.0f;
-                if (rest.sum != 0.0f)
-                    w.A = within((float)((double)w.k * (soft * out.f / (double)rest.sum +
-                                                        ((double)w.hard - soft * F) * exp(far) / total)));
-                w.div = (float)(all[0] + out.div);
-                w.nll = in.label ? (float)(ln - ((double)at - (double)top) * (double)in.scale) : 0.0f;
-                w.covered = (float)all[2];
-            }
-            terms[t] = w;
-            div[t] = w.div;
+            div[t] = 0.0f;
+            terms[t] = DistillTerms{0.0f, 0.0f, 0.0f};
         }
-        __syncthreads();
+        if (dlogits) clear_row<TYPE>(out, V);
+        return;
     }
+    const RowCut<TYPE> r(row, V);
+    const int used = (int)min((r.full + step - 1) / step, (uint32_t)NV);
+    Piece<TYPE> x[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        x[j].none();
+        if (tid + step * j < r.full) x[j].w = load_vec<u32x4, KEEP>(row + r.piece(tid + step * j));
+    }
+    float single = tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
+    // the list's marks
+    const uint32_t words = (r.full * N + 31) / 32;
+    for (uint32_t i = tid; i < words; i += step) s_marks[i] = 0;
+    if (tid < 4) s_single[tid] = 0;
+    if (tid == 4) s_list.dup = 0;
+    __syncthreads();
+    for (uint32_t i = tid; i < a.count; i += step) {
+        const Entry e(a, t, i, V);
+        s_list.id[i] = e.v;
+        s_list.value[i] = e.value;
+        if (e.v < V) {
+            s_list.x[i] = (float)row[e.v];
+            const bool in_piece = r.in_piece(e.v);
+            const uint32_t bit = in_piece ? e.v - r.head : e.v < r.head ? e.v : e.v - r.full * N;
+            uint32_t* word = (in_piece ? s_marks : s_single) + bit / 32;
+            if (atomicOr(word, 1u << (bit % 32)) >> (bit % 32) & 1u) s_list.dup = 1;
+        }
+    }
+    __syncthreads();
+    s_list.drop_repeats(a.count);
+    const float at = tid < 64 && in.label ? (float)row[in.label[t]] : -INFINITY;
+    if (tid < r.singles && s_single[tid / 32] >> (tid % 32) & 1u) single = -INFINITY;
+    Own own = {single, single == -INFINITY ? 0.0f : 1.0f};
+    for (uint32_t j = tid + step * NV, slot = tid; j < r.full; j += step, slot += step) {
+        Piece<TYPE> q[1];
+        q[0].w = load_vec<u32x4, true>(row + r.piece(j));
+        const uint32_t marks = marks_of<TYPE>(s_marks, j);
+        if (marks) hide(q[0], marks);
+        own.add(q, 1, c);
+        if (LP && slot < LP * step) s_keep[slot] = q[0].w;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i >= used) break;
+        const uint32_t j = tid + step * i, marks = j < r.full ? marks_of<TYPE>(s_marks, j) : 0u;
+        if (marks) hide(x[i], marks);
+    }
+    own.add(x, used, c);
+    {
+        float top = wave_join<false>(own.top);
+        if (top == -INFINITY) top = 0.0f;
+        const float sum = wave_join<true>(own.sum * exp2_fast((own.top - top) * c));
+        if (lane == 0) s_part[tid >> 6] = Part{top, sum};
+    }
+    __syncthreads();
+    if (tid < 64) {
+        // a lane a wave's part
+        const Part rest = join_slices(s_part, step / 64, 64, c);
+        const DistillTerms d = list_terms(in, a, t, rest, at, s_list);
+        if (tid == 0) {
+            div[t] = d.div;
+            terms[t] = d;
+        }
+    }
+    __syncthreads();
+    if (!dlogits) return;
+    const float A = s_list.row.A, top = s_list.row.top;
+    uint32_t j = tid + step * (NV + LP);
+    Piece<TYPE> next;
+    if (j < r.full) next.w = load_vec<u32x4>(row + r.piece(j));
+    auto write = [&](Piece<TYPE>& q, uint32_t at) {
+        q.repack();
+        float z[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = entry(q.get(i), c, top, A);
+        q.put(z);
+        if (at < r.full) store_vec(out + r.piece(at), q.w);
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (i >= used) break;
+        write(x[i], tid + step * i);
+    }
+    for (uint32_t i = 0; i < (uint32_t)LP && tid + step * (NV + i) < r.full; ++i) {
+        Piece<TYPE> now;
+        now.w = s_keep[tid + step * i];
+        write(now, tid + step * (NV + i));
+    }
+    for (; j < r.full; j += step) {
+        Piece<TYPE> now = next;
+        if (j + step < r.full) next.w = load_vec<u32x4>(row + r.piece(j + step));
+        write(now, j);
+    }
+    if (tid < r.singles) out[r.single(tid)] = (E)entry(single, c, top, A);
+    // (every store before this is done before the next ones begin)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (uint32_t i = tid; i < a.count; i += step)
+        if (s_list.id[i] < V) out[s_list.id[i]] = (E)s_list.grad[i];
+    if (tid == 0 && s_list.row.given == s_list.row.given) out[in.label[t]] = (E)s_list.row.given;
 }
 
-// ---------------------------------------------------------------- gradient
-
-constexpr int kDistillU = 2;
+// ---------------------------------------------------------------- gradient by slices
 
 // A factor of 0 takes an infinity away.
 __device__ __forceinline__ double weighed(double w, double x) { return w == 0.0 ? 0.0 : w * x; }
 
-// Slice s of a gradient row, 256 kDistillU pieces; workgroup 0: the sums over
-// the rows.
+// The sums over rows, by one workgroup (fixed order).
+template <class Load>
+__device__ __forceinline__ void put_distill_stats(const Logits& in, const DistillArgs& a, double (*s_w)[4], float* stats,
+                                                  Load load)
+{
+    double x[4] = {0.0, 0.0, 0.0, 0.0};
+    const double soft = 1.0 - (double)a.hard;
+    for (uint64_t t = threadIdx.x; t < in.rows; t += blockDim.x) {
+        if (!distilled(in, a, t)) continue;
+        const DistillTerms d = load(t);
+        const double w = a.weight ? (double)a.weight[t] : 1.0;
+        x[0] += w * (weighed(soft, (double)d.div) + weighed((double)a.hard, (double)d.nll));
+        x[1] += w * (double)d.div;
+        x[2] += w * (double)d.nll;
+        x[3] += w * (double)d.covered;
+    }
+    block_sum(x, s_w, 4);
+    if (threadIdx.x == 0)
+        for (int i = 0; i < 4; ++i) stats[i] = (float)x[i];
+}
+__global__ void __launch_bounds__(1024) k_distill_stats(Logits in, DistillArgs a, const DistillTerms* terms, float* stats)
+{
+    __shared__ double s_w[16][4];
+    put_distill_stats(in, a, s_w, stats, [&](uint64_t t) { return terms[t]; });
+}
+
+constexpr int kDistillU = 2;
+constexpr uint32_t kTable = 1024;  // places for a list's tokens, to find repeats
+
+// Slice s of a gradient row, 256 kDistillU pieces; every workgroup finds its
+// row's terms, a row's first writes them, and the last of these to finish sums
+// them up.  (Without a gradient: G == 1, nothing but that.)
 template <int TYPE>
-__global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, uint32_t G, float c,
-                                                      const DistillRow* terms, float* stats, void* dlogits, uint64_t ldd)
+__global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, uint32_t S, uint32_t G, float c,
+                                                      const Part* part, const float* at_list, const float* at_label,
+                                                      DistillTerms* terms, uint32_t* ticket, float* div, float* stats,
+                                                      void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     constexpr int N = Piece<TYPE>::N, U = kDistillU;
     __shared__ double s_w[4][4];
-    __shared__ uint32_t s_id[kMaxTop], s_n[4];
-    __shared__ uint8_t s_given;
+    __shared__ List s_list;
+    __shared__ uint32_t s_table[kTable], s_last;
     const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
-    if (blockIdx.x == 0) {
-        double x[4] = {0.0, 0.0, 0.0, 0.0};
-        for (uint64_t t = tid; t < in.rows; t += 256) {
-            const DistillRow& w = terms[t];
-            if (!distilled(in, a, t)) continue;
-            const double weight = a.weight ? (double)a.weight[t] : 1.0, soft = 1.0 - (double)a.hard;
-            x[0] += weight * (weighed(soft, (double)w.div) + weighed((double)a.hard, (double)w.nll));
-            x[1] += weight * (double)w.div;
-            x[2] += weight * (double)w.nll;
-            x[3] += weight * (double)w.covered;
-        }
-        block_sum(x, s_w, 4);
-        if (tid == 0)
-            for (int i = 0; i < 4; ++i) stats[i] = (float)x[i];
-        return;
-    }
-    for (uint64_t b = blockIdx.x - 1; b < in.rows * G; b += gridDim.x - 1) {
+    bool last = false;
+    for (uint64_t b = blockIdx.x; b < in.rows * G; b += gridDim.x) {
         const uint64_t t = b / G;
         const uint32_t s = (uint32_t)(b % G);
         const E* row = static_cast<const E*>(in.x) + t * in.ld;
         E* out = static_cast<E*>(dlogits) + t * ldd;
-        const RowCut<TYPE> r(row, V);
+        const RowCut<TYPE> r(row, dlogits ? V : 0);
         const uint32_t first = min(r.full, s * (256 * U)), end = min(r.full, first + 256 * U);
         const bool use = distilled(in, a, t);
-        const DistillRow w = terms[t];
-        const uint32_t label = in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu;
-        auto inside = [&](uint32_t v) {
-            if (v >= V) return false;
-            if (!r.in_piece(v)) return s == 0;
-            return (v - r.head) / N >= first && (v - r.head) / N < end;
-        };
-        Entry e(a, t, tid, V);
-        const bool mine = use && inside(e.v);
-        const float x = mine ? (float)row[e.v] : -INFINITY;
-        const float at = use && inside(label) ? (float)row[label] : -INFINITY;
-        const float single = use && s == 0 && tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
+        float single = -INFINITY;
         Piece<TYPE> y[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             y[u].none();
             if (use && first + tid + 256 * u < end) y[u].w = load_vec<u32x4>(row + r.piece(first + tid + 256 * u));
         }
-        // the slice's part of the list, in its order
-        const uint64_t mask = __ballot(mine);
-        if ((tid & 63) == 0) s_n[tid >> 6] = (uint32_t)__popcll(mask);
-        if (tid == 0) s_given = 0;
-        // (in place, what is read above lies before what is written below)
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        uint32_t before = 0, count = 0;
-        for (uint32_t q = 0; q < 4; ++q) {
-            if (q < tid >> 6) before += s_n[q];
-            count += s_n[q];
+        if (use && s == 0 && tid < r.singles) single = (float)row[r.single(tid)];
+        DistillTerms d = {0.0f, 0.0f, 0.0f};
+        if (use) {
+            const Entry e(a, t, tid, V);
+            for (uint32_t i = tid; i < kTable; i += 256) s_table[i] = 0xFFFFFFFFu;
+            s_list.id[tid] = e.v;
+            s_list.value[tid] = e.value;
+            if (tid < a.count) s_list.x[tid] = at_list[t * a.count + tid];
+            if (tid == 0) s_list.dup = 0;
+            __syncthreads();
+            if (e.v < V)
+                for (uint32_t h = e.v * 2654435761u >> 22;; h = (h + 1) % kTable) {  // (a quarter of them are taken at most)
+                    const uint32_t was = atomicCAS(&s_table[h], 0xFFFFFFFFu, e.v);
+                    if (was == e.v) s_list.dup = 1;
+                    if (was == e.v || was == 0xFFFFFFFFu) break;
+                }
+            __syncthreads();
+            s_list.drop_repeats(a.count);
+            if (tid < 64) {
+                const Part rest = join_slices(part + t * S, S, 64, c);
+                d = list_terms(in, a, t, rest, at_label[t], s_list);
+            }
+            __syncthreads();
         }
-        const uint32_t place = before + (uint32_t)__popcll(mask & ((1ull << (tid & 63)) - 1));
-        if (mine) s_id[place] = e.v;
-        auto off = [&](float v) { return w.A == 0.0f ? 0.0f : entry(v, c, w.rest_top, w.A); };
+        if (s == 0 && tid == 0) {
+            div[t] = d.div;
+            // (device-scope accesses, each done before the next)
+            float* w = &terms[t].div;
+            for (int i = 0; i < 3; ++i)
+                __hip_atomic_store(w + i, i == 0 ? d.div : i == 1 ? d.nll : d.covered, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            last = atomicAdd(ticket, 1u) == (uint32_t)in.rows - 1;
+        }
+        if (!dlogits) {
+            __syncthreads();
+            continue;
+        }
+        const float A = use ? s_list.row.A : 0.0f, top = use ? s_list.row.top : 0.0f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float z[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) z[i] = off(y[u].get(i));
+            for (int i = 0; i < N; ++i) z[i] = A == 0.0f ? 0.0f : entry(y[u].get(i), c, top, A);
             y[u].put(z);
             if (first + tid + 256 * u < end) store_vec(out + r.piece(first + tid + 256 * u), y[u].w);
         }
-        if (s == 0 && tid < r.singles) out[r.single(tid)] = (E)off(single);
+        if (s == 0 && tid < r.singles) out[r.single(tid)] = (E)(A == 0.0f ? 0.0f : entry(single, c, top, A));
         // (every store before this is done before the next ones begin)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const float given = w.k * w.hard;
-        if (mine) {
-            bool lead = true;
-            for (uint32_t i = 0; i < place; ++i) lead &= s_id[i] != e.v;
-            if (lead) {
-                out[e.v] = (E)(listed_entry(a, w, e.value, x, in.scale) - (e.v == label ? given : 0.0f));
-                if (e.v == label) s_given = 1;
-            }
+        if (use) {
+            auto inside = [&](uint32_t v) {
+                if (v >= V) return false;
+                if (!r.in_piece(v)) return s == 0;
+                return (v - r.head) / N >= first && (v - r.head) / N < end;
+            };
+            if (tid < a.count && inside(s_list.id[tid])) out[s_list.id[tid]] = (E)s_list.grad[tid];
+            const float given = s_list.row.given;
+            if (tid == 0 && given == given && inside((uint32_t)in.label[t])) out[in.label[t]] = (E)given;
         }
         __syncthreads();
-        if (tid == 0 && at != -INFINITY && !s_given) out[label] = (E)(off(at) - given);
-        __syncthreads();
     }
+    if (tid == 0) s_last = last;
+    __syncthreads();
+    if (!s_last) return;
+    put_distill_stats(in, a, s_w, stats, [&](uint64_t t) {
+        float w[3];
+        for (int i = 0; i < 3; ++i)
+            w[i] = __hip_atomic_load(&terms[t].div + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return DistillTerms{w[0], w[1], w[2]};
+    });
 }
 
 // ---------------------------------------------------------------- host
 
 constexpr uint32_t kDistillGrid = 1u << 22;
-constexpr uint64_t kDistillSlices = 1024;  // of few rows together
+constexpr uint64_t kDistillSlices = 1024;   // of few rows together
+constexpr uint64_t kDistillMany = 128;      // from so many rows on, a workgroup a row,
+constexpr uint64_t kMarked = 5 * 32768;     // of at most so many logits
+constexpr uint64_t kDistillRows = 1u << 21; // of a launch with a workgroup a row (fewer than 2^32 threads)
+constexpr uint32_t kDistillHold = 8, kDistillHoldLds = 3;
 
 struct DistillCut {
     uint32_t S, W, G;
+    uint64_t pieces;
+    bool many;
 };
 uint64_t most_rest_slices(uint64_t pieces) { return std::min<uint64_t>(64, (pieces + 511) / 512); }
 DistillCut cut_distill(uint64_t rows, uint64_t vocab, uint32_t type)
 {
     DistillCut r;
-    const uint64_t pieces = vocab / (type == kF32 ? 4 : 8) + 1;
+    r.pieces = vocab / (type == kF32 ? 4 : 8) + 1;
+    r.many = rows >= kDistillMany && vocab <= kMarked;
     const uint64_t want = kDistillSlices / std::min(rows, kDistillSlices);
-    const uint64_t S = std::max<uint64_t>(1, std::min(most_rest_slices(pieces), want));
-    r.W = (uint32_t)((pieces + S - 1) / S);
-    r.S = (uint32_t)((pieces + r.W - 1) / r.W);
-    r.G = (uint32_t)((pieces + 256 * kDistillU - 1) / (256 * kDistillU));
+    const uint64_t S = std::max<uint64_t>(1, std::min(most_rest_slices(r.pieces), want));
+    r.W = (uint32_t)((r.pieces + S - 1) / S);
+    r.S = (uint32_t)((r.pieces + r.W - 1) / r.W);
+    r.G = (uint32_t)((r.pieces + 256 * kDistillU - 1) / (256 * kDistillU));
     return r;
 }
 
 struct DistillSpace {
+    DistillTerms* terms;
+    uint32_t* ticket;
     Part* part;
-    DistillRow* terms;
+    float *at_list, *at_label;
 };
-DistillSpace carve_distill(void* ws, uint64_t rows, uint64_t parts, size_t* bytes)
+DistillSpace carve_distill(void* ws, uint64_t rows, uint64_t sliced, uint64_t parts, uint32_t count, size_t* bytes)
 {
     Carve c(ws);
     DistillSpace r;
+    r.terms = c.take<DistillTerms>(rows);
+    r.ticket = c.take<uint32_t>(1);
     r.part = c.take<Part>(parts);
-    r.terms = c.take<DistillRow>(rows);
+    r.at_list = c.take<float>(sliced * count);
+    r.at_label = c.take<float>(sliced);
     if (bytes) *bytes = c.used;
     return r;
 }
@@ -387,35 +620,68 @@ DistillSpace carve_distill(void* ws, uint64_t rows, uint64_t parts, size_t* byte
 }  // namespace
 
 // (Enough for every type and every call of fewer rows, a smaller vocabulary or
-// shorter lists.)
-size_t distill_workspace(uint32_t, uint64_t rows, uint64_t vocab)
+// shorter lists: what is counted are the rows that may go by slices.)
+size_t distill_workspace(uint32_t count, uint64_t rows, uint64_t vocab)
 {
     size_t b = 0;
-    const uint64_t parts = std::max(rows, std::min(kDistillSlices, rows * most_rest_slices(vocab / 4 + 1)));
-    carve_distill(nullptr, rows, parts, &b);
+    const uint64_t sliced = vocab > kMarked ? rows : std::min(rows, kDistillMany - 1);
+    const uint64_t parts = std::max(sliced, std::min(kDistillSlices, sliced * most_rest_slices(vocab / 4 + 1)));
+    carve_distill(nullptr, rows, sliced, parts, count, &b);
     return b;
 }
 
-hipError_t distill_run(const Logits& in, const DistillArgs& a, float* div, float* stats, void* dlogits, uint64_t ldd,
+hipError_t distill_run(const Logits& in0, const DistillArgs& a0, float* div, float* stats, void* dlogits, uint64_t ldd,
                        void* ws, hipStream_t s)
 {
+    Logits in = in0;
+    DistillArgs a = a0;
     const DistillCut cut = cut_distill(in.rows, in.vocab, in.type);
-    const DistillSpace sp = carve_distill(ws, in.rows, in.rows * cut.S, nullptr);
     const float c = in.scale * kLog2e;
-    const uint32_t slices = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kDistillGrid);
-    const uint32_t rows = (uint32_t)std::min<uint64_t>(in.rows, kDistillGrid);
-    const uint32_t grads = dlogits ? (uint32_t)std::min<uint64_t>(in.rows * cut.G, kDistillGrid) : 0;
+    if (!cut.many) {
+        const DistillSpace sp = carve_distill(ws, in.rows, in.rows, in.rows * cut.S, a.count, nullptr);
+        const uint32_t slices = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kDistillGrid);
+        const uint32_t G = dlogits ? cut.G : 1, grads = (uint32_t)std::min<uint64_t>(in.rows * G, kDistillGrid);
+        by_type(in.type, [&](auto ty) {
+            constexpr int TY = decltype(ty)::value;
+            timer_begin(kTLossRows, s);
+            hipLaunchKernelGGL((k_rest_slices<TY>), dim3(slices), dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part, sp.at_list,
+                               sp.at_label, sp.ticket);
+            timer_end(kTLossRows, s);
+            timer_begin(kTLossGrad, s);
+            hipLaunchKernelGGL((k_distill_grad<TY>), dim3(grads), dim3(256), 0, s, in, a, cut.S, G, c, sp.part, sp.at_list,
+                               sp.at_label, sp.terms, sp.ticket, div, stats, dlogits, ldd);
+            timer_end(kTLossGrad, s);
+        });
+        return hipGetLastError();
+    }
+    const DistillSpace sp = carve_distill(ws, in.rows, 0, 0, a.count, nullptr);
+    const uint64_t most = cut.pieces <= 1024 * kDistillHold ? 512 : 1024, size = in.type == kF32 ? 4 : 2;
+    const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kDistillHold * 64 - 1) / (kDistillHold * 64) * 64);
+    const size_t lds = (in.vocab + 31) / 32 * 4 + 4;
+    timer_begin(kTLossRows, s);
     by_type(in.type, [&](auto ty) {
         constexpr int TY = decltype(ty)::value;
-        timer_begin(kTLossRows, s);
-        hipLaunchKernelGGL((k_rest_slices<TY>), dim3(slices), dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part);
-        timer_end(kTLossRows, s);
-        timer_begin(kTLossGrad, s);
-        hipLaunchKernelGGL((k_distill_terms<TY>), dim3(rows), dim3(256), 0, s, in, a, cut.S, c, sp.part, sp.terms, div);
-        hipLaunchKernelGGL((k_distill_grad<TY>), dim3(grads + 1), dim3(256), 0, s, in, a, cut.G, c, sp.terms, stats, dlogits,
-                           ldd);
-        timer_end(kTLossGrad, s);
+        for (uint64_t r0 = 0; r0 < in0.rows; r0 += kDistillRows) {
+            const dim3 grid((uint32_t)std::min(in0.rows - r0, kDistillRows)), block((uint32_t)std::min(threads, most));
+            in.x = static_cast<const uint8_t*>(in0.x) + r0 * in.ld * size;
+            in.label = in0.label ? in0.label + r0 : nullptr;
+            a.id = a0.id + r0 * a.ld;
+            a.value = static_cast<const uint8_t*>(a0.value) + r0 * a.ld * (a.type == kF32 ? 4 : 2);
+            a.weight = a0.weight ? a0.weight + r0 : nullptr;
+            void* d = dlogits ? static_cast<uint8_t*>(dlogits) + r0 * ldd * size : nullptr;
+            auto go = [&](auto kern) {
+                hipLaunchKernelGGL(kern, grid, block, lds, s, in, a, c, div + r0, sp.terms + r0, d, ldd);
+            };
+            if (most == 512)
+                go(k_distill_row<TY, 512, kDistillHold, 0, false>);
+            else
+                go(k_distill_row<TY, 1024, kDistillHold, kDistillHoldLds, false>);
+        }
     });
+    timer_end(kTLossRows, s);
+    timer_begin(kTLossGrad, s);
+    hipLaunchKernelGGL(k_distill_stats, dim3(1), dim3(1024), 0, s, in0, a0, sp.terms, stats);
+    timer_end(kTLossGrad, s);
     return hipGetLastError();
 }
 
