@@ -118,102 +118,165 @@ __device__ __forceinline__ double wave_sum(double x)
     return x;
 }
 
-// A list in LDS: its tokens, the teacher's values, the student's logits, and
-// from the row's terms on the tokens' gradients.
+// LDS accesses of one wave before and behind this keep their order.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A row's list in LDS, made by one wave: entries lane, lane + 64, ...  What
+// depends on the list alone (take, prepare) is there before the row's sum, so
+// that little is left to do behind it (finish).
 struct List {
     uint32_t id[kMaxTop], dup;
-    float value[kMaxTop], x[kMaxTop], grad[kMaxTop];
+    float value[kMaxTop], x[kMaxTop];  // the teacher's value, the student's logit
+    float q[kMaxTop], e[kMaxTop];      // the teacher's probability; e^(scale (x - top)), then the token's gradient
     DistillRow row;
-    // Entries that repeat an earlier one (found by whoever sets dup) go; every
-    // thread of the workgroup takes part.
+    DistillTerms terms;
+
+    __device__ __forceinline__ bool there(uint32_t i, uint32_t V) const { return id[i] < V; }
+    // Entries that repeat an earlier one go (dup: there is one).
     __device__ __forceinline__ void drop_repeats(uint32_t count)
     {
+        wave_fence();
         if (!dup) return;
         uint32_t again = 0;
-        for (uint32_t i = threadIdx.x, k = 0; i < count; i += blockDim.x, ++k)
+        for (uint32_t i = threadIdx.x & 63, k = 0; i < count; i += 64, ++k)
             for (uint32_t j = 0; j < i; ++j) again |= (uint32_t)(id[j] == id[i]) << k;
-        __syncthreads();
-        for (uint32_t i = threadIdx.x, k = 0; i < count; i += blockDim.x, ++k)
+        wave_fence();
+        for (uint32_t i = threadIdx.x & 63, k = 0; i < count; i += 64, ++k)
             if (again >> k & 1u) id[i] = 0xFFFFFFFFu;
-        __syncthreads();
+        wave_fence();
     }
 };
 
-// A row's terms and its list's gradients, by one wave: from the sum over the
-// unlisted tokens and the given token's logit.
-__device__ __forceinline__ DistillTerms list_terms(const Logits& in, const DistillArgs& a, uint64_t t, const Part& rest,
-                                                   float at, List& list)
+// Sums over a list: its largest logit (0: there is none), ln q = value ts - off,
+// Q = sum q, QF the same without tokens of -Inf, Z = sum e, and of the products
+// with logarithms those that beta needs (u against lq, w against scale (x - top)).
+struct ListSums {
+    float top;
+    double ts, off, Q, QF, Z, u, w;
+};
+__device__ __forceinline__ ListSums prepare_list(const DistillArgs& a, double scale, uint32_t V, List& list)
 {
-    const uint32_t lane = threadIdx.x & 63, V = (uint32_t)in.vocab;
-    const double scale = (double)in.scale, ts = a.rest ? 1.0 : (double)a.teacher_scale;
-    float M = rest.sum == 0.0f ? -INFINITY : rest.top, best = -INFINITY;
+    const uint32_t lane = threadIdx.x & 63;
+    ListSums s = {-INFINITY, a.rest ? 1.0 : (double)a.teacher_scale, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
+    float best = -INFINITY;
     for (uint32_t i = lane; i < a.count; i += 64)
-        if (list.id[i] < V) {
+        if (list.there(i, V)) {
+            s.top = fmaxf(s.top, list.x[i]);
             best = fmaxf(best, list.value[i]);
-            M = fmaxf(M, list.x[i]);
         }
-    M = wave_join<false>(M);
+    s.top = wave_join<false>(s.top);
     best = a.rest ? 0.0f : wave_join<false>(best);
-    const float top = M == -INFINITY ? 0.0f : M;
-    double q = 0.0, near = 0.0;
+    const float top = s.top == -INFINITY ? 0.0f : s.top;
 #pragma unroll 1
     for (uint32_t i = lane; i < a.count; i += 64)
-        if (list.id[i] < V) {
-            q += exp64(((double)list.value[i] - (double)best) * ts);
-            near += exp64(((double)list.x[i] - (double)top) * scale);
+        if (list.there(i, V)) {
+            const double q = exp64(((double)list.value[i] - (double)best) * s.ts);
+            const double e = exp64(((double)list.x[i] - (double)top) * scale);
+            list.q[i] = (float)q;
+            list.e[i] = (float)e;
+            s.Q += q;
+            s.QF += list.x[i] == -INFINITY ? 0.0 : q;
+            s.Z += e;
         }
-    q = wave_sum(q);
-    near = wave_sum(near);
-    // the teacher's log probabilities: value ts - off
-    const double off = !a.rest && q != 0.0 ? (double)best * ts + ln64(q) : 0.0;
-    const double far = ((double)rest.top - (double)top) * scale;
-    const double outside = rest.sum == 0.0f ? 0.0 : exp64(far) * (double)rest.sum;
-    const double total = outside + near, ln = ln64(total);
-    double div = 0.0, F = 0.0, covered = 0.0;
-#pragma unroll 1
+    s.Q = wave_sum(s.Q);
+    s.QF = wave_sum(s.QF);
+    s.Z = wave_sum(s.Z);
+    double each = 1.0;
+    if (!a.rest && s.Q != 0.0) {
+        s.off = (double)best * s.ts + ln64(s.Q);
+        each = 1.0 / s.Q;
+        s.QF *= each;
+        s.Q = 1.0;
+    }
+    const bool back = a.beta == 1.0f;  // (otherwise only beta == 0 has a use for these)
     for (uint32_t i = lane; i < a.count; i += 64)
-        if (list.id[i] < V) {
-            const double lp = ((double)list.x[i] - (double)top) * scale - ln;
-            const Share s = share_of(a.beta, (double)list.value[i] * ts - off, lp);
-            div += s.div;
-            F += s.f;
-            covered += exp64(lp);
+        if (list.there(i, V)) {
+            const double q = (double)list.q[i] * each, p = back ? (double)list.e[i] : q;
+            list.q[i] = (float)q;
+            s.u += product(p, (double)list.value[i] * s.ts - s.off);
+            s.w += product(p, ((double)list.x[i] - (double)top) * scale);
         }
-    div = wave_sum(div);
-    F = wave_sum(F);
-    covered = wave_sum(covered);
+    s.u = wave_sum(s.u);
+    s.w = wave_sum(s.w);
+    return s;
+}
+
+// A row's terms and its list's gradients from the sum over the unlisted tokens,
+// by the same wave; at: the given token's logit, label the token or none.
+__device__ __forceinline__ void finish_list(const DistillArgs& a, double scale, uint32_t V, const ListSums& s,
+                                            const Part& rest, uint32_t label, float at, double weight, List& list)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const bool outside = rest.sum != 0.0f;
+    const float M = fmaxf(s.top, outside ? rest.top : -INFINITY);
+    if (M == -INFINITY) {  // nothing but -Inf
+        for (uint32_t i = lane; i < a.count; i += 64) list.e[i] = 0.0f;
+        if (lane == 0) {
+            list.row = DistillRow{0.0f, 0.0f, __builtin_nanf("")};
+            list.terms = DistillTerms{0.0f, 0.0f, 0.0f};
+        }
+        return;
+    }
+    // against M: the list's part, the rest's; ln p = scale (x - top) - ln
+    const float top = s.top == -INFINITY ? M : s.top;
+    const double step = ((double)top - (double)M) * scale, far = outside ? ((double)rest.top - (double)M) * scale : 0.0;
+    const double g = exp64(step), h = outside ? exp64(far) : 0.0;
+    const double total = g * s.Z + h * (double)rest.sum, all = ln64(total), ln = all - step, one = g / total;
+    double div, F;
+    if (a.beta == 0.0f) {
+        div = s.u - s.w + ln * s.Q;
+        F = -s.QF;
+    } else if (a.beta == 1.0f) {
+        div = F = one * (s.w - s.u - ln * s.Z);
+    } else {
+        div = F = 0.0;
+        const double b = (double)a.beta;
+#pragma unroll 1
+        for (uint32_t i = lane; i < a.count; i += 64)
+            if (list.there(i, V)) {
+                const double lp = ((double)list.x[i] - (double)top) * scale - ln, q = (double)list.q[i];
+                const double p = (double)list.e[i] * one, lm = ln64(b * q + (1.0 - b) * p);
+                const double f = (1.0 - b) * product(p, lp - lm);
+                div += b * product(q, (double)list.value[i] * s.ts - s.off - lm) + f;
+                F += f;
+                list.q[i] = (float)f;
+            }
+        div = wave_sum(div);
+        F = wave_sum(F);
+    }
     Share out = {0.0, 0.0};
-    if (a.rest && rest.sum != 0.0f)
-        out = share_of(a.beta, ln64(fmax(1.0 - q, 0x1p-24)), far + part_ln(rest.sum) - ln);
+    if (a.rest && outside) out = share_of(a.beta, ln64(fmax(1.0 - s.Q, 0x1p-24)), far + part_ln(rest.sum) - all);
     div += out.div;
     F += out.f;
-    const bool some = total != 0.0;  // (a row of nothing but -Inf adds nothing)
-    const double soft = 1.0 - (double)a.hard, hard = in.label && at != -INFINITY ? (double)a.hard : 0.0;
-    const double k0 = (double)within((float)((a.weight ? (double)a.weight[t] : 1.0) * (double)a.grad_scale * scale));
-    const uint32_t label = in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu;
+    const double soft = 1.0 - (double)a.hard, hard = at != -INFINITY ? (double)a.hard : 0.0;
+    const double k0 = (double)within((float)(weight * (double)a.grad_scale * scale));
+    const double both = hard - soft * F;
     bool listed = false;
-#pragma unroll 1
     for (uint32_t i = lane; i < a.count; i += 64)
-        if (list.id[i] < V) {
-            const double lp = ((double)list.x[i] - (double)top) * scale - ln;
-            const Share s = share_of(a.beta, (double)list.value[i] * ts - off, lp);
+        if (list.there(i, V)) {
+            const double p = (double)list.e[i] * one;
+            double f = a.beta == 0.0f ? list.x[i] == -INFINITY ? 0.0 : -(double)list.q[i] : (double)list.q[i];
+            if (a.beta == 1.0f)
+                f = product(p, ((double)list.x[i] - (double)top) * scale - ln - ((double)list.value[i] * s.ts - s.off));
             const bool given = list.id[i] == label;
-            const double g = soft * s.f + exp64(lp) * (hard - soft * F) - (given ? hard : 0.0);
-            list.grad[i] = some ? within((float)(k0 * g)) : 0.0f;
+            list.e[i] = within((float)(k0 * (soft * f + p * both - (given ? hard : 0.0))));
             listed |= given;
         }
     listed = __any(listed);
     if (lane == 0) {
-        const double A = rest.sum == 0.0f ? 0.0 : k0 * (soft * out.f / (double)rest.sum + (hard - soft * F) * exp64(far) / total);
-        const float A32 = within((float)A);
+        const float A = outside ? within((float)(k0 * (soft * out.f / (double)rest.sum + both * h / total))) : 0.0f;
         // (NaN where the token has its place on the list, or none)
         const float given = listed || hard == 0.0
                                 ? __builtin_nanf("")
-                                : within((float)(A32 * exp64(((double)at - (double)rest.top) * scale) - k0 * hard));
-        list.row = some ? DistillRow{A32, rest.top, given} : DistillRow{0.0f, 0.0f, __builtin_nanf("")};
+                                : within((float)((double)A * exp64(((double)at - (double)rest.top) * scale) - k0 * hard));
+        list.row = DistillRow{A, rest.top, given};
+        const double nll = label < V ? all - ((double)at - (double)M) * scale : 0.0;
+        list.terms = DistillTerms{(float)div, (float)nll, (float)(s.Z * one)};
     }
-    const double nll = in.label ? ln - ((double)at - (double)top) * scale : 0.0;
-    return some ? DistillTerms{(float)div, (float)nll, (float)covered} : DistillTerms{0.0f, 0.0f, 0.0f};
 }
 
 // Marks of a piece's elements (a bit each) and what is left of the piece
@@ -302,11 +365,12 @@ __global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, u
 
 // ---------------------------------------------------------------- a workgroup a row
 
-// Row blockIdx.x by one workgroup, as k_row takes it (the first NV pieces of a
-// thread in registers between the passes, LP more in LDS, the rest read once
-// more): the marks of its list, the sum over the unlisted tokens, by the first
-// wave the list's terms (four entries a lane) and the row's coefficient, the
-// gradient, and behind it the listed and the given token's places once more.
+// Row blockIdx.x by one workgroup, whose first wave has the list, and the others
+// the row, as k_row takes it (the first NV pieces of a thread in registers
+// between the passes, LP more in LDS, the rest read once more): the list's
+// marks, the sum over the unlisted tokens beside the list's own sums, the row's
+// terms, the gradient, and behind it the listed and the given token's places
+// once more.
 template <int TYPE, int THREADS, int NV, int LP, bool KEEP>
 __global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(8)))
 k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms, void* dlogits, uint64_t ldd)
@@ -314,16 +378,16 @@ k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms
     typedef typename Elem<TYPE>::type E;
     constexpr int N = Piece<TYPE>::N;
     extern __shared__ uint32_t s_marks[];
-    __shared__ u32x4 s_keep[LP ? LP * THREADS : 1];
+    __shared__ u32x4 s_keep[LP ? LP * (THREADS - 64) : 1];
     __shared__ Part s_part[THREADS / 64];
     __shared__ uint32_t s_single[4];
     __shared__ List s_list;
     const uint64_t t = blockIdx.x;
-    const uint32_t V = (uint32_t)in.vocab, tid = threadIdx.x, step = blockDim.x, lane = tid & 63;
+    const uint32_t V = (uint32_t)in.vocab, lane = threadIdx.x & 63;
     const E* row = static_cast<const E*>(in.x) + t * in.ld;
     E* out = static_cast<E*>(dlogits) + t * ldd;
     if (!distilled(in, a, t)) {
-        if (tid == 0) {
+        if (threadIdx.x == 0) {
             div[t] = 0.0f;
             terms[t] = DistillTerms{0.0f, 0.0f, 0.0f};
         }
@@ -331,6 +395,54 @@ k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms
         return;
     }
     const RowCut<TYPE> r(row, V);
+    const uint32_t words = (r.full * N + 31) / 32;
+    for (uint32_t i = threadIdx.x; i < words; i += blockDim.x) s_marks[i] = 0;
+    if (threadIdx.x < 4) s_single[threadIdx.x] = 0;
+    if (threadIdx.x == 4) s_list.dup = 0;
+    // (a branch of whole waves: both sides have their own barriers, five each, or
+    // three without a gradient)
+    if ((uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x) < 64) {
+        const double scale = (double)in.scale;
+        for (uint32_t i = lane; i < a.count; i += 64) {
+            const Entry e(a, t, i, V);
+            s_list.id[i] = e.v;
+            s_list.value[i] = e.value;
+        }
+        __syncthreads();
+        for (uint32_t i = lane; i < a.count; i += 64) {
+            const uint32_t v = s_list.id[i];
+            if (v >= V) continue;
+            const bool in_piece = r.in_piece(v);
+            const uint32_t bit = in_piece ? v - r.head : v < r.head ? v : v - r.full * N;
+            uint32_t* word = (in_piece ? s_marks : s_single) + bit / 32;
+            if (atomicOr(word, 1u << (bit % 32)) >> (bit % 32) & 1u) s_list.dup = 1;
+        }
+        __syncthreads();
+        s_list.drop_repeats(a.count);
+        for (uint32_t i = lane; i < a.count; i += 64) {
+            const uint32_t v = s_list.id[i];
+            if (v < V) s_list.x[i] = (float)row[v];
+        }
+        const uint32_t label = in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu;
+        const float at = in.label ? (float)row[label] : -INFINITY;
+        const double weight = a.weight ? (double)a.weight[t] : 1.0;
+        const ListSums sums = prepare_list(a, scale, V, s_list);
+        __syncthreads();
+        finish_list(a, scale, V, sums, join_slices(s_part, blockDim.x / 64 - 1, 64, c), label, at, weight, s_list);
+        wave_fence();
+        if (lane == 0) {
+            div[t] = s_list.terms.div;
+            terms[t] = s_list.terms;
+        }
+        if (!dlogits) return;
+        __syncthreads();
+        __syncthreads();
+        for (uint32_t i = lane; i < a.count; i += 64)
+            if (s_list.id[i] < V) out[s_list.id[i]] = (E)s_list.e[i];
+        if (lane == 0 && s_list.row.given == s_list.row.given) out[label] = (E)s_list.row.given;
+        return;
+    }
+    const uint32_t tid = threadIdx.x - 64, step = blockDim.x - 64;
     const int used = (int)min((r.full + step - 1) / step, (uint32_t)NV);
     Piece<TYPE> x[NV];
 #pragma unroll
@@ -339,27 +451,8 @@ k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms
         if (tid + step * j < r.full) x[j].w = load_vec<u32x4, KEEP>(row + r.piece(tid + step * j));
     }
     float single = tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
-    // the list's marks
-    const uint32_t words = (r.full * N + 31) / 32;
-    for (uint32_t i = tid; i < words; i += step) s_marks[i] = 0;
-    if (tid < 4) s_single[tid] = 0;
-    if (tid == 4) s_list.dup = 0;
     __syncthreads();
-    for (uint32_t i = tid; i < a.count; i += step) {
-        const Entry e(a, t, i, V);
-        s_list.id[i] = e.v;
-        s_list.value[i] = e.value;
-        if (e.v < V) {
-            s_list.x[i] = (float)row[e.v];
-            const bool in_piece = r.in_piece(e.v);
-            const uint32_t bit = in_piece ? e.v - r.head : e.v < r.head ? e.v : e.v - r.full * N;
-            uint32_t* word = (in_piece ? s_marks : s_single) + bit / 32;
-            if (atomicOr(word, 1u << (bit % 32)) >> (bit % 32) & 1u) s_list.dup = 1;
-        }
-    }
     __syncthreads();
-    s_list.drop_repeats(a.count);
-    const float at = tid < 64 && in.label ? (float)row[in.label[t]] : -INFINITY;
     if (tid < r.singles && s_single[tid / 32] >> (tid % 32) & 1u) single = -INFINITY;
     Own own = {single, single == -INFINITY ? 0.0f : 1.0f};
     for (uint32_t j = tid + step * NV, slot = tid; j < r.full; j += step, slot += step) {
@@ -384,21 +477,12 @@ k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms
         if (lane == 0) s_part[tid >> 6] = Part{top, sum};
     }
     __syncthreads();
-    if (tid < 64) {
-        // a lane a wave's part
-        const Part rest = join_slices(s_part, step / 64, 64, c);
-        const DistillTerms d = list_terms(in, a, t, rest, at, s_list);
-        if (tid == 0) {
-            div[t] = d.div;
-            terms[t] = d;
-        }
-    }
-    __syncthreads();
     if (!dlogits) return;
-    const float A = s_list.row.A, top = s_list.row.top;
     uint32_t j = tid + step * (NV + LP);
     Piece<TYPE> next;
     if (j < r.full) next.w = load_vec<u32x4>(row + r.piece(j));
+    __syncthreads();
+    const float A = s_list.row.A, top = s_list.row.top;
     auto write = [&](Piece<TYPE>& q, uint32_t at) {
         q.repack();
         float z[N];
@@ -426,9 +510,6 @@ k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms
     // (every store before this is done before the next ones begin)
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    for (uint32_t i = tid; i < a.count; i += step)
-        if (s_list.id[i] < V) out[s_list.id[i]] = (E)s_list.grad[i];
-    if (tid == 0 && s_list.row.given == s_list.row.given) out[in.label[t]] = (E)s_list.row.given;
 }
 
 // ---------------------------------------------------------------- gradient by slices
@@ -499,12 +580,12 @@ __global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, 
         if (use && s == 0 && tid < r.singles) single = (float)row[r.single(tid)];
         DistillTerms d = {0.0f, 0.0f, 0.0f};
         if (use) {
-            const Entry e(a, t, tid, V);
             for (uint32_t i = tid; i < kTable; i += 256) s_table[i] = 0xFFFFFFFFu;
+            if (tid == 0) s_list.dup = 0;
+            const Entry e(a, t, tid, V);
             s_list.id[tid] = e.v;
             s_list.value[tid] = e.value;
             if (tid < a.count) s_list.x[tid] = at_list[t * a.count + tid];
-            if (tid == 0) s_list.dup = 0;
             __syncthreads();
             if (e.v < V)
                 for (uint32_t h = e.v * 2654435761u >> 22;; h = (h + 1) % kTable) {  // (a quarter of them are taken at most)
@@ -513,12 +594,15 @@ __global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, 
                     if (was == e.v || was == 0xFFFFFFFFu) break;
                 }
             __syncthreads();
-            s_list.drop_repeats(a.count);
             if (tid < 64) {
-                const Part rest = join_slices(part + t * S, S, 64, c);
-                d = list_terms(in, a, t, rest, at_label[t], s_list);
+                s_list.drop_repeats(a.count);
+                const double scale = (double)in.scale;
+                const ListSums sums = prepare_list(a, scale, V, s_list);
+                finish_list(a, scale, V, sums, join_slices(part + t * S, S, 64, c), in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu,
+                            at_label[t], a.weight ? (double)a.weight[t] : 1.0, s_list);
             }
             __syncthreads();
+            d = s_list.terms;
         }
         if (s == 0 && tid == 0) {
             div[t] = d.div;
@@ -553,7 +637,7 @@ __global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, 
                 if (!r.in_piece(v)) return s == 0;
                 return (v - r.head) / N >= first && (v - r.head) / N < end;
             };
-            if (tid < a.count && inside(s_list.id[tid])) out[s_list.id[tid]] = (E)s_list.grad[tid];
+            if (tid < a.count && inside(s_list.id[tid])) out[s_list.id[tid]] = (E)s_list.e[tid];
             const float given = s_list.row.given;
             if (tid == 0 && given == given && inside((uint32_t)in.label[t])) out[in.label[t]] = (E)given;
         }
@@ -656,7 +740,7 @@ hipError_t distill_run(const Logits& in0, const DistillArgs& a0, float* div, flo
     }
     const DistillSpace sp = carve_distill(ws, in.rows, 0, 0, a.count, nullptr);
     const uint64_t most = cut.pieces <= 1024 * kDistillHold ? 512 : 1024, size = in.type == kF32 ? 4 : 2;
-    const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kDistillHold * 64 - 1) / (kDistillHold * 64) * 64);
+    const uint64_t threads = 64 + std::max<uint64_t>(kMinThreads, (cut.pieces + kDistillHold * 64 - 1) / (kDistillHold * 64) * 64);
     const size_t lds = (in.vocab + 31) / 32 * 4 + 4;
     timer_begin(kTLossRows, s);
     by_type(in.type, [&](auto ty) {
