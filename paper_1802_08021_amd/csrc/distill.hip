@@ -112,10 +112,27 @@ __device__ __forceinline__ Share share_of(float beta, double lq, double lp)
     return r;
 }
 
+// Sum of the 64 lanes' values, in every lane: steps as in wave_join.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double wave_step64(double x)
+{
+    const long long v = __double_as_longlong(x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+    return x + __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
 __device__ __forceinline__ double wave_sum(double x)
 {
-    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-    return x;
+    x = wave_step64<0x111, 0xF>(x);
+    x = wave_step64<0x112, 0xF>(x);
+    x = wave_step64<0x114, 0xF>(x);
+    x = wave_step64<0x118, 0xF>(x);
+    x = wave_step64<0x142, 0xA>(x);
+    x = wave_step64<0x143, 0xC>(x);
+    const long long v = __double_as_longlong(x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
 }
 
 // LDS accesses of one wave before and behind this keep their order.
@@ -129,9 +146,10 @@ __device__ __forceinline__ void wave_fence()
 // depends on the list alone (take, prepare) is there before the row's sum, so
 // that little is left to do behind it (finish).
 struct List {
-    uint32_t id[kMaxTop], dup;
+    uint32_t id[kMaxTop];
     float value[kMaxTop], x[kMaxTop];  // the teacher's value, the student's logit
     float q[kMaxTop], e[kMaxTop];      // the teacher's probability; e^(scale (x - top)), then the token's gradient
+    uint32_t dup;
     DistillRow row;
     DistillTerms terms;
 
@@ -141,12 +159,20 @@ struct List {
     {
         wave_fence();
         if (!dup) return;
-        uint32_t again = 0;
-        for (uint32_t i = threadIdx.x & 63, k = 0; i < count; i += 64, ++k)
-            for (uint32_t j = 0; j < i; ++j) again |= (uint32_t)(id[j] == id[i]) << k;
+        const uint32_t lane = threadIdx.x & 63;
+        uint32_t v[kMaxTop / 64], again = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kMaxTop / 64; ++k) v[k] = lane + 64 * k < count ? id[lane + 64 * k] : 0u;
+#pragma unroll 8
+        for (uint32_t j = 0; j < count; ++j) {
+            const uint32_t w = id[j];
+#pragma unroll
+            for (uint32_t k = 0; k < kMaxTop / 64; ++k) again |= (uint32_t)(w == v[k] && j < lane + 64 * k) << k;
+        }
         wave_fence();
-        for (uint32_t i = threadIdx.x & 63, k = 0; i < count; i += 64, ++k)
-            if (again >> k & 1u) id[i] = 0xFFFFFFFFu;
+#pragma unroll
+        for (uint32_t k = 0; k < kMaxTop / 64; ++k)
+            if (lane + 64 * k < count && (again >> k & 1u)) id[lane + 64 * k] = 0xFFFFFFFFu;
         wave_fence();
     }
 };
@@ -302,30 +328,71 @@ __device__ __forceinline__ void hide(Piece<TYPE>& x, uint32_t marks)
 
 constexpr uint32_t kWindow = 4096;  // pieces whose marks lie in LDS at a time
 
+// What the first of two launches leaves of a row's list: five arrays of `count`
+// (tokens, values, logits, q, e), and its sums.
+struct Prepared {
+    float* arrays;  // [rows][5][count]
+    ListSums* sums;
+    float* at_label;
+};
+constexpr uint32_t kTable = 1024;  // places for a list's tokens, to find repeats
+
 // Slice s of a row, as k_slices takes them: (M, Z) over the unlisted tokens.
+// Slice S is the row's list.
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, uint32_t S, uint32_t W, float c, Part* part,
-                                                     float* at_list, float* at_label, uint32_t* ticket)
+                                                     Prepared to, uint32_t* ticket)
 {
     typedef typename Elem<TYPE>::type E;
-    constexpr uint32_t N = Piece<TYPE>::N;
+    constexpr uint32_t N = Piece<TYPE>::N, kMarks = kWindow * N / 32, kListWords = (sizeof(List) + 3) / 4 + kTable;
     __shared__ float s_top[4], s_sum[4];
-    __shared__ uint32_t s_marks[kWindow * N / 32], s_single[4];
+    __shared__ uint32_t s_words[kMarks > kListWords ? kMarks : kListWords], s_single[4];
+    uint32_t* const s_marks = s_words;
     const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
     if (blockIdx.x == 0 && tid == 0) *ticket = 0;  // for k_distill_grad
-    for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
-        const uint64_t t = b / S;
-        const uint32_t s = (uint32_t)(b % S);
+    for (uint64_t b = blockIdx.x; b < in.rows * (S + 1); b += gridDim.x) {
+        const uint64_t t = b / (S + 1);
+        const uint32_t s = (uint32_t)(b % (S + 1));
         if (!distilled(in, a, t)) continue;
         const E* row = static_cast<const E*>(in.x) + t * in.ld;
+        if (s == S) {
+            List& list = *reinterpret_cast<List*>(s_words + kTable);
+            const Entry e(a, t, tid, V);
+            for (uint32_t i = tid; i < kTable; i += 256) s_words[i] = 0xFFFFFFFFu;
+            if (tid == 0) list.dup = 0;
+            list.id[tid] = e.v;
+            list.value[tid] = e.value;
+            list.x[tid] = e.v < V ? (float)row[e.v] : -INFINITY;
+            if (tid == 0) to.at_label[t] = in.label ? (float)row[in.label[t]] : -INFINITY;
+            __syncthreads();
+            if (e.v < V)
+                for (uint32_t h = e.v * 2654435761u >> 22;; h = (h + 1) % kTable) {  // (a quarter of them are taken at most)
+                    const uint32_t was = atomicCAS(&s_words[h], 0xFFFFFFFFu, e.v);
+                    if (was == e.v) list.dup = 1;
+                    if (was == e.v || was == 0xFFFFFFFFu) break;
+                }
+            __syncthreads();
+            if (tid < 64) {
+                list.drop_repeats(a.count);
+                const ListSums sums = prepare_list(a, (double)in.scale, V, list);
+                if (tid == 0) to.sums[t] = sums;
+            }
+            __syncthreads();
+            if (tid < a.count) {
+                float* out = to.arrays + t * 5 * a.count + tid;
+                out[0] = __uint_as_float(list.id[tid]);
+                out[a.count] = list.value[tid];
+                out[2 * a.count] = list.x[tid];
+                out[3 * a.count] = list.q[tid];
+                out[4 * a.count] = list.e[tid];
+            }
+            __syncthreads();
+            continue;
+        }
         const RowCut<TYPE> r(row, V);
         const uint32_t first = (uint32_t)min((uint64_t)r.full, (uint64_t)s * W);
         const uint32_t end = (uint32_t)min((uint64_t)r.full, (uint64_t)(s + 1) * W);
         const Entry mine(a, t, tid, V);
-        if (s == 0) {  // (in place, the gradient's slices find each other's logits gone)
-            if (tid < a.count) at_list[t * a.count + tid] = mine.v < V ? (float)row[mine.v] : -INFINITY;
-            if (tid == 0) at_label[t] = in.label ? (float)row[in.label[t]] : -INFINITY;
-        }
         if (tid < 4) s_single[tid] = 0;
         Own own = {-INFINITY, 0.0f};
         for (uint32_t at = first; at < end || at == first; at += kWindow) {
@@ -358,7 +425,7 @@ __global__ void __launch_bounds__(256) k_rest_slices(Logits in, DistillArgs a, u
         float high = join_waves<false>(own.top, s_top);
         if (high == -INFINITY) high = 0.0f;
         const float sum = join_waves<true>(own.sum * exp2_fast((own.top - high) * c), s_sum);
-        if (tid == 0) part[b] = Part{high, sum};
+        if (tid == 0) part[t * S + s] = Part{high, sum};
         __syncthreads();
     }
 }
@@ -544,22 +611,21 @@ __global__ void __launch_bounds__(1024) k_distill_stats(Logits in, DistillArgs a
 }
 
 constexpr int kDistillU = 2;
-constexpr uint32_t kTable = 1024;  // places for a list's tokens, to find repeats
 
 // Slice s of a gradient row, 256 kDistillU pieces; every workgroup finds its
 // row's terms, a row's first writes them, and the last of these to finish sums
 // them up.  (Without a gradient: G == 1, nothing but that.)
 template <int TYPE>
 __global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, uint32_t S, uint32_t G, float c,
-                                                      const Part* part, const float* at_list, const float* at_label,
-                                                      DistillTerms* terms, uint32_t* ticket, float* div, float* stats,
-                                                      void* dlogits, uint64_t ldd)
+                                                      const Part* part, Prepared from, DistillTerms* terms,
+                                                      uint32_t* ticket, float* div, float* stats, void* dlogits,
+                                                      uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     constexpr int N = Piece<TYPE>::N, U = kDistillU;
     __shared__ double s_w[4][4];
     __shared__ List s_list;
-    __shared__ uint32_t s_table[kTable], s_last;
+    __shared__ uint32_t s_last;
     const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
     bool last = false;
     for (uint64_t b = blockIdx.x; b < in.rows * G; b += gridDim.x) {
@@ -580,27 +646,20 @@ __global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, 
         if (use && s == 0 && tid < r.singles) single = (float)row[r.single(tid)];
         DistillTerms d = {0.0f, 0.0f, 0.0f};
         if (use) {
-            for (uint32_t i = tid; i < kTable; i += 256) s_table[i] = 0xFFFFFFFFu;
-            if (tid == 0) s_list.dup = 0;
-            const Entry e(a, t, tid, V);
-            s_list.id[tid] = e.v;
-            s_list.value[tid] = e.value;
-            if (tid < a.count) s_list.x[tid] = at_list[t * a.count + tid];
-            __syncthreads();
-            if (e.v < V)
-                for (uint32_t h = e.v * 2654435761u >> 22;; h = (h + 1) % kTable) {  // (a quarter of them are taken at most)
-                    const uint32_t was = atomicCAS(&s_table[h], 0xFFFFFFFFu, e.v);
-                    if (was == e.v) s_list.dup = 1;
-                    if (was == e.v || was == 0xFFFFFFFFu) break;
-                }
-            __syncthreads();
-            if (tid < 64) {
-                s_list.drop_repeats(a.count);
-                const double scale = (double)in.scale;
-                const ListSums sums = prepare_list(a, scale, V, s_list);
-                finish_list(a, scale, V, sums, join_slices(part + t * S, S, 64, c), in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu,
-                            at_label[t], a.weight ? (double)a.weight[t] : 1.0, s_list);
+            if (tid < a.count) {
+                const float* list = from.arrays + t * 5 * a.count + tid;
+                s_list.id[tid] = __float_as_uint(list[0]);
+                s_list.value[tid] = list[a.count];
+                s_list.x[tid] = list[2 * a.count];
+                s_list.q[tid] = list[3 * a.count];
+                s_list.e[tid] = list[4 * a.count];
             }
+            const ListSums sums = from.sums[t];
+            __syncthreads();
+            if (tid < 64)
+                finish_list(a, (double)in.scale, V, sums, join_slices(part + t * S, S, 64, c),
+                            in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu, from.at_label[t],
+                            a.weight ? (double)a.weight[t] : 1.0, s_list);
             __syncthreads();
             d = s_list.terms;
         }
@@ -686,7 +745,7 @@ struct DistillSpace {
     DistillTerms* terms;
     uint32_t* ticket;
     Part* part;
-    float *at_list, *at_label;
+    Prepared lists;
 };
 DistillSpace carve_distill(void* ws, uint64_t rows, uint64_t sliced, uint64_t parts, uint32_t count, size_t* bytes)
 {
@@ -695,8 +754,9 @@ DistillSpace carve_distill(void* ws, uint64_t rows, uint64_t sliced, uint64_t pa
     r.terms = c.take<DistillTerms>(rows);
     r.ticket = c.take<uint32_t>(1);
     r.part = c.take<Part>(parts);
-    r.at_list = c.take<float>(sliced * count);
-    r.at_label = c.take<float>(sliced);
+    r.lists.arrays = c.take<float>(sliced * 5 * count);
+    r.lists.sums = c.take<ListSums>(sliced);
+    r.lists.at_label = c.take<float>(sliced);
     if (bytes) *bytes = c.used;
     return r;
 }
@@ -723,17 +783,17 @@ hipError_t distill_run(const Logits& in0, const DistillArgs& a0, float* div, flo
     const float c = in.scale * kLog2e;
     if (!cut.many) {
         const DistillSpace sp = carve_distill(ws, in.rows, in.rows, in.rows * cut.S, a.count, nullptr);
-        const uint32_t slices = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kDistillGrid);
+        const uint32_t slices = (uint32_t)std::min<uint64_t>(in.rows * (cut.S + 1), kDistillGrid);
         const uint32_t G = dlogits ? cut.G : 1, grads = (uint32_t)std::min<uint64_t>(in.rows * G, kDistillGrid);
         by_type(in.type, [&](auto ty) {
             constexpr int TY = decltype(ty)::value;
             timer_begin(kTLossRows, s);
-            hipLaunchKernelGGL((k_rest_slices<TY>), dim3(slices), dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part, sp.at_list,
-                               sp.at_label, sp.ticket);
+            hipLaunchKernelGGL((k_rest_slices<TY>), dim3(slices), dim3(256), 0, s, in, a, cut.S, cut.W, c, sp.part, sp.lists,
+                               sp.ticket);
             timer_end(kTLossRows, s);
             timer_begin(kTLossGrad, s);
-            hipLaunchKernelGGL((k_distill_grad<TY>), dim3(grads), dim3(256), 0, s, in, a, cut.S, G, c, sp.part, sp.at_list,
-                               sp.at_label, sp.terms, sp.ticket, div, stats, dlogits, ldd);
+            hipLaunchKernelGGL((k_distill_grad<TY>), dim3(grads), dim3(256), 0, s, in, a, cut.S, G, c, sp.part, sp.lists,
+                               sp.terms, sp.ticket, div, stats, dlogits, ldd);
             timer_end(kTLossGrad, s);
         });
         return hipGetLastError();
