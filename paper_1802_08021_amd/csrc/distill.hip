@@ -112,29 +112,6 @@ __device__ __forceinline__ Share share_of(float beta, double lq, double lp)
     return r;
 }
 
-// Sum of the 64 lanes' values, in every lane: steps as in wave_join.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double wave_step64(double x)
-{
-    const long long v = __double_as_longlong(x);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
-    return x + __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
-}
-__device__ __forceinline__ double wave_sum(double x)
-{
-    x = wave_step64<0x111, 0xF>(x);
-    x = wave_step64<0x112, 0xF>(x);
-    x = wave_step64<0x114, 0xF>(x);
-    x = wave_step64<0x118, 0xF>(x);
-    x = wave_step64<0x142, 0xA>(x);
-    x = wave_step64<0x143, 0xC>(x);
-    const long long v = __double_as_longlong(x);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
-    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
-}
-
 // LDS accesses of one wave before and behind this keep their order.
 __device__ __forceinline__ void wave_fence()
 {

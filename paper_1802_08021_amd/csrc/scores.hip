@@ -737,16 +737,18 @@ constexpr int kScoreGradU = 2;
 // The gradient of slice s of a row, W pieces: with p_v = 2^(d_v - log2 Z) the
 // softmax, s p_v (on - entropy' (ln p_v + H)) everywhere, and in the places of
 // the row's token and of its list their own derivatives beside it, stored once
-// more behind the slice's other entries.
-template <int TYPE, bool ENTROPY>
-__global__ void __launch_bounds__(256) k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits,
-                                                     uint64_t ldd)
+// more behind the slice's other entries.  A row's first pieces are under way
+// while its factors are found.
+template <int TYPE, int THREADS, bool ENTROPY, bool LIST>
+__global__ void __launch_bounds__(THREADS)
+k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits, uint64_t ldd)
 {
     typedef typename Elem<TYPE>::type E;
     constexpr int N = Piece<TYPE>::N, U = kScoreGradU;
-    __shared__ double s_w[4][4];
-    __shared__ uint32_t s_id[kMaxTop + 1], s_n[5];
-    __shared__ float s_x[kMaxTop + 1], s_g[kMaxTop + 1];
+    constexpr uint32_t kWaves = THREADS < kMaxTop ? THREADS / 64 : kMaxTop / 64;  // that have entries of a list
+    __shared__ double s_sum[kWaves];
+    __shared__ uint32_t s_id[LIST ? kMaxTop : 1], s_n[kWaves], s_some[kWaves], s_token;
+    __shared__ float s_x[LIST ? kMaxTop : 1], s_g[LIST ? kMaxTop : 1];
     const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
     const float c = in.scale * kLog2e;
     for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
@@ -754,54 +756,76 @@ __global__ void __launch_bounds__(256) k_scores_grad(Logits in, ScoresGrad a, ui
         const uint32_t s = (uint32_t)(b % S);
         const E* row = static_cast<const E*>(in.x) + t * in.ld;
         E* out = static_cast<E*>(dlogits) + t * ldd;
-        const RowCut<TYPE> r(row, V);
+        // (one wave has no lane for each single beside a line)
+        const RowCut<TYPE> r = THREADS == 64 ? RowCut<TYPE>(V) : RowCut<TYPE>(row, V);
         const uint32_t first = (uint32_t)min((uint64_t)r.full, (uint64_t)s * W);
         const uint32_t end = (uint32_t)min((uint64_t)r.full, (uint64_t)(s + 1) * W);
         const uint32_t label = in.label ? (uint32_t)in.label[t] : 0xFFFFFFFFu;
-        const bool use = scored(in, t) && a.norm[2 * t + 1] > -INFINITY;
+        const bool scored = !in.label || label < V;
+        Piece<TYPE> y[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            y[u].none();
+            if (scored && (uint64_t)first + tid + THREADS * u < end) y[u].w = load_vec<u32x4>(row + r.piece(first + tid + THREADS * u));
+        }
         // the token and the list, an entry a thread
-        const float d_logp = a.d_logp && in.label ? a.d_logp[t] : 0.0f;
-        const float d_lse = a.d_lse ? a.d_lse[t] : 0.0f, d_h = ENTROPY ? a.d_entropy[t] : 0.0f;
         uint32_t id = 0xFFFFFFFFu;
-        float g = 0.0f, x = -INFINITY;
-        if (a.d_top && tid < a.top) {
+        float g = 0.0f, x = -INFINITY, at = -INFINITY, single = -INFINITY;
+        if (LIST && scored && tid < a.top) {
             id = (uint32_t)a.top_id[t * a.top + tid];
             g = a.d_top[t * a.top + tid];
         }
-        float at = -INFINITY;
-        bool any = false;
-        if (use) {
+        const float top = a.norm[2 * t], ln = a.norm[2 * t + 1];
+        const float d_logp = a.d_logp ? a.d_logp[t] : 0.0f, d_lse = a.d_lse ? a.d_lse[t] : 0.0f;
+        const float d_h = ENTROPY ? a.d_entropy[t] : 0.0f;
+        if (scored && label < V) at = (float)row[label];
+        if (scored && s == 0 && tid < r.singles) single = (float)row[r.single(tid)];
+        const float one = at == -INFINITY ? 0.0f : d_logp;
+        double total = 0.0;
+        bool any = scored && ln > -INFINITY && (one != 0.0f || d_lse != 0.0f || d_h != 0.0f);
+        if constexpr (LIST) {
             if (id < V) x = (float)row[id];
             if (x == -INFINITY) g = 0.0f;
-            if (label < V) at = (float)row[label];
+            if (tid < 64 * kWaves) {
+                const double sum = wave_sum((double)g);
+                const bool some = __any(g != 0.0f);
+                if ((tid & 63) == 0) {
+                    s_sum[tid >> 6] = sum;
+                    s_some[tid >> 6] = some;
+                }
+            }
+            if (tid == 0) s_token = 1;
+            __syncthreads();
+            uint32_t some = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                total += s_sum[w];
+                some |= s_some[w];
+            }
+            any = any || (some && scored && ln > -INFINITY);
         }
-        const float one = at == -INFINITY ? 0.0f : d_logp;
-        double total[1] = {(double)g};
-        if (a.d_top) block_sum(total, s_w, 1);
-        any = use && (one != 0.0f || d_lse != 0.0f || d_h != 0.0f || __syncthreads_or(g != 0.0f));
         if (!any) {
             const u32x4 zero = {0u, 0u, 0u, 0u};
-            for (uint32_t j = first + tid; j < end; j += 256) store_vec(out + r.piece(j), zero);
+            for (uint64_t j = first + tid; j < end; j += THREADS) store_vec(out + r.piece((uint32_t)j), zero);
             if (s == 0 && tid < r.singles) out[r.single(tid)] = (E)0.0f;
-            __syncthreads();
+            if (LIST) __syncthreads();
             continue;
         }
-        const float top = a.norm[2 * t], l2 = a.norm[2 * t + 1] * kLog2e;
-        const float on = in.scale * (float)((double)d_lse - (double)one - total[0]);
+        const float l2 = ln * kLog2e, on = in.scale * (float)((double)d_lse - (double)one - total);
         const float A = ENTROPY ? on - in.scale * d_h * a.entropy[t] : on;
         const float B = ENTROPY ? -in.scale * d_h * 0.693147180559945309f : 0.0f;
         auto entry_of = [&](float v) {
             const float d = (v - top) * c - l2, e = exp2_fast(d);
-            return ENTROPY ? e * (A + B * fmaxf(d, -1e4f)) : e * A;
+            return ENTROPY ? e * __builtin_fmaf(B, fmaxf(d, -1e4f), A) : e * A;
         };
-        const float single = s == 0 && tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
+        // (in place, the token and the list are read before any of it is written)
         __syncthreads();
-        for (uint32_t j = first + tid; j < end; j += 256 * U) {
-            Piece<TYPE> y[U];
+        for (uint64_t j = first + tid; j < end; j += THREADS * U) {
+            Piece<TYPE> next[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                y[u].none();
-                if ((uint64_t)j + 256 * u < end) y[u].w = load_vec<u32x4>(row + r.piece(j + 256 * u));
+                next[u].none();
+                if (j + THREADS * (U + u) < end) next[u].w = load_vec<u32x4>(row + r.piece((uint32_t)j + THREADS * (U + u)));
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -809,52 +833,59 @@ __global__ void __launch_bounds__(256) k_scores_grad(Logits in, ScoresGrad a, ui
 #pragma unroll
                 for (int i = 0; i < N; ++i) e[i] = entry_of(y[u].get(i));
                 y[u].put(e);
-                if ((uint64_t)j + 256 * u < end) store_vec(out + r.piece(j + 256 * u), y[u].w);
+                if (j + THREADS * u < end) store_vec(out + r.piece((uint32_t)j + THREADS * u), y[u].w);
+                y[u] = next[u];
             }
         }
         if (s == 0 && tid < r.singles) out[r.single(tid)] = (E)entry_of(single);
-        // what lies in this slice of the list, in its order, and the token
         auto inside = [&](uint32_t v, float x) {
             if (v >= V || x == -INFINITY) return false;
             if (!r.in_piece(v)) return s == 0;
             const uint32_t j = (v - r.head) / N;
             return j >= first && j < end;
         };
-        const bool mine = inside(id, x);
-        const uint64_t mask = __ballot(mine);
-        if ((tid & 63) == 0) s_n[tid >> 6] = (uint32_t)__popcll(mask);
+        const bool token = inside(label, at);
         // (every store before this is done before the next ones begin)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        uint32_t before = 0, count = 0;
-        for (uint32_t w = 0; w < 4; ++w) {
-            if (w < tid >> 6) before += s_n[w];
-            count += s_n[w];
-        }
-        if (mine) {
-            const uint32_t i = before + (uint32_t)__popcll(mask & ((1ull << (tid & 63)) - 1));
-            s_id[i] = id;
-            s_x[i] = x;
-            s_g[i] = g;
-        }
-        const bool token = inside(label, at);
-        if (token && tid == 0) {
-            s_id[count] = label;
-            s_x[count] = at;
-            s_g[count] = one;
-        }
-        count += token;
-        __syncthreads();
-        for (uint32_t i = tid; i < count; i += 256) {
-            // (a token that is there twice: its first entry takes all of them)
-            float more = 0.0f;
-            bool lead = true;
-            for (uint32_t k = 0; k < count; ++k)
-                if (s_id[k] == s_id[i]) {
-                    more += s_g[k];
-                    lead &= k >= i;
+        if constexpr (!LIST) {
+            __syncthreads();
+            if (token && tid == 0) out[label] = (E)(entry_of(at) + in.scale * one);
+        } else {
+            // what lies in this slice of the list, in its order
+            const bool mine = inside(id, x);
+            const uint64_t mask = __ballot(mine);
+            if ((tid & 63) == 0 && tid < 64 * kWaves) s_n[tid >> 6] = (uint32_t)__popcll(mask);
+            __syncthreads();
+            uint32_t before = 0, count = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                if (w < tid >> 6) before += s_n[w];
+                count += s_n[w];
+            }
+            if (mine) {
+                const uint32_t i = before + (uint32_t)__popcll(mask & ((1ull << (tid & 63)) - 1));
+                s_id[i] = id;
+                s_x[i] = x;
+                s_g[i] = g;
+            }
+            __syncthreads();
+            for (uint32_t i = tid; i < count; i += THREADS) {
+                // (a token that is there twice: its first entry takes all of them)
+                float more = 0.0f;
+                bool lead = true;
+                for (uint32_t k = 0; k < count; ++k)
+                    if (s_id[k] == s_id[i]) {
+                        more += s_g[k];
+                        lead &= k >= i;
+                    }
+                if (s_id[i] == label) {
+                    more += one;
+                    s_token = 0;  // (it has its place on the list)
                 }
-            if (lead) out[s_id[i]] = (E)(entry_of(s_x[i]) + in.scale * more);
+                if (lead) out[s_id[i]] = (E)(entry_of(s_x[i]) + in.scale * more);
+            }
+            __syncthreads();
+            if (token && tid == 0 && s_token) out[label] = (E)(entry_of(at) + in.scale * one);
         }
         __syncthreads();
     }
@@ -954,18 +985,37 @@ hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_
 hipError_t scores_grad_run(const Logits& in, const ScoresGrad& a, void* dlogits, uint64_t ldd, hipStream_t s)
 {
     const uint64_t pieces = in.vocab / (in.type == kF32 ? 4 : 8) + 1;
-    // (in place, a row's token and list are read before any of it is written:
-    // one workgroup a row)
+    // (in place, a row's token and list are read before any of it is written: one
+    // workgroup a row)
     const bool whole = dlogits == in.x && (a.d_logp || a.d_top);
-    const uint32_t W = whole ? (uint32_t)pieces : 256 * kScoreGradU, S = (uint32_t)((pieces + W - 1) / W);
+    // Slices of 1024 pieces, of 512 where there are few (37 x 32000 fp32 4.6 us
+    // against 5.2), of 2048 with long lists, which every slice looks through (8192
+    // x 131072 bf16 and 64 tokens 724 us against 754; without a list 689 with
+    // 1024, 762 with 512, 746 with 2048, 807 by whole rows).
+    const bool few = in.rows * pieces < 1024 * 1024;
+    const uint32_t W = whole ? (uint32_t)pieces : few ? 512 : a.top > 32 ? 2048 : 1024;
+    // One wave for the shortest rows; for whole rows, few and long, 1024 threads.
+    const uint32_t T = pieces <= 64 * kScoreGradU && a.top <= 64 ? 64 : whole && pieces > 1024 && in.rows < 1024 ? 1024 : 256;
+    const uint32_t S = (uint32_t)((pieces + W - 1) / W);
     const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * S, kScoreGrid);
     timer_begin(kTScoresGrad, s);
     by_type(in.type, [&](auto ty) {
         constexpr int TY = decltype(ty)::value;
+        auto go = [&](auto kern, uint32_t threads) {
+            hipLaunchKernelGGL(kern, dim3(grid), dim3(threads), 0, s, in, a, S, W, dlogits, ldd);
+        };
+        auto with = [&](auto entropy, auto list) {
+            constexpr bool H = decltype(entropy)::value, L = decltype(list)::value;
+            T == 64    ? go(k_scores_grad<TY, 64, H, L>, 64)
+            : T == 256 ? go(k_scores_grad<TY, 256, H, L>, 256)
+                       : go(k_scores_grad<TY, 1024, H, L>, 1024);
+        };
+        typedef std::true_type Y;
+        typedef std::false_type N;
         if (a.d_entropy)
-            hipLaunchKernelGGL((k_scores_grad<TY, true>), dim3(grid), dim3(256), 0, s, in, a, S, W, dlogits, ldd);
+            a.d_top ? with(Y(), Y()) : with(Y(), N());
         else
-            hipLaunchKernelGGL((k_scores_grad<TY, false>), dim3(grid), dim3(256), 0, s, in, a, S, W, dlogits, ldd);
+            a.d_top ? with(N(), Y()) : with(N(), N());
     });
     timer_end(kTScoresGrad, s);
     return hipGetLastError();

@@ -89,6 +89,29 @@ __device__ __forceinline__ float wave_join(float x)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+// The sum in fp64.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double wave_step64(double x)
+{
+    const long long v = __double_as_longlong(x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
+    return x + __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+__device__ __forceinline__ double wave_sum(double x)
+{
+    x = wave_step64<0x111, 0xF>(x);
+    x = wave_step64<0x112, 0xF>(x);
+    x = wave_step64<0x114, 0xF>(x);
+    x = wave_step64<0x118, 0xF>(x);
+    x = wave_step64<0x142, 0xA>(x);
+    x = wave_step64<0x143, 0xC>(x);
+    const long long v = __double_as_longlong(x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+
 // Largest of the 64 lanes' values, in every lane: shifts within rows of 16
 // lanes, then the row broadcasts.
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
