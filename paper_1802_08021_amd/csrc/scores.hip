@@ -8,12 +8,14 @@
 // Both of its terms are positive, so nothing cancels.  U moves with the maximum
 // as Z does: from M to M' it becomes 2^-h (U + h Z), h = c (M' - M).
 //
-// The n most likely tokens of a row: every thread of a workgroup keeps the
-// largest logit of each of four groups of its pieces, and the n-th largest of
-// all groups' is a bound that at least n logits reach and few more do (of 2048
-// groups about 65 for n = 64).  Groups below it need no second look; those of
-// the others are looked through once more, and what reaches the bound is put in
-// order.
+// The n most likely tokens of a row: the pass over its logits leaves the largest
+// of each of up to 1024 groups of its lines (128 bytes; of up to 2048 groups of
+// a lane's pieces where a list is long for its row), and the n-th largest of
+// these is a bound that at least n logits reach and few more do (of 1024 groups
+// about 66 for n = 64).  A second launch finds it, looks through the groups that
+// reach it once more, and puts what it finds in order.
+// (Lists by the first pass' own workgroups kept these from their next row: 4096
+// x 131072 bf16 with 64 tokens 190 us, 8192 x 8000 with 20 80 us.)
 #include "rows_device.h"
 
 #include <algorithm>
@@ -174,213 +176,89 @@ __device__ __forceinline__ float placed(uint32_t k)
 // No two tokens of a row share a key; the lower index comes first.
 __device__ __forceinline__ uint64_t key_of(uint32_t place, uint32_t v) { return (uint64_t)place << 32 | (uint32_t)~v; }
 
-constexpr int kScoreU = 4;       // pieces of a thread where a row is one turn,
-constexpr uint32_t kGroups = 4;  // groups of them: a piece each; else
-constexpr uint32_t kSubs = 16;   // smaller ones that are looked through again
-static_assert(kScoreU == kGroups, "a piece a group");
+constexpr int kScoreU = 4;  // pieces of a thread where a row is one turn
+constexpr uint32_t kLineGroups = 1024, kLaneGroups = 2048;  // groups of a row at most
 
-// What a workgroup puts a row together in.
-template <int THREADS, bool ONE>
-struct TopSpace {
-    static constexpr uint32_t kWaves = THREADS / 64, kCands = THREADS < 256 ? 512 : 1024;
-    static constexpr uint32_t kHeld = ONE ? 1 : kSubs;  // numbers a thread keeps here
-    struct Wave {
-        float top, sum, bend;
-        uint32_t there, low, high;  // of its groups: how many hold a logit, ~least, largest
-    } wave[kWaves];
-    uint32_t reach[3][3];  // (a step's, the next one's, the one's behind it)
-    uint32_t count, groups, bound, above;
-    union {
-        uint32_t high[kHeld * THREADS];  // the groups' largest (read before there are candidates)
-        uint64_t key[kCands];            // candidates
-    };
-    union {
-        uint16_t who[kCands];  // groups at or above the bound
-        struct {
-            uint64_t out[kMaxTop];
-            uint32_t hist[256];
-        };
-    };
-};
-
-// The waves' parts joined (nothing: M is -Inf); M in every thread, the sums in
-// the first `lanes`.
-template <int WAVES, class W>
-__device__ __forceinline__ ScorePart join_parts(const W* wave, float c, uint32_t lanes)
+// The waves' parts joined (nothing: M is -Inf).
+template <int WAVES>
+__device__ __forceinline__ ScorePart join_parts(const ScorePart* wave, float c)
 {
     ScorePart p = {-INFINITY, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) p.top = fmaxf(p.top, wave[w].top);
-    if (threadIdx.x >= ((lanes + 63) & ~63u)) return p;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
-        const ScorePart q = moved(ScorePart{wave[w].top, wave[w].sum, wave[w].bend}, p.top, c);
+        const ScorePart q = moved(wave[w], p.top, c);
         p.sum += q.sum;
         p.bend += q.bend;
     }
     return p;
 }
 
-template <class Space>
-__device__ __forceinline__ void clear_counts(Space& s)
-{
-    if (threadIdx.x < 9) s.reach[threadIdx.x / 3][threadIdx.x % 3] = 0;
-    if (threadIdx.x == 9) s.count = s.groups = 0;
-}
-
-// What each wave has of its row, by its first lane.
-template <class Space>
-__device__ __forceinline__ void put_wave(Space& s, const ScorePart& q, const uint32_t (&v)[kGroups])
-{
-    uint32_t there = 0, low = 0, high = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kGroups; ++i) {
-        there += (uint32_t)__popcll(__ballot(v[i] != 0));
-        low = max(low, v[i] ? ~v[i] : 0u);
-        high = max(high, v[i]);
-    }
-    low = wave_max(low);
-    high = wave_max(high);
-    if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = {q.top, q.sum, q.bend, there, low, high};
-}
-
-// A bound that at least n of the threads' numbers v reach (1 if fewer are not
-// 0) and few more do: two bits a step from the first in which they differ.
-template <class Space>
-__device__ __forceinline__ uint32_t find_bound(Space& s, const uint32_t (&v)[kGroups], uint32_t n)
-{
-    constexpr uint32_t kWaves = Space::kWaves;
-    uint32_t there = 0, low = 0, high = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        there += s.wave[w].there;
-        low = max(low, s.wave[w].low);
-        high = max(high, s.wave[w].high);
-    }
-    if (there < n) return 1;
-    low = (uint32_t)__builtin_amdgcn_readfirstlane((int)~low);
-    high = (uint32_t)__builtin_amdgcn_readfirstlane((int)high);
-    if (low == high) return low;
-    int bit = 31 - __clz((int)(low ^ high));
-    uint32_t t = high & ~((2u << bit) - 1);
-    for (uint32_t turn = 0; bit >= 0; bit -= 2, turn = turn == 2 ? 0 : turn + 1) {
-        const uint32_t shift = bit > 0 ? bit - 1 : 0, steps = bit > 0 ? 3 : 1;
-        uint32_t reach[3] = {0, 0, 0};
-#pragma unroll
-        for (uint32_t k = 0; k < 3; ++k) {
-            if (k >= steps) break;
-#pragma unroll
-            for (uint32_t i = 0; i < kGroups; ++i) reach[k] += (uint32_t)__popcll(__ballot(v[i] >= t + ((k + 1) << shift)));
-        }
-        if (kWaves > 1) {
-            const uint32_t lane = threadIdx.x & 63;
-            if (lane < 3) atomicAdd(&s.reach[turn][lane], lane == 0 ? reach[0] : lane == 1 ? reach[1] : reach[2]);
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 3; ++k) reach[k] = (uint32_t)__builtin_amdgcn_readfirstlane((int)s.reach[turn][k]);
-            // (read by all before the barrier above, added to behind the next)
-            if (threadIdx.x < 3) s.reach[turn == 0 ? 2 : turn - 1][threadIdx.x] = 0;
-        }
-        const uint32_t best = reach[2] >= n ? 3 : reach[1] >= n ? 2 : reach[0] >= n ? 1 : 0;
-        t += best << shift;
-        if (best && reach[best - 1] <= n + n / 8 + 2) break;
-    }
-    return t ? t : 1u;
-}
-
-// The n largest of s.key[0, count) in order to s.out, count <= kCands: up to 128
-// by counting the larger ones, beyond by waves that put 64 at a time in order
-// and look up how many of each other 64 are larger.
-template <class Space>
-__device__ __forceinline__ void put_in_order(Space& s, uint32_t count, uint32_t n)
-{
-    constexpr uint32_t kWaves = Space::kWaves, kMost = Space::kCands / 64 / kWaves;
-    const uint32_t tid = threadIdx.x;
-    if (count <= 128) {
-        for (uint32_t i = tid; i < count; i += 64 * kWaves) {
-            const uint64_t k = s.key[i];
-            uint32_t rank = 0, j = 0;
-            for (; j + 8 <= count; j += 8)
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) rank += s.key[j + e] > k;
-            for (; j < count; ++j) rank += s.key[j] > k;
-            if (rank < n) s.out[rank] = k;
-        }
-        __syncthreads();
-        return;
-    }
-    const uint32_t lane = tid & 63, wave = tid >> 6, blocks = (count + 63) / 64;
-    for (uint32_t b = wave; b < blocks; b += kWaves) {
-        uint64_t k = 64 * b + lane < count ? s.key[64 * b + lane] : 0;
-        for (uint32_t run = 2; run <= 64; run *= 2)
-            for (uint32_t gap = run / 2; gap; gap /= 2) {
-                const uint64_t o = __shfl_xor((unsigned long long)k, (int)gap);
-                const bool larger = ((lane & run) == 0) == ((lane & gap) == 0);  // who keeps the larger one
-                k = (o > k) == larger ? o : k;
-            }
-        s.key[64 * b + lane] = k;
-    }
-    __syncthreads();
-    for (uint32_t b = wave; b < blocks; b += kWaves) {
-        const uint64_t k = s.key[64 * b + lane];
-        uint32_t rank = lane;
-        if (lane >= n) continue;  // (its own 64 hold n larger ones)
-        for (uint32_t w = 0; w < blocks; ++w) {
-            if (w == b) continue;
-            const uint64_t* list = s.key + 64 * w;
-            uint32_t at = 0;  // of the list, how many are larger
-#pragma unroll
-            for (uint32_t half = 32; half; half /= 2)
-                if (list[at + half - 1] > k) at += half;
-            rank += at + (at == 63 && list[63] > k);
-        }
-        if (k && rank < n) s.out[rank] = k;
-    }
-    __syncthreads();
-}
-
-// Piece u of a thread's K in a turn over a long row.  (Side by side, what is
-// looked through again would lie in half the lines or a quarter, but the first
-// pass is slower: 2048 x 131072 fp32 298 us against 156.)
-template <int K, int THREADS>
-__device__ __forceinline__ uint64_t long_piece(uint64_t turn, uint32_t u, uint32_t tid)
-{
-    return (turn * K + u) * THREADS + tid;
-}
-
-// Pieces [first, end) of a row and, with `singles`, its singles.
+// A row's cut into pieces, for a pass of `threads`: one wave has no lane for
+// each single beside a line.
 template <int TYPE>
-struct Span {
-    typedef typename Elem<TYPE>::type E;
-    const E* row;
-    RowCut<TYPE> r;
-    uint32_t first, end;
-    bool singles;
-    // Calls f(logit, token) for every token.
-    template <class F>
-    __device__ __forceinline__ void each(F f) const
-    {
-        if (singles && threadIdx.x < r.singles) f((float)row[r.single(threadIdx.x)], r.single(threadIdx.x));
-        for (uint64_t j = first + threadIdx.x; j < end; j += blockDim.x) {
-            Piece<TYPE> x;
-            x.w = load_vec<u32x4, true>(row + r.piece((uint32_t)j));
-#pragma unroll
-            for (int i = 0; i < Piece<TYPE>::N; ++i) f(x.get(i), r.piece((uint32_t)j) + i);
-        }
-    }
+__device__ __forceinline__ RowCut<TYPE> cut_of(const void* row, uint32_t V, bool one_wave)
+{
+    return one_wave ? RowCut<TYPE>(V) : RowCut<TYPE>(row, V);
+}
+
+// Another lane's word, `gap` apart (an exclusive or): within rows of 16 by moves
+// of the vector unit.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved_word(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+template <int GAP>
+__device__ __forceinline__ uint32_t across(uint32_t x)
+{
+    if constexpr (GAP == 1) return moved_word<0xB1>(x);                     // quad_perm 1 0 3 2
+    if constexpr (GAP == 2) return moved_word<0x4E>(x);                     // quad_perm 2 3 0 1
+    if constexpr (GAP == 4) return moved_word<0x1B>(moved_word<0x141>(x));  // row_half_mirror, quad_perm 3 2 1 0
+    if constexpr (GAP == 8) return moved_word<0x128>(x);                    // row_ror 8
+    return (uint32_t)__shfl_xor((int)x, GAP);
+}
+// The largest of eight neighbours' values.
+__device__ __forceinline__ float largest_of_8(float x)
+{
+    auto with = [](float x, uint32_t y) { return largest(x, __uint_as_float(y), x); };
+    x = with(x, across<1>(__float_as_uint(x)));
+    x = with(x, across<2>(__float_as_uint(x)));
+    return with(x, moved_word<0x141>(__float_as_uint(x)));
+}
+
+// Groups of a row's pieces: LANES adjacent lanes' (1 or 8), `units` of each, a
+// pass' threads apart; `each` groups a slice, of S slices.
+struct Groups {
+    uint32_t* largest;  // places, [rows][S each]
+    uint32_t units, each;
 };
 
-// A span's part once more, its largest logit known and so large that the
-// difference has to be taken first.
+// ---------------------------------------------------------------- the pass
+
+__device__ __forceinline__ bool scored(const Logits& in, uint64_t t) { return !in.label || has_token(in, t); }
+
+// A part once more of pieces [first, end) and, with `singles`, the singles: its
+// largest logit is known, and so large that the difference has to be taken first.
 template <int TYPE, int THREADS>
-__device__ __attribute__((noinline)) ScorePart far_part(Span<TYPE> span, float top, float c, float (*s_far)[THREADS / 64])
+__device__ __attribute__((noinline)) ScorePart far_part(const typename Elem<TYPE>::type* row, RowCut<TYPE> r, uint32_t first,
+                                                        uint32_t end, bool singles, float top, float c,
+                                                        float (*s_far)[THREADS / 64])
 {
     float z = 0.0f, b = 0.0f;
-    span.each([&](float x, uint32_t) {
+    auto take = [&](float x) {
         const float d = (x - top) * c, e = exp2_fast(d);
         z += e;
         b = __builtin_fmaf(-fmaxf(d, -1e4f), e, b);
-    });
+    };
+    if (singles && threadIdx.x < r.singles) take((float)row[r.single(threadIdx.x)]);
+    for (uint64_t j = first + threadIdx.x; j < end; j += THREADS) {
+        Piece<TYPE> x;
+        x.w = load_vec<u32x4, true>(row + r.piece((uint32_t)j));
+#pragma unroll
+        for (int i = 0; i < Piece<TYPE>::N; ++i) take(x.get(i));
+    }
     z = wave_join<true>(z);
     b = wave_join<true>(b);
     if ((threadIdx.x & 63) == 0) {
@@ -397,16 +275,281 @@ __device__ __attribute__((noinline)) ScorePart far_part(Span<TYPE> span, float t
     return ScorePart{top, z, b};
 }
 
+// Slice s of a row: pieces [s W, (s + 1) W); slice 0 takes the singles too.
+// With one slice a row its numbers at once, and its part where its list needs
+// it or there are more; LANES: the groups' for a list, or 0.  ONE: a slice is a
+// turn, kScoreU pieces a thread.
+template <int TYPE, int THREADS, int LANES, bool ONE>
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(6)))
+k_scores(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, ScorePart* part, Groups groups)
+{
+    typedef typename Elem<TYPE>::type E;
+    constexpr int K = 16 / Piece<TYPE>::N;
+    __shared__ ScorePart s_wave[THREADS / 64];
+    __shared__ float s_far[2][THREADS / 64];
+    __shared__ uint32_t s_largest[LANES == 8 ? kLineGroups : 1];
+    const uint32_t tid = threadIdx.x;
+    for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
+        const uint64_t t = b / S;
+        const uint32_t s = (uint32_t)(b % S);
+        if (!scored(in, t)) {
+            if (S == 1) put_unused(o, t);
+            continue;
+        }
+        const E* row = static_cast<const E*>(in.x) + t * in.ld;
+        const RowCut<TYPE> r = cut_of<TYPE>(row, (uint32_t)in.vocab, THREADS == 64);
+        const uint32_t first = (uint32_t)min((uint64_t)r.full, (uint64_t)s * W);
+        const uint32_t end = (uint32_t)min((uint64_t)r.full, (uint64_t)(s + 1) * W);
+        const uint32_t count = end - first;
+        const float single = s == 0 && tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
+        const float at = tid == 0 && in.label ? (float)row[in.label[t]] : 0.0f;
+        // group number g of the thread's lanes
+        uint32_t* largest_of = LANES ? groups.largest + b * groups.each : nullptr;
+        auto note = [&](float most, uint32_t g) {
+            if (LANES == 1) largest_of[g * THREADS + tid] = place(most);
+            if (LANES == 8) {
+                most = largest_of_8(most);
+                if ((tid & 7) == 0) s_largest[g * (THREADS / 8) + tid / 8] = place(most);
+            }
+        };
+        Piece<TYPE> x[kScoreU];
+        float most[kScoreU];
+        Tally own;
+        if constexpr (ONE) {
+#pragma unroll
+            for (int u = 0; u < kScoreU; ++u) {
+                x[u].none();
+                if (tid + THREADS * u < count) x[u].w = load_vec<u32x4>(row + r.piece(first + tid + THREADS * u));
+            }
+            own.add_one(single, c);
+#pragma unroll
+            for (int u = 0; u < kScoreU; u += K) own.add<TYPE, K>(x + u, most + u, c);
+            if (LANES) {
+                if (groups.units == 1) {
+#pragma unroll
+                    for (int u = 0; u < kScoreU; ++u) note(most[u], u);
+                } else if (groups.units == 2) {
+                    note(fmaxf(most[0], most[1]), 0);
+                    note(fmaxf(most[2], most[3]), 1);
+                } else {
+                    note(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), 0);
+                }
+            }
+        } else {
+            // K pieces at a time, the next ones under way (loads past the end
+            // read the last piece, and count for nothing)
+            const uint32_t below = tid & ~63u;  // a wave has mine of the turns
+            const uint32_t mine = count > below ? (count - below + K * THREADS - 1) / (K * THREADS) : 0u;
+            const uint8_t* from = reinterpret_cast<const uint8_t*>(row + r.piece(first));
+            const uint32_t last = count ? (count - 1) * 16 : 0, per = LANES ? groups.units / K : 0;
+            Piece<TYPE> y[K];
+            Piece<TYPE>(&z)[K] = reinterpret_cast<Piece<TYPE>(&)[K]>(x);
+            auto ask = [&](Piece<TYPE>(&q)[K], uint32_t turn) {
+#pragma unroll
+                for (int u = 0; u < K; ++u)
+                    q[u].w = load_vec<u32x4>(reinterpret_cast<const E*>(from + min(((turn * K + u) * THREADS + tid) * 16, last)));
+            };
+            float group = -INFINITY;
+            uint32_t left = per, g = 0;
+            auto take = [&](Piece<TYPE>(&q)[K], uint32_t turn) {
+                if (turn + 1 == mine)
+#pragma unroll
+                    for (int u = 0; u < K; ++u)
+                        if ((turn * K + u) * THREADS + tid >= count) q[u].none();
+                const float high = own.add<TYPE, K>(q, most, c);
+                if (LANES) {
+                    group = largest(group, high, high);
+                    if (--left == 0 || turn + 1 == mine) {
+                        note(group, g++);
+                        group = -INFINITY;
+                        left = per;
+                    }
+                }
+            };
+            if (mine) ask(z, 0);
+            own.add_one(single, c);
+            for (uint32_t turn = 0; turn < mine; turn += 2) {
+                if (turn + 1 < mine) ask(y, turn + 1);
+                take(z, turn);
+                if (turn + 1 >= mine) break;
+                if (turn + 2 < mine) ask(z, turn + 2);
+                take(y, turn + 1);
+            }
+            if (LANES)  // (groups that this wave has no piece of)
+                for (; g * THREADS < groups.each * LANES; ++g) note(-INFINITY, g);
+        }
+        ScorePart p = own.join_lanes(c);
+        if (THREADS > 64) {
+            if ((tid & 63) == 0) s_wave[tid >> 6] = p;
+            __syncthreads();
+            p = join_parts<THREADS / 64>(s_wave, c);
+        }
+        if (p.top != -INFINITY && !(fabsf(p.top * c) < kFar)) {
+            __syncthreads();
+            p = far_part<TYPE, THREADS>(row, r, first, end, s == 0, p.top, c, s_far);
+        }
+        if (LANES == 8)
+            for (uint32_t i = tid; i < groups.each; i += THREADS) largest_of[i] = s_largest[i];
+        if (p.top == -INFINITY) p.top = 0.0f;
+        if (tid == 0) {
+            if (LANES || S > 1) part[b] = p;
+            if (S == 1) put_scores(o, t, p, in.label != nullptr, at, in.scale);
+        }
+        if (THREADS > 64) __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- lists
+
+// What a row's list is found in; up to kCands candidates.
+template <int THREADS>
+struct TopSpace {
+    static constexpr uint32_t kWaves = THREADS / 64, kCands = THREADS == 64 ? 512 : 1024;
+    uint32_t count, groups, bound, above;
+    uint32_t there[kWaves], low[kWaves], high[kWaves];
+    ScorePart part;
+    alignas(16) uint32_t hist[256];
+    uint32_t who[kCands], stop[kCands];  // groups at or above the bound: first piece, end
+    uint64_t key[kCands], out[kMaxTop];
+};
+
+// A bound that at least n of the numbers that each(f) calls f with reach (1 if
+// fewer are not 0) and few more do: the range that holds the n-th largest is cut
+// into 256, until few are left in its part (once, as a rule).
+template <int THREADS, class Each>
+__device__ __forceinline__ uint32_t find_bound(TopSpace<THREADS>& s, uint32_t n, Each each)
+{
+    constexpr uint32_t kWaves = THREADS / 64;
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t there = 0, low = 0, high = 0;  // low: of the complements
+    each([&](uint32_t v) {
+        there += v != 0;
+        low = max(low, v ? ~v : 0u);
+        high = max(high, v);
+    });
+    there = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(there), 63);
+    low = wave_max(low);
+    high = wave_max(high);
+    if (lane == 0) {
+        s.there[threadIdx.x >> 6] = there;
+        s.low[threadIdx.x >> 6] = low;
+        s.high[threadIdx.x >> 6] = high;
+    }
+    for (uint32_t i = threadIdx.x; i < 256; i += THREADS) s.hist[i] = 0;
+    __syncthreads();
+    if (kWaves > 1) {
+        there = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) {
+            there += s.there[w];
+            low = max(low, s.low[w]);
+            high = max(high, s.high[w]);
+        }
+    }
+    if (there < n) return 1;
+    low = (uint32_t)__builtin_amdgcn_readfirstlane((int)~low);
+    high = (uint32_t)__builtin_amdgcn_readfirstlane((int)high);
+    for (uint32_t above = 0;;) {  // above: how many lie beyond high
+        const uint32_t range = high - low, shift = range < 256 ? 0 : 24 - __clz((int)range);
+        each([&](uint32_t v) {
+            if (v >= low && v <= high) atomicAdd(&s.hist[(v - low) >> shift], 1u);
+        });
+        __syncthreads();
+        // (every wave for itself: a lane four parts, the highest first)
+        const u32x4 h = *reinterpret_cast<const u32x4*>(&s.hist[252 - 4 * lane]);
+        const uint32_t all = h[0] + h[1] + h[2] + h[3], upto = wave_scan(all) + above;
+        const int at = __ffsll((unsigned long long)__ballot(upto >= n)) - 1;
+        uint32_t more = upto - all, cut = 255 - 4 * lane;
+#pragma unroll
+        for (int k = 3; k >= 0; --k)
+            if (more < n) {
+                more += h[k];
+                cut = 252 - 4 * lane + k;
+            }
+        more = (uint32_t)__builtin_amdgcn_readlane((int)more, at);
+        cut = (uint32_t)__builtin_amdgcn_readlane((int)cut, at);
+        const uint32_t from = low + (cut << shift);
+        if (more <= n + n / 4 + 8 || shift == 0) return from;
+        above = more - s.hist[cut];
+        low = from;
+        high = from + ((1u << shift) - 1);
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 256; i += THREADS) s.hist[i] = 0;
+        __syncthreads();
+    }
+}
+
+template <int RUN, int GAP>
+__device__ __forceinline__ void exchange(uint64_t& k)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const uint64_t o = (uint64_t)across<GAP>((uint32_t)(k >> 32)) << 32 | across<GAP>((uint32_t)k);
+    const bool larger = ((lane & RUN) == 0) == ((lane & GAP) == 0);  // who keeps the larger one
+    k = (o > k) == larger ? o : k;
+    if constexpr (GAP > 1) exchange<RUN, GAP / 2>(k);
+}
+template <int RUN>
+__device__ __forceinline__ void sort_lanes(uint64_t& k)
+{
+    if constexpr (RUN > 2) sort_lanes<RUN / 2>(k);
+    exchange<RUN, RUN / 2>(k);
+}
+
+// The n largest of s.key[0, count) in order to s.out, count <= kCands: up to 128
+// by counting the larger ones, beyond by waves that put 64 at a time in order
+// and look up how many of each other 64 are larger.
+template <int THREADS>
+__device__ __forceinline__ void put_in_order(TopSpace<THREADS>& s, uint32_t count, uint32_t n)
+{
+    constexpr uint32_t kWaves = THREADS / 64;
+    const uint32_t tid = threadIdx.x;
+    if (count <= 128) {
+        for (uint32_t i = tid; i < count; i += THREADS) {
+            const uint64_t k = s.key[i];
+            uint32_t rank = 0;
+            for (uint32_t j = 0; j < count; j += 8)
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) rank += j + e < count && s.key[j + e] > k;
+            if (rank < n) s.out[rank] = k;
+        }
+        __syncthreads();
+        return;
+    }
+    const uint32_t lane = tid & 63, wave = tid >> 6, blocks = (count + 63) / 64;
+    for (uint32_t b = wave; b < blocks; b += kWaves) {
+        uint64_t k = 64 * b + lane < count ? s.key[64 * b + lane] : 0;
+        sort_lanes<64>(k);
+        s.key[64 * b + lane] = k;
+    }
+    __syncthreads();
+    for (uint32_t b = wave; b < blocks; b += kWaves) {
+        if (lane >= n) continue;  // (its own 64 hold n larger ones)
+        const uint64_t k = s.key[64 * b + lane];
+        uint32_t rank = lane;
+        for (uint32_t w = 0; w < blocks; ++w) {
+            if (w == b) continue;
+            const uint64_t* list = s.key + 64 * w;
+            uint32_t at = 0;  // of the list, how many are larger
+#pragma unroll
+            for (uint32_t half = 32; half; half /= 2)
+                if (list[at + half - 1] > k) at += half;
+            rank += at + (at == 63 && list[63] > k);
+        }
+        if (k && rank < n) s.out[rank] = k;
+    }
+    __syncthreads();
+}
+
 // The n largest of more than n keys, that each(f) calls f with, to s.key, eight
 // bits a pass: for rows where too many logits reach the bound (most of them
 // equal).
-template <class Space, class Each>
-__device__ void narrow(Space& s, uint32_t n, Each each)
+template <int THREADS, class Each>
+__device__ __attribute__((noinline)) void narrow(TopSpace<THREADS>& s, uint32_t n, Each each)
 {
     const uint32_t all = n;
     uint64_t prefix = 0;
     for (int shift = 56; shift >= 0; shift -= 8) {
-        for (uint32_t i = threadIdx.x; i < 256; i += 64 * Space::kWaves) s.hist[i] = 0;
+        for (uint32_t i = threadIdx.x; i < 256; i += THREADS) s.hist[i] = 0;
         __syncthreads();
         each([&](uint64_t k) {
             if (shift < 56 && k >> (shift + 8) != prefix) return;
@@ -442,290 +585,108 @@ __device__ void narrow(Space& s, uint32_t n, Each each)
     __syncthreads();
 }
 
-// The n most likely tokens of a span in order in s.out; returns how many there
-// are (at most n).  v: the thread's groups' largest.  ONE: its pieces are
-// groups, and still in x; else s.high has those of kSubs smaller groups, of
-// `per` turns of K pieces.  single: the thread's single.  (After put_wave and a
-// barrier.)
-template <int TYPE, int THREADS, bool ONE>
-__device__ __forceinline__ uint32_t top_of(TopSpace<THREADS, ONE>& s, const Span<TYPE>& span, uint32_t n, uint32_t per,
-                                           Piece<TYPE> (&x)[kScoreU], const uint32_t (&v)[kGroups], float single)
-{
-    constexpr int N = Piece<TYPE>::N, K = 16 / N;
-    constexpr uint32_t kCands = TopSpace<THREADS, ONE>::kCands;
-    const uint32_t tid = threadIdx.x;
-    const uint32_t bound = find_bound(s, v, n);
-    const float least = bound > place(-3.402823466e38f) ? placed(bound) : -3.402823466e38f;
-    auto add = [&](uint32_t at, float y, uint32_t j) {
-        if (at < kCands) s.key[at] = key_of(place(y), j);
-    };
-    if (ONE) {
-        if (span.singles && single >= least) add(atomicAdd(&s.count, 1u), single, span.r.single(tid));
-        // counted first, so that a wave asks for its places once
-        uint32_t mine = 0;
-        const bool some = max(max(v[0], v[1]), max(v[2], v[3])) >= bound;
-        if (__ballot(some)) {
-            // (unpacked again each time: nothing is kept from the sums to here)
-            if (some)
-#pragma unroll
-                for (int u = 0; u < kScoreU; ++u) {
-                    x[u].repack();
-#pragma unroll
-                    for (int e = 0; e < N; ++e) mine += x[u].get(e) >= least;
-                }
-            const uint32_t upto = wave_scan(mine);
-            uint32_t at = 0;
-            if ((tid & 63) == 63) at = atomicAdd(&s.count, upto);
-            at = (uint32_t)__builtin_amdgcn_readlane((int)at, 63) + upto - mine;
-            if (some)
-#pragma unroll
-                for (int u = 0; u < kScoreU; ++u) {
-                    x[u].repack();
-#pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (x[u].get(e) >= least) add(at++, x[u].get(e), span.r.piece(span.first + tid + THREADS * u) + e);
-                }
-        }
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < kGroups; ++i)
-            if (v[i] >= bound)
-                for (uint32_t q = i * (kSubs / kGroups); q < (i + 1) * (kSubs / kGroups); ++q)
-                    if (s.high[q * THREADS + tid] >= bound) {
-                        const uint32_t at = atomicAdd(&s.groups, 1u);
-                        if (at < kCands) s.who[at] = (uint16_t)(q * THREADS + tid);
-                    }
-        __syncthreads();
-        if (span.singles && single >= least) add(atomicAdd(&s.count, 1u), single, span.r.single(tid));
-        // a lane a group, and the lanes that are left over at its further pieces
-        // (each group has a candidate: too many groups are too many of these)
-        const uint32_t groups = s.groups, wide = groups <= 1 ? 0 : 32 - __clz((int)(groups - 1));
-        const uint32_t lanes = min(1u << wide, (uint32_t)THREADS), apart = THREADS / lanes;
-        if (groups > kCands && tid == 0) s.count = kCands + 1;
-        for (uint32_t g = tid & (lanes - 1); g < groups && groups <= kCands; g += lanes) {
-            const uint32_t w = s.who[g], at = w % THREADS;
-            for (uint32_t nth = tid / lanes; nth < per * K; nth += apart) {
-                const uint64_t j = span.first + long_piece<K, THREADS>((uint64_t)(w / THREADS) * per + nth / K, nth % K, at);
-                if (j >= span.end) break;
-                Piece<TYPE> y;
-                y.w = load_vec<u32x4, true>(span.row + span.r.piece((uint32_t)j));
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (y.get(e) >= least) add(atomicAdd(&s.count, 1u), y.get(e), span.r.piece((uint32_t)j) + e);
-            }
-        }
-    }
-    __syncthreads();
-    if (s.count > kCands)
-        narrow(s, n, [&](auto f) {
-            span.each([&](float y, uint32_t token) {
-                if (place(y)) f(key_of(place(y), token));
-            });
-        });
-    const uint32_t count = s.count;
-    put_in_order(s, count, n);
-    return min(count, n);
-}
-
-template <class Space>
-__device__ __forceinline__ void put_top(const ScoresOut& o, uint64_t t, const Space& s, uint32_t found,
-                                        Part p, float scale)
-{
-    for (uint32_t i = threadIdx.x; i < o.top; i += 64 * Space::kWaves) {
-        const uint64_t k = i < found ? s.out[i] : 0;
-        o.top_id[t * o.top + i] = i < found ? (int32_t)~(uint32_t)k : -1;
-        o.top_logp[t * o.top + i] = i < found ? (float)part_logp(p, placed((uint32_t)(k >> 32)), scale) : -INFINITY;
-    }
-}
-
-// ---------------------------------------------------------------- forward
-
-__device__ __forceinline__ bool scored(const Logits& in, uint64_t t) { return !in.label || has_token(in, t); }
-
-// Slice s of a row: pieces [s W, (s + 1) W); slice 0 takes the singles too.
-// With one slice a row its scores at once, else its part and its list.  ONE: a
-// slice is a turn, kScoreU pieces a thread.
-template <int TYPE, int THREADS, bool LIST, bool ONE>
-__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(LIST ? 5 : 6)))
-k_scores(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, ScorePart* part, uint64_t* keys)
+// A row's list, from its parts and groups; with more than one slice (at most 64)
+// its numbers too, by the last wave.  threads: of the pass.
+template <int TYPE, int THREADS, int LANES>
+__global__ void __launch_bounds__(THREADS) k_lists(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c,
+                                                   const ScorePart* part, Groups groups, uint32_t threads)
 {
     typedef typename Elem<TYPE>::type E;
-    constexpr int K = 16 / Piece<TYPE>::N;
-    __shared__ TopSpace<LIST ? THREADS : 64, ONE || !LIST> s_list;
-    __shared__ typename TopSpace<THREADS, ONE>::Wave s_wave[LIST ? 1 : THREADS / 64];
-    __shared__ float s_far[2][THREADS / 64];
-    const uint32_t tid = threadIdx.x, n = o.top;
-    for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
-        const uint64_t t = b / S;
-        const uint32_t s = (uint32_t)(b % S);
-        if (!scored(in, t)) {
-            if (S == 1) put_unused(o, t);
-            continue;
-        }
-        const E* row = static_cast<const E*>(in.x) + t * in.ld;
-        // (one wave has no lane for each single beside a line)
-        const RowCut<TYPE> r = THREADS == 64 ? RowCut<TYPE>((uint32_t)in.vocab) : RowCut<TYPE>(row, (uint32_t)in.vocab);
-        const uint32_t first = (uint32_t)min((uint64_t)r.full, (uint64_t)s * W);
-        const uint32_t end = (uint32_t)min((uint64_t)r.full, (uint64_t)(s + 1) * W);
-        auto fetch = [&](Piece<TYPE>& x, uint64_t j) {
-            x.none();
-            if (j < end) x.w = load_vec<u32x4>(row + r.piece((uint32_t)j));
-        };
-        const float single = s == 0 && tid < r.singles ? (float)row[r.single(tid)] : -INFINITY;
-        const float at = tid == 0 && in.label ? (float)row[in.label[t]] : 0.0f;
-        Piece<TYPE> x[kScoreU];
-        float most[kScoreU];
-        uint32_t v[kGroups] = {0, 0, 0, 0}, per = 0;
-        Tally own;
-        if constexpr (ONE) {
-#pragma unroll
-            for (int u = 0; u < kScoreU; ++u) fetch(x[u], (uint64_t)first + tid + THREADS * u);
-            own.add_one(single, c);
-#pragma unroll
-            for (int u = 0; u < kScoreU; u += K) own.add<TYPE, K>(x + u, most + u, c);
-            if (LIST)
-#pragma unroll
-                for (int u = 0; u < kScoreU; ++u) v[u] = place(most[u]);
-        } else {
-            // K pieces at a time, the next ones under way (loads past the end
-            // read the last piece, and count for nothing)
-            const uint32_t count = end - first, turns = (count + K * THREADS - 1) / (K * THREADS);
-            const uint32_t below = tid & ~63u;  // a wave has mine of the turns
-            const uint32_t mine = count > below ? (count - below + K * THREADS - 1) / (K * THREADS) : 0u;
-            per = (turns + kSubs - 1) / kSubs;
-            const uint8_t* from = reinterpret_cast<const uint8_t*>(row + r.piece(first));
-            const uint32_t last = count ? (count - 1) * 16 : 0;
-            Piece<TYPE> y[K];
-            auto ask = [&](Piece<TYPE>(&q)[K], uint32_t turn) {
-#pragma unroll
-                for (int u = 0; u < K; ++u)
-                    q[u].w = load_vec<u32x4>(reinterpret_cast<const E*>(
-                        from + min((uint32_t)long_piece<K, THREADS>(turn, u, tid) * 16, last)));
-            };
-            float group = -INFINITY;
-            uint32_t left = per, sub = 0;
-            if (LIST)
-#pragma unroll
-                for (uint32_t q = 0; q < kSubs; ++q) s_list.high[q * THREADS + tid] = 0;  // (its own places: no barrier)
-            auto take = [&](Piece<TYPE>(&q)[K], uint32_t turn) {
-                if (turn + 1 == mine)
-#pragma unroll
-                    for (int u = 0; u < K; ++u)
-                        if (long_piece<K, THREADS>(turn, u, tid) >= count) q[u].none();
-                const float high = own.add<TYPE, K>(q, most, c);
-                if (LIST) {
-                    group = largest(group, high, high);
-                    if (--left == 0 || turn + 1 == mine) {
-                        s_list.high[sub * THREADS + tid] = place(group);
-                        group = -INFINITY;
-                        left = per;
-                        ++sub;
-                    }
-                }
-            };
-            Piece<TYPE>(&z)[K] = reinterpret_cast<Piece<TYPE>(&)[K]>(x);
-            if (mine) ask(z, 0);
-            own.add_one(single, c);
-            for (uint32_t turn = 0; turn < mine; turn += 2) {
-                if (turn + 1 < mine) ask(y, turn + 1);
-                take(z, turn);
-                if (turn + 1 >= mine) break;
-                if (turn + 2 < mine) ask(z, turn + 2);
-                take(y, turn + 1);
-            }
-            if (LIST)
-#pragma unroll
-                for (uint32_t q = 0; q < kSubs; ++q)
-                    v[q / (kSubs / kGroups)] = max(v[q / (kSubs / kGroups)], s_list.high[q * THREADS + tid]);
-        }
-        const Span<TYPE> span = {row, r, first, end, s == 0};
-        ScorePart p = own.join_lanes(c);
-        if constexpr (LIST) {
-            put_wave(s_list, p, v);
-            clear_counts(s_list);
-            __syncthreads();
-            p = join_parts<THREADS / 64>(s_list.wave, c, max(n, 1u));
-        } else {
-            if ((tid & 63) == 0) s_wave[tid >> 6] = {p.top, p.sum, p.bend, 0, 0, 0};
-            __syncthreads();
-            p = join_parts<THREADS / 64>(s_wave, c, 1u);
-        }
-        if (p.top != -INFINITY && !(fabsf(p.top * c) < kFar)) {
-            __syncthreads();  // (s_far lies apart, but the waves' parts are read above)
-            p = far_part<TYPE, THREADS>(span, p.top, c, s_far);
-        }
-        if (p.top == -INFINITY) p.top = 0.0f;
-        if (tid == 0) {
-            if (S > 1)
-                part[b] = p;
-            else
-                put_scores(o, t, p, in.label != nullptr, at, in.scale);
-        }
-        if constexpr (LIST) {
-            const uint32_t found = top_of<TYPE, THREADS, ONE>(s_list, span, n, per, x, v, single);
-            if (S > 1)
-                for (uint32_t i = tid; i < n; i += THREADS) keys[b * n + i] = i < found ? s_list.out[i] : 0;
-            else
-                put_top(o, t, s_list, found, Part{p.top, p.sum}, in.scale);
-        }
-        __syncthreads();
-    }
-}
-
-// A row's slices joined (at most 64 of them).
-template <int TYPE>
-__global__ void __launch_bounds__(256) k_join_scores(Logits in, ScoresOut o, uint32_t S, float c,
-                                                     const ScorePart* part, const uint64_t* keys)
-{
-    typedef typename Elem<TYPE>::type E;
-    __shared__ TopSpace<256, true> s_space;
+    constexpr int N = Piece<TYPE>::N, R = (LANES == 1 ? kLaneGroups : kLineGroups) / 256;
+    constexpr uint32_t kCands = TopSpace<THREADS>::kCands;
+    __shared__ TopSpace<THREADS> s;
     const uint32_t tid = threadIdx.x, n = o.top;
     for (uint64_t t = blockIdx.x; t < in.rows; t += gridDim.x) {
         if (!scored(in, t)) {
-            put_unused(o, t);
+            if (S > 1) put_unused(o, t);
             continue;
         }
-        // a lane of the first wave a slice, and the first of every slice's list
-        // for a bound: 2 n keys and more (at most 2 n + 64 of them)
-        const uint64_t* list = keys + t * S * n;
-        const uint32_t heads = n ? min(n, (2 * n + S - 1) / S) : 0;
-        uint32_t v[kGroups];
+        const E* row = static_cast<const E*>(in.x) + t * in.ld;
+        const RowCut<TYPE> r = cut_of<TYPE>(row, (uint32_t)in.vocab, threads == 64);
+        const bool last = tid >= THREADS - 64;
+        const uint32_t lane = tid & 63;
+        ScorePart p = {0.0f, 0.0f, 0.0f};
+        float at = 0.0f;
+        if (last && lane < S) p = part[t * S + lane];
+        if (last && S > 1 && in.label) at = (float)row[in.label[t]];
+        uint32_t v[LANES ? R : 1];
+        if (LANES) {
+            const uint32_t* group = groups.largest + t * S * groups.each;
 #pragma unroll
-        for (uint32_t k = 0; k < kGroups; ++k) {
-            const uint32_t i = tid + 256 * k;
-            v[k] = i < S * heads ? (uint32_t)(list[(uint64_t)(i / heads) * n + i % heads] >> 32) : 0u;
+            for (int e = 0; e < R; ++e) v[e] = tid + e * THREADS < S * groups.each ? group[tid + e * THREADS] : 0u;
         }
-        ScorePart p = tid < S ? part[t * S + tid] : ScorePart{0.0f, 0.0f, 0.0f};
-        if (p.sum == 0.0f) p.top = -INFINITY;
-        const float top = wave_join<false>(p.top);
-        p = moved(p, top, c);
-        put_wave(s_space, ScorePart{top, wave_join<true>(p.sum), wave_join<true>(p.bend)}, v);
-        clear_counts(s_space);
-        __syncthreads();
-        p = join_parts<4>(s_space.wave, c, max(n, 1u));
-        if (p.top == -INFINITY) p.top = 0.0f;
-        if (tid == 0) {
-            const float at = in.label ? (float)(static_cast<const E*>(in.x) + t * in.ld)[in.label[t]] : 0.0f;
-            put_scores(o, t, p, in.label != nullptr, at, in.scale);
+        if (tid == 0) s.count = s.groups = 0;
+        if (last) {
+            // (a lane a slice)
+            if (p.sum == 0.0f) p.top = -INFINITY;
+            const float top = wave_join<false>(p.top);
+            p = moved(p, top, c);
+            p = {top == -INFINITY ? 0.0f : top, wave_join<true>(p.sum), wave_join<true>(p.bend)};
+            if (lane == 0) s.part = p;
         }
-        if (n) {
-            constexpr uint32_t kCands = TopSpace<256, true>::kCands;
-            const uint32_t bound = find_bound(s_space, v, n);
-            auto each = [&](auto f) {
-                for (uint32_t i = tid; i < S * n; i += 256)
-                    if (const uint64_t k = list[i]) f(k);
-            };
-            each([&](uint64_t k) {
-                if ((uint32_t)(k >> 32) < bound) return;
-                const uint32_t at = atomicAdd(&s_space.count, 1u);
-                if (at < kCands) s_space.key[at] = k;
+        if constexpr (LANES > 0) {
+            const uint32_t bound = find_bound(s, n, [&](auto f) {
+#pragma unroll
+                for (int e = 0; e < R; ++e) f(v[e]);
             });
+            const float least = bound > place(-3.402823466e38f) ? placed(bound) : -3.402823466e38f;
+            auto add = [&](float y, uint32_t token) {
+                const uint32_t at = atomicAdd(&s.count, 1u);
+                if (at < kCands) s.key[at] = key_of(place(y), token);
+            };
+#pragma unroll
+            for (int e = 0; e < R; ++e)
+                if (v[e] >= bound) {
+                    const uint32_t i = tid + e * THREADS, at = atomicAdd(&s.groups, 1u);
+                    // the group's first piece, and the end of its slice
+                    const uint32_t slice = S == 1 ? 0 : i / groups.each, g = i - slice * groups.each;
+                    const uint32_t row_of = threads / LANES;
+                    if (at < kCands) {
+                        s.who[at] = slice * W + g / row_of * groups.units * threads + g % row_of * LANES;
+                        s.stop[at] = min(r.full, (slice + 1) * W);
+                    }
+                }
+            for (uint32_t i = tid; i < r.singles; i += THREADS) {
+                const float y = (float)row[r.single(i)];
+                if (y >= least) add(y, r.single(i));
+            }
             __syncthreads();
-            if (s_space.count > kCands) narrow(s_space, n, each);
-            const uint32_t count = s_space.count;
-            put_in_order(s_space, count, n);
-            put_top(o, t, s_space, min(count, n), Part{p.top, p.sum}, in.scale);
+            // a lane a piece (each group has a candidate: too many groups are too
+            // many of these)
+            const uint32_t found = s.groups, pieces = groups.units * LANES, shift = 31 - __clz((int)pieces);
+            if (found > kCands && tid == 0) s.count = kCands + 1;
+            for (uint32_t i = tid; i < found << shift && found <= kCands; i += THREADS) {
+                const uint32_t w = i >> shift, k = i & (pieces - 1), j = s.who[w] + k / LANES * threads + k % LANES;
+                if (j >= s.stop[w]) continue;
+                Piece<TYPE> y;
+                y.w = load_vec<u32x4, true>(row + r.piece(j));
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (y.get(e) >= least) add(y.get(e), r.piece(j) + e);
+            }
+            __syncthreads();
+            if (s.count > kCands)
+                narrow(s, n, [&](auto f) {
+                    for (uint32_t i = tid; i < r.singles; i += THREADS)
+                        if (const uint32_t k = place((float)row[r.single(i)])) f(key_of(k, r.single(i)));
+                    for (uint64_t j = tid; j < r.full; j += THREADS) {
+                        Piece<TYPE> y;
+                        y.w = load_vec<u32x4, true>(row + r.piece((uint32_t)j));
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (const uint32_t k = place(y.get(e))) f(key_of(k, r.piece((uint32_t)j) + e));
+                    }
+                });
+            const uint32_t count = s.count;
+            put_in_order(s, count, n);
+            const Part q = {s.part.top, s.part.sum};
+            for (uint32_t i = tid; i < n; i += THREADS) {
+                const uint64_t k = i < count ? s.out[i] : 0;
+                o.top_id[t * n + i] = i < count ? (int32_t)~(uint32_t)k : -1;
+                o.top_logp[t * n + i] = i < count ? (float)part_logp(q, placed((uint32_t)(k >> 32)), in.scale) : -INFINITY;
+            }
         }
+        if (S > 1 && tid == THREADS - 64) put_scores(o, t, p, in.label != nullptr, at, in.scale);
         __syncthreads();
     }
 }
@@ -894,11 +855,14 @@ k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits, ui
 // ---------------------------------------------------------------- host
 
 constexpr uint32_t kScoreGrid = 1u << 21;  // (of up to 1024 threads each)
-constexpr int kLongThreads = 256;  // of a row of several turns
-constexpr uint64_t kScoreSlices = 1024;  // of few rows together
+constexpr uint64_t kScoreSlices = 1024;    // of few rows together
+constexpr int kLongThreads = 256;          // of a row of several turns
 
+// S slices of W pieces; groups of `lanes` (0: no list) and `units`, `each` a
+// slice.
 struct ScoreCut {
-    uint32_t S, W, threads;
+    uint32_t S, W, threads, lanes, units, each;
+    bool one;
 };
 // Slices of a row at most.
 uint64_t most_score_slices(uint64_t pieces) { return std::min<uint64_t>(64, (pieces + 511) / 512); }
@@ -907,76 +871,105 @@ ScoreCut cut_scores(uint64_t rows, uint64_t vocab, uint32_t type, uint32_t top)
     ScoreCut r;
     const uint64_t pieces = vocab / (type == kF32 ? 4 : 8) + 1;
     const uint64_t want = kScoreSlices / std::min(rows, kScoreSlices);
-    const uint64_t S = std::max<uint64_t>(1, std::min(most_score_slices(pieces), want));
-    r.W = (uint32_t)((pieces + S - 1) / S);
-    r.S = (uint32_t)((pieces + r.W - 1) / r.W);
-    const uint32_t threads = (r.W + kScoreU - 1) / kScoreU;
-    r.threads = threads <= 64 ? 64 : threads <= 128 ? 128 : threads <= 256 ? 256 : 512;
-    if (top > 64) r.threads = std::max(r.threads, 256u);
-    return r;
+    for (uint64_t S = std::max<uint64_t>(1, std::min(most_score_slices(pieces), want));; S /= 2) {
+        r.W = (uint32_t)(((pieces + S - 1) / S + 7) / 8 * 8);
+        r.S = (uint32_t)((pieces + r.W - 1) / r.W);
+        const uint32_t threads = (r.W + kScoreU - 1) / kScoreU;
+        r.one = threads <= 512;
+        r.threads = threads <= 64 ? 64 : threads <= 128 ? 128 : threads <= 256 ? 256 : r.one ? 512 : kLongThreads;
+        // (a group of lines of each lane at least)
+        if (!top || S == 1 || r.S * (r.threads / 8) <= kLineGroups) break;
+    }
+    r.lanes = r.units = r.each = 0;
+    if (!top) return r;
+    // groups of lines, unless the list is more than half as long as they are many
+    const uint32_t least = r.one ? 1 : type == kF32 ? 4 : 2, all = r.one ? kScoreU : (r.W + r.threads - 1) / r.threads;
+    for (r.lanes = 8;; r.lanes = 1) {
+        const uint32_t most = r.lanes == 8 ? kLineGroups : kLaneGroups;
+        for (r.units = least;; r.units *= 2) {
+            r.each = (all + r.units - 1) / r.units * (r.threads / r.lanes);
+            if (r.S * r.each <= most || r.units >= all) break;
+        }
+        if (r.lanes == 1 || r.S * r.each >= 2 * top) return r;
+    }
 }
 
 struct ScoreSpace {
     ScorePart* part;
-    uint64_t* keys;
+    uint32_t* largest;
 };
-ScoreSpace carve_scores(void* ws, uint64_t parts, uint32_t top, size_t* bytes)
+ScoreSpace carve_scores(void* ws, uint64_t parts, uint64_t groups, size_t* bytes)
 {
     Carve c(ws);
     ScoreSpace r;
     r.part = c.take<ScorePart>(parts);
-    r.keys = c.take<uint64_t>(parts * top);
+    r.largest = c.take<uint32_t>(groups);
     if (bytes) *bytes = c.used;
     return r;
 }
 
 }  // namespace
 
-// (Enough for every type and for every call of fewer rows, a smaller
-// vocabulary or shorter lists: parts are counted by what bounds them.)
+// (Enough for every type and for every call of fewer rows, a smaller vocabulary
+// or shorter lists: parts and groups are counted by what bounds them.)
 size_t scores_workspace(uint32_t top, uint64_t rows, uint64_t vocab)
 {
-    const uint64_t pieces = vocab / 4 + 1;
     size_t b = 0;
-    Carve c(nullptr);
-    const uint64_t parts = std::min(kScoreSlices, rows * most_score_slices(pieces));
-    c.take<ScorePart>(parts);
-    c.take<uint64_t>(parts * top);
-    b = c.used;
+    carve_scores(nullptr, std::max(rows, std::min(kScoreSlices, rows * most_score_slices(vocab / 4 + 1))),
+                 top ? rows * kLaneGroups : 0, &b);
     return b;
 }
 
 hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_t s)
 {
     const ScoreCut cut = cut_scores(in.rows, in.vocab, in.type, o.top);
-    const ScoreSpace sp = carve_scores(ws, cut.S > 1 ? in.rows * cut.S : 0, o.top, nullptr);
+    const ScoreSpace sp = carve_scores(ws, in.rows * cut.S, in.rows * cut.S * cut.each, nullptr);
+    const Groups groups = {sp.largest, cut.units, cut.each};
     const float c = in.scale * kLog2e;
     const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kScoreGrid);
+    const uint32_t rows = (uint32_t)std::min<uint64_t>(in.rows, kScoreGrid);
     timer_begin(kTScores, s);
     by_type(in.type, [&](auto ty) {
         constexpr int TY = decltype(ty)::value;
-        auto go = [&](auto kern, uint32_t threads) {
-            hipLaunchKernelGGL(kern, dim3(grid), dim3(threads), 0, s, in, o, cut.S, cut.W, c, sp.part, sp.keys);
-        };
-        auto with = [&](auto threads, auto one) {
-            constexpr int T = decltype(threads)::value;
-            constexpr bool O = decltype(one)::value;
-            o.top ? go(k_scores<TY, T, true, O>, T) : go(k_scores<TY, T, false, O>, T);
-        };
         typedef std::true_type Y;
-        switch (cut.threads) {
-        case 64: with(std::integral_constant<int, 64>(), Y()); break;
-        case 128: with(std::integral_constant<int, 128>(), Y()); break;
-        case 256: with(std::integral_constant<int, 256>(), Y()); break;
-        default:
-            if (cut.W <= kScoreU * 512)
-                with(std::integral_constant<int, 512>(), Y());
+        auto by_lanes = [&](auto f) {
+            if (cut.lanes == 8)
+                f(std::integral_constant<int, 8>());
+            else if (cut.lanes == 1)
+                f(std::integral_constant<int, 1>());
             else
-                with(std::integral_constant<int, kLongThreads>(), std::false_type());
-        }
-        if (cut.S > 1)
-            hipLaunchKernelGGL((k_join_scores<TY>), dim3((uint32_t)std::min<uint64_t>(in.rows, kScoreGrid)), dim3(256), 0,
-                               s, in, o, cut.S, c, sp.part, sp.keys);
+                f(std::integral_constant<int, 0>());
+        };
+        auto pass = [&](auto threads, auto one) {
+            by_lanes([&](auto lanes) {
+                constexpr int T = decltype(threads)::value;
+                hipLaunchKernelGGL((k_scores<TY, T, decltype(lanes)::value, decltype(one)::value>), dim3(grid), dim3(T), 0, s,
+                                   in, o, cut.S, cut.W, c, sp.part, groups);
+            });
+        };
+        if (!cut.one)
+            pass(std::integral_constant<int, kLongThreads>(), std::false_type());
+        else if (cut.threads == 64)
+            pass(std::integral_constant<int, 64>(), Y());
+        else if (cut.threads == 128)
+            pass(std::integral_constant<int, 128>(), Y());
+        else if (cut.threads == 256)
+            pass(std::integral_constant<int, 256>(), Y());
+        else
+            pass(std::integral_constant<int, 512>(), Y());
+        if (!cut.lanes && cut.S == 1) return;
+        by_lanes([&](auto lanes) {
+            constexpr int L = decltype(lanes)::value;
+            auto go = [&](auto threads) {
+                constexpr int T = decltype(threads)::value;
+                hipLaunchKernelGGL((k_lists<TY, T, L>), dim3(rows), dim3(T), 0, s, in, o, cut.S, cut.W, c, sp.part, groups,
+                                   cut.threads);
+            };
+            if (cut.S * cut.each <= (L == 1 ? kLaneGroups : kLineGroups) / 4 && o.top <= 64)
+                go(std::integral_constant<int, 64>());
+            else
+                go(std::integral_constant<int, 256>());
+        });
     });
     timer_end(kTScores, s);
     return hipGetLastError();
