@@ -495,27 +495,13 @@ __device__ __forceinline__ void sort_lanes(uint64_t& k)
     exchange<RUN, RUN / 2>(k);
 }
 
-// The n largest of s.key[0, count) in order to s.out, count <= kCands: up to 128
-// by counting the larger ones, beyond by waves that put 64 at a time in order
-// and look up how many of each other 64 are larger.
+// The n largest of s.key[0, count) in order to s.out, count <= kCands: waves put
+// 64 at a time in order and look up how many of each other 64 are larger.
 template <int THREADS>
 __device__ __forceinline__ void put_in_order(TopSpace<THREADS>& s, uint32_t count, uint32_t n)
 {
     constexpr uint32_t kWaves = THREADS / 64;
-    const uint32_t tid = threadIdx.x;
-    if (count <= 128) {
-        for (uint32_t i = tid; i < count; i += THREADS) {
-            const uint64_t k = s.key[i];
-            uint32_t rank = 0;
-            for (uint32_t j = 0; j < count; j += 8)
-#pragma unroll
-                for (uint32_t e = 0; e < 8; ++e) rank += j + e < count && s.key[j + e] > k;
-            if (rank < n) s.out[rank] = k;
-        }
-        __syncthreads();
-        return;
-    }
-    const uint32_t lane = tid & 63, wave = tid >> 6, blocks = (count + 63) / 64;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = (count + 63) / 64;
     for (uint32_t b = wave; b < blocks; b += kWaves) {
         uint64_t k = 64 * b + lane < count ? s.key[64 * b + lane] : 0;
         sort_lanes<64>(k);
@@ -586,13 +572,13 @@ __device__ __attribute__((noinline)) void narrow(TopSpace<THREADS>& s, uint32_t 
 }
 
 // A row's list, from its parts and groups; with more than one slice (at most 64)
-// its numbers too, by the last wave.  threads: of the pass.
-template <int TYPE, int THREADS, int LANES>
+// its numbers too, by the last wave.  R groups a thread; threads: of the pass.
+template <int TYPE, int THREADS, int LANES, int R>
 __global__ void __launch_bounds__(THREADS) k_lists(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c,
                                                    const ScorePart* part, Groups groups, uint32_t threads)
 {
     typedef typename Elem<TYPE>::type E;
-    constexpr int N = Piece<TYPE>::N, R = (LANES == 1 ? kLaneGroups : kLineGroups) / 256;
+    constexpr int N = Piece<TYPE>::N;
     constexpr uint32_t kCands = TopSpace<THREADS>::kCands;
     __shared__ TopSpace<THREADS> s;
     const uint32_t tid = threadIdx.x, n = o.top;
@@ -655,14 +641,35 @@ __global__ void __launch_bounds__(THREADS) k_lists(Logits in, ScoresOut o, uint3
             // many of these)
             const uint32_t found = s.groups, pieces = groups.units * LANES, shift = 31 - __clz((int)pieces);
             if (found > kCands && tid == 0) s.count = kCands + 1;
-            for (uint32_t i = tid; i < found << shift && found <= kCands; i += THREADS) {
-                const uint32_t w = i >> shift, k = i & (pieces - 1), j = s.who[w] + k / LANES * threads + k % LANES;
-                if (j >= s.stop[w]) continue;
-                Piece<TYPE> y;
-                y.w = load_vec<u32x4, true>(row + r.piece(j));
+            // (eight of a lane's under way: a round trip to memory is 2 us)
+            for (uint32_t i = tid; i < found << shift && found <= kCands; i += 8 * THREADS) {
+                Piece<TYPE> y[8];
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (y.get(e) >= least) add(y.get(e), r.piece(j) + e);
+                for (int u = 0; u < 8; ++u) {
+                    const uint32_t w = min((i + u * THREADS) >> shift, kCands - 1), k = (i + u * THREADS) & (pieces - 1);
+                    y[u].none();
+                    const uint32_t j = s.who[w] + k / LANES * threads + k % LANES;
+                    if (i + u * THREADS < found << shift && j < s.stop[w]) y[u].w = load_vec<u32x4, true>(row + r.piece(j));
+                }
+                // (marks first, then a mark of each lane at a time, read once more:
+                // a place for every element in the code takes longer to fetch)
+                uint64_t marks = 0;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) m |= (uint32_t)(y[u].get(e) >= least) << e;
+                    marks |= (uint64_t)m << (8 * u);
+                }
+                while (__any(marks != 0)) {
+                    if (marks) {
+                        const uint32_t bit = (uint32_t)__ffsll((unsigned long long)marks) - 1;
+                        marks &= marks - 1;
+                        const uint32_t at = i + bit / 8 * THREADS, k = at & (pieces - 1);
+                        const uint32_t token = r.piece(s.who[at >> shift] + k / LANES * threads + k % LANES) + bit % 8;
+                        add((float)row[token], token);
+                    }
+                }
             }
             __syncthreads();
             if (s.count > kCands)
@@ -869,7 +876,7 @@ uint64_t most_score_slices(uint64_t pieces) { return std::min<uint64_t>(64, (pie
 ScoreCut cut_scores(uint64_t rows, uint64_t vocab, uint32_t type, uint32_t top)
 {
     ScoreCut r;
-    const uint64_t pieces = vocab / (type == kF32 ? 4 : 8) + 1;
+    const uint64_t pieces = std::max<uint64_t>(1, vocab / (type == kF32 ? 4 : 8));
     const uint64_t want = kScoreSlices / std::min(rows, kScoreSlices);
     for (uint64_t S = std::max<uint64_t>(1, std::min(most_score_slices(pieces), want));; S /= 2) {
         r.W = (uint32_t)(((pieces + S - 1) / S + 7) / 8 * 8);
@@ -893,6 +900,8 @@ ScoreCut cut_scores(uint64_t rows, uint64_t vocab, uint32_t type, uint32_t top)
         if (r.lanes == 1 || r.S * r.each >= 2 * top) return r;
     }
 }
+
+constexpr uint64_t kManyLists = 1024;  // rows whose lists are by a wave each
 
 struct ScoreSpace {
     ScorePart* part;
@@ -925,6 +934,7 @@ hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_
     const ScoreCut cut = cut_scores(in.rows, in.vocab, in.type, o.top);
     const ScoreSpace sp = carve_scores(ws, in.rows * cut.S, in.rows * cut.S * cut.each, nullptr);
     const Groups groups = {sp.largest, cut.units, cut.each};
+    const bool many = in.rows >= kManyLists;
     const float c = in.scale * kLog2e;
     const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kScoreGrid);
     const uint32_t rows = (uint32_t)std::min<uint64_t>(in.rows, kScoreGrid);
@@ -960,15 +970,26 @@ hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_
         if (!cut.lanes && cut.S == 1) return;
         by_lanes([&](auto lanes) {
             constexpr int L = decltype(lanes)::value;
-            auto go = [&](auto threads) {
+            auto go = [&](auto threads, auto held) {
                 constexpr int T = decltype(threads)::value;
-                hipLaunchKernelGGL((k_lists<TY, T, L>), dim3(rows), dim3(T), 0, s, in, o, cut.S, cut.W, c, sp.part, groups,
-                                   cut.threads);
+                hipLaunchKernelGGL((k_lists<TY, T, L, decltype(held)::value>), dim3(rows), dim3(T), 0, s, in, o, cut.S, cut.W, c,
+                                   sp.part, groups, cut.threads);
             };
-            if (cut.S * cut.each <= (L == 1 ? kLaneGroups : kLineGroups) / 4 && o.top <= 64)
-                go(std::integral_constant<int, 64>());
-            else
-                go(std::integral_constant<int, 256>());
+            typedef std::integral_constant<int, 64> One;
+            typedef std::integral_constant<int, 256> Four;
+            const uint32_t all = cut.S * cut.each;
+            if ((many || all <= 256) && o.top <= 128 && L) {
+                if (all <= 256)
+                    go(One(), std::integral_constant<int, 4>());
+                else if (all <= 512)
+                    go(One(), std::integral_constant<int, 8>());
+                else if (all <= 1024)
+                    go(One(), std::integral_constant<int, 16>());
+                else
+                    go(One(), std::integral_constant<int, L == 1 ? 32 : 16>());
+            } else {
+                go(Four(), std::integral_constant<int, L == 1 ? 8 : 4>());
+            }
         });
     });
     timer_end(kTScores, s);
