@@ -13,9 +13,12 @@
 // a lane's pieces where a list is long for its row), and the n-th largest of
 // these is a bound that at least n logits reach and few more do (of 1024 groups
 // about 66 for n = 64).  A second launch finds it, looks through the groups that
-// reach it once more, and puts what it finds in order.
-// (Lists by the first pass' own workgroups kept these from their next row: 4096
-// x 131072 bf16 with 64 tokens 190 us, 8192 x 8000 with 20 80 us.)
+// reach it once more, and puts what it finds in order.  In the pass' own
+// workgroups, where a list keeps these from their next row, it takes 190 us
+// against 212 at 4096 x 131072 bf16 with 64 tokens, but 15.5 against 12.3 at 5 x
+// 131072 f32 with 20, 93 against 87 at 4096 x 50001 bf16 and 80 against 53 at
+// 8192 x 8000; without a list these are 163, 7, 66 and 33 us, of which the reads
+// alone take 151, 0.4, 58 and 18.
 #include "rows_device.h"
 
 #include <algorithm>
@@ -401,16 +404,22 @@ k_scores(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, ScorePart* par
 
 // ---------------------------------------------------------------- lists
 
-// What a row's list is found in; up to kCands candidates.
+// What a row's list is found in; up to kCands candidates.  (Little, where a wave
+// has a row: the waves of a CU wait for memory in turn.)
+constexpr uint32_t kShortTop = 64;
 template <int THREADS>
 struct TopSpace {
-    static constexpr uint32_t kWaves = THREADS / 64, kCands = THREADS == 64 ? 512 : 1024;
+    static constexpr uint32_t kWaves = THREADS / 64, kCands = THREADS == 64 ? 256 : 1024;
+    static constexpr uint32_t kTop = THREADS == 64 ? kShortTop : kMaxTop;
     uint32_t count, groups, bound, above;
     uint32_t there[kWaves], low[kWaves], high[kWaves];
     ScorePart part;
     alignas(16) uint32_t hist[256];
-    uint32_t who[kCands], stop[kCands];  // groups at or above the bound: first piece, end
-    uint64_t key[kCands], out[kMaxTop];
+    union {
+        uint32_t who[kCands];  // first pieces of groups at or above the bound
+        uint64_t out[kTop];    // the list in order
+    };
+    uint64_t key[kCands];  // candidates
 };
 
 // A bound that at least n of the numbers that each(f) calls f with reach (1 if
@@ -574,8 +583,8 @@ __device__ __attribute__((noinline)) void narrow(TopSpace<THREADS>& s, uint32_t 
 // A row's list, from its parts and groups; with more than one slice (at most 64)
 // its numbers too, by the last wave.  R groups a thread; threads: of the pass.
 template <int TYPE, int THREADS, int LANES, int R>
-__global__ void __launch_bounds__(THREADS) k_lists(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c,
-                                                   const ScorePart* part, Groups groups, uint32_t threads)
+__global__ void __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(THREADS == 64 && R <= 16 ? 5 : 4)))
+k_lists(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, const ScorePart* part, Groups groups, uint32_t threads)
 {
     typedef typename Elem<TYPE>::type E;
     constexpr int N = Piece<TYPE>::N;
@@ -624,13 +633,10 @@ __global__ void __launch_bounds__(THREADS) k_lists(Logits in, ScoresOut o, uint3
             for (int e = 0; e < R; ++e)
                 if (v[e] >= bound) {
                     const uint32_t i = tid + e * THREADS, at = atomicAdd(&s.groups, 1u);
-                    // the group's first piece, and the end of its slice
+                    // the group's first piece
                     const uint32_t slice = S == 1 ? 0 : i / groups.each, g = i - slice * groups.each;
                     const uint32_t row_of = threads / LANES;
-                    if (at < kCands) {
-                        s.who[at] = slice * W + g / row_of * groups.units * threads + g % row_of * LANES;
-                        s.stop[at] = min(r.full, (slice + 1) * W);
-                    }
+                    if (at < kCands) s.who[at] = slice * W + g / row_of * groups.units * threads + g % row_of * LANES;
                 }
             for (uint32_t i = tid; i < r.singles; i += THREADS) {
                 const float y = (float)row[r.single(i)];
@@ -641,47 +647,63 @@ __global__ void __launch_bounds__(THREADS) k_lists(Logits in, ScoresOut o, uint3
             // many of these)
             const uint32_t found = s.groups, pieces = groups.units * LANES, shift = 31 - __clz((int)pieces);
             if (found > kCands && tid == 0) s.count = kCands + 1;
-            // (eight of a lane's under way: a round trip to memory is 2 us)
-            for (uint32_t i = tid; i < found << shift && found <= kCands; i += 8 * THREADS) {
-                Piece<TYPE> y[8];
+            auto piece_of = [&](uint32_t i) {
+                const uint32_t k = i & (pieces - 1);
+                return s.who[i >> shift] + k / LANES * threads + k % LANES;
+            };
+            auto stop_of = [&](uint32_t j) { return S == 1 ? r.full : min(r.full, (j / W + 1) * W); };
+            // (several of a lane's under way: a round trip to memory is 2 us)
+            constexpr int U = THREADS == 64 ? 4 : 8;
+            for (uint32_t i = tid; i < found << shift && found <= kCands; i += U * THREADS) {
+                Piece<TYPE> y[U];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const uint32_t w = min((i + u * THREADS) >> shift, kCands - 1), k = (i + u * THREADS) & (pieces - 1);
+                for (int u = 0; u < U; ++u) {
                     y[u].none();
-                    const uint32_t j = s.who[w] + k / LANES * threads + k % LANES;
-                    if (i + u * THREADS < found << shift && j < s.stop[w]) y[u].w = load_vec<u32x4, true>(row + r.piece(j));
+                    if (i - tid + u * THREADS >= found << shift) continue;  // (of the whole workgroup)
+                    const uint32_t at = min(i + u * THREADS, (found << shift) - 1), j = piece_of(at);
+                    if (at == i + u * THREADS && j < stop_of(s.who[at >> shift])) y[u].w = load_vec<u32x4, true>(row + r.piece(j));
                 }
-                // (marks first, then a mark of each lane at a time, read once more:
-                // a place for every element in the code takes longer to fetch)
-                uint64_t marks = 0;
+                // (a mark of each lane at a time: a place in the code for every element
+                // takes longer to fetch)
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    uint32_t m = 0;
+                for (int u = 0; u < U; ++u) {
+                    if (i - tid + u * THREADS >= found << shift) continue;
+                    uint32_t marks = 0;
 #pragma unroll
-                    for (int e = 0; e < N; ++e) m |= (uint32_t)(y[u].get(e) >= least) << e;
-                    marks |= (uint64_t)m << (8 * u);
-                }
-                while (__any(marks != 0)) {
-                    if (marks) {
-                        const uint32_t bit = (uint32_t)__ffsll((unsigned long long)marks) - 1;
-                        marks &= marks - 1;
-                        const uint32_t at = i + bit / 8 * THREADS, k = at & (pieces - 1);
-                        const uint32_t token = r.piece(s.who[at >> shift] + k / LANES * threads + k % LANES) + bit % 8;
-                        add((float)row[token], token);
+                    for (int e = 0; e < N; ++e) marks |= (uint32_t)(y[u].get(e) >= least) << e;
+                    while (__any(marks != 0)) {
+                        if (marks) {
+                            const int e = __ffs((int)marks) - 1;
+                            marks &= marks - 1;
+                            float v = y[u].get(0);
+#pragma unroll
+                            for (int q = 1; q < N; ++q) v = e == q ? y[u].get(q) : v;
+                            add(v, r.piece(piece_of(i + u * THREADS)) + e);
+                        }
                     }
                 }
             }
             __syncthreads();
             if (s.count > kCands)
-                narrow(s, n, [&](auto f) {
+                // (by value: what a call might change stays in memory for all of the
+                // kernel, 88 against 93 us at 4096 x 50001 bf16 with 20 tokens)
+                narrow(s, n, [=, known = found <= kCands, of = s.who](auto f) {
                     for (uint32_t i = tid; i < r.singles; i += THREADS)
                         if (const uint32_t k = place((float)row[r.single(i)])) f(key_of(k, r.single(i)));
-                    for (uint64_t j = tid; j < r.full; j += THREADS) {
+                    // the groups that reach the bound, where they are known
+                    const uint32_t all = known ? found << shift : r.full;
+                    for (uint32_t i = tid; i < all; i += THREADS) {
+                        uint32_t j = i;
+                        if (known) {
+                            const uint32_t k = i & (pieces - 1), first = of[i >> shift];
+                            j = first + k / LANES * threads + k % LANES;
+                            if (j >= (S == 1 ? r.full : min(r.full, (first / W + 1) * W))) continue;
+                        }
                         Piece<TYPE> y;
-                        y.w = load_vec<u32x4, true>(row + r.piece((uint32_t)j));
+                        y.w = load_vec<u32x4, true>(row + r.piece(j));
 #pragma unroll
                         for (int e = 0; e < N; ++e)
-                            if (const uint32_t k = place(y.get(e))) f(key_of(k, r.piece((uint32_t)j) + e));
+                            if (const uint32_t k = place(y.get(e))) f(key_of(k, r.piece(j) + e));
                     }
                 });
             const uint32_t count = s.count;
@@ -978,7 +1000,7 @@ hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_
             typedef std::integral_constant<int, 64> One;
             typedef std::integral_constant<int, 256> Four;
             const uint32_t all = cut.S * cut.each;
-            if ((many || all <= 256) && o.top <= 128 && L) {
+            if (many && o.top <= kShortTop && L) {
                 if (all <= 256)
                     go(One(), std::integral_constant<int, 4>());
                 else if (all <= 512)
