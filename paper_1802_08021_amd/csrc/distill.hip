@@ -694,8 +694,11 @@ __global__ void __launch_bounds__(256) k_distill_grad(Logits in, DistillArgs a, 
 
 constexpr uint32_t kDistillGrid = 1u << 22;
 constexpr uint64_t kDistillSlices = 1024;   // of few rows together
-constexpr uint64_t kDistillMany = 128;      // from so many rows on, a workgroup a row,
-constexpr uint64_t kMarked = 5 * 32768;     // of at most so many logits
+// From so many rows on a workgroup a row, whose pieces it holds (bf16 with 64
+// tokens: 64 x 131072 30 us against 25 by slices and two launches, 128 x 131072
+// 30 against 38; 64 x 32000 16 against 15, 200 x 32000 17 against 24),
+constexpr uint64_t kDistillMany = 128;
+constexpr uint64_t kMarked = 5 * 32768;     // of at most so many logits (20 KB of marks)
 constexpr uint64_t kDistillRows = 1u << 21; // of a launch with a workgroup a row (fewer than 2^32 threads)
 constexpr uint32_t kDistillHold = 8, kDistillHoldLds = 3;
 

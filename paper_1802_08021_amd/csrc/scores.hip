@@ -391,6 +391,7 @@ k_scores(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, ScorePart* par
             __syncthreads();
             p = far_part<TYPE, THREADS>(row, r, first, end, s == 0, p.top, c, s_far);
         }
+        if (LANES == 8 && THREADS == 64) __syncthreads();
         if (LANES == 8)
             for (uint32_t i = tid; i < groups.each; i += THREADS) largest_of[i] = s_largest[i];
         if (p.top == -INFINITY) p.top = 0.0f;
@@ -923,7 +924,11 @@ ScoreCut cut_scores(uint64_t rows, uint64_t vocab, uint32_t type, uint32_t top)
     }
 }
 
-constexpr uint64_t kManyLists = 1024;  // rows whose lists are by a wave each
+// Rows whose lists are by a wave each, of at most kShortTop tokens; fewer have
+// 256 threads each (bf16: 512 x 131072 with 20 tokens 36 us against 41 by waves,
+// 1000 x 32000 with 64 27 against 35; 1500 x 32000 39 against 41, 8192 x 32000
+// 152 against 129, 8192 x 8000 with 20 82 against 53).
+constexpr uint64_t kManyLists = 1024;
 
 struct ScoreSpace {
     ScorePart* part;
@@ -946,8 +951,11 @@ ScoreSpace carve_scores(void* ws, uint64_t parts, uint64_t groups, size_t* bytes
 size_t scores_workspace(uint32_t top, uint64_t rows, uint64_t vocab)
 {
     size_t b = 0;
+    // (a wave's lanes with kScoreU groups each, or a group for every piece where the
+    // threads round up to a power of two: at most two for each of the row's)
+    const uint64_t groups = std::min<uint64_t>(kLaneGroups, std::max<uint64_t>(256, vocab + 4));
     carve_scores(nullptr, std::max(rows, std::min(kScoreSlices, rows * most_score_slices(vocab / 4 + 1))),
-                 top ? rows * kLaneGroups : 0, &b);
+                 top ? rows * groups : 0, &b);
     return b;
 }
 

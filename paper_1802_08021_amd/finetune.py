@@ -12,7 +12,10 @@ torch's: the next token is drawn from softmax(tanh(E[token]) @ W).
 
 The task: the right answer to token x is (7 x + 3) mod V.  Pairs of answers
 (right, wrong) come first, then answers drawn by the model itself with a
-reward for each right one.
+reward for each right one and, if asked for, one for the entropy of what they
+are drawn from (token_scores, token_scores_grad).  At the end a model that
+starts anew learns from the first one's most likely answers (token_scores,
+distill_loss).
 """
 from __future__ import annotations
 
@@ -96,9 +99,10 @@ class Trainer:
         self.step()
         return torch.stack(stats).mean(0)
 
-    def policy_step(self):
-        """Answers drawn by the model, rewarded where right.  Returns the mean
-        of the ranks' stats and the mean reward (device)."""
+    def policy_step(self, entropy=0.0):
+        """Answers drawn by the model, rewarded where right; entropy: what each
+        unit of the answers' mean entropy is worth beside that.  Returns the
+        mean of the ranks' stats and the mean reward (device)."""
         stats, rewards = [], []
         for rank in range(self.P):
             x = self.draw(self.T)
@@ -109,12 +113,34 @@ class Trainer:
             old, _ = S.token_logprob(z, y)
             ref, _ = S.token_logprob(self.logits(x, self.start)[1], y)
             weight = torch.full((self.T,), 1.0 / self.T, device=self.dev)
+            if entropy:
+                sure = S.token_scores(z)
+                more = S.token_scores_grad(z, sure["norm"], entropy=sure["entropy"], d_entropy=-entropy * weight)
             r = S.policy_loss(z, y, old, reward - reward.mean(), weight, ref=ref, kl=1e-3, dlogits="inplace")
+            if entropy:
+                r["dlogits"].add_(more)
             self.backward(rank, x, h, r["dlogits"])
             stats.append(r["stats"])
             rewards.append(reward.mean())
         self.step()
         return torch.stack(stats).mean(0), torch.stack(rewards).mean()
+
+    def distill_step(self, teacher, top=16, hard=0.0, beta=0.0):
+        """The teacher's `top` most likely answers to drawn tokens, with their
+        probabilities, and a share `hard` of the right ones.  Returns the mean
+        of the ranks' stats (device)."""
+        stats = []
+        for rank in range(self.P):
+            x = self.draw(self.T)
+            told = S.token_scores(teacher.logits(x)[1], top=top)
+            h, z = self.logits(x)
+            weight = torch.full((self.T,), 1.0 / self.T, device=self.dev)
+            r = S.distill_loss(z, told["top_id"], told["top_logp"], weight=weight, beta=beta, hard=hard,
+                               labels=self.right(x).int() if hard else None, dlogits="inplace")
+            self.backward(rank, x, h, r["dlogits"])
+            stats.append(r["stats"])
+        self.step()
+        return torch.stack(stats).mean(0)
 
 
 def main(argv=None):
@@ -122,6 +148,8 @@ def main(argv=None):
     ap.add_argument("--ranks", type=int, default=4)
     ap.add_argument("--pairs-steps", type=int, default=60)
     ap.add_argument("--policy-steps", type=int, default=60)
+    ap.add_argument("--distill-steps", type=int, default=60)
+    ap.add_argument("--entropy", type=float, default=0.0)
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=8)
     a = ap.parse_args(argv)
     t = Trainer(ranks=a.ranks, state_bits=a.state_bits)
@@ -132,10 +160,17 @@ def main(argv=None):
             print(f"pairs  {i + 1:3d}: loss {loss:.4f}, in order {won:.2f}, rewards {good:+.3f} {bad:+.3f}, "
                   f"norm {float(t.update.out[0]):.3f}", flush=True)
     for i in range(a.policy_steps):
-        stats, reward = t.policy_step()
+        stats, reward = t.policy_step(a.entropy)
         if i % 10 == 9:
             print(f"policy {i + 1:3d}: loss {float(stats[0]):+.4f}, KL {float(stats[2]):.4f}, "
                   f"right answers {float(reward):.3f}, norm {float(t.update.out[0]):.3f}", flush=True)
+    if a.distill_steps:
+        student = Trainer(ranks=a.ranks, state_bits=a.state_bits, seed=1)
+    for i in range(a.distill_steps):
+        stats = student.distill_step(t)
+        if i % 10 == 9:
+            print(f"distil {i + 1:3d}: divergence {float(stats[1]):.4f}, on the list {float(stats[3]):.3f}, "
+                  f"norm {float(student.update.out[0]):.3f}", flush=True)
 
 
 if __name__ == "__main__":
