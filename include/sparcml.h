@@ -693,7 +693,7 @@ SPARCML_API int sparcml_preference_loss(const sparcml_logits* in, int pairs, con
  * 0 there, the list holds -1 and -Inf.  A row that holds nothing but -Inf has
  * lse, log probability and norm[t][1] -Inf, norm[t][0] and entropy 0.  NaN or
  * +Inf among a row's logits makes its numbers NaN; the list then holds the
- * largest of the logits that are not NaN.
+ * largest of the logits that are not NaN (a signalling NaN may hide others).
  * Sums are taken in fp32 over the differences to the maximum, both terms of the
  * entropy (log of the sum, mean difference) without cancellation.
  *   logp, lse, entropy  device float[rows] or NULL; norm float[rows][2] or NULL.
@@ -721,9 +721,9 @@ SPARCML_API int sparcml_token_scores(const sparcml_logits* in, const sparcml_sco
  *   dlogits[t][v] = scale (d_logp [v == label] + sum_i d_top_i [v == top_id_i]
  *       + p_v (d_lse - d_logp - sum_i d_top_i - d_entropy (log p_v + entropy)))
  * Rows that are not in use, rows of nothing but -Inf and rows whose derivatives
- * are all 0 have a zero gradient and are not read; a token whose own logit is
- * -Inf has no log probability that moves (its derivative is left out), and no
- * gradient.  A derivative that is NULL is 0.  Entries of top_id outside
+ * are all 0 have a zero gradient, whatever else they hold; a token whose own
+ * logit is -Inf has no log probability that moves (its derivative is left out),
+ * and no gradient.  Where norm is NaN all of the row's gradient is.  A derivative that is NULL is 0.  Entries of top_id outside
  * [0, vocab) are none; a token that is there twice counts twice.
  *   norm, entropy, top_id  as sparcml_token_scores wrote them for these logits
  *            and this scale (entropy only with d_entropy, top_id with d_top).
@@ -768,8 +768,10 @@ SPARCML_API int sparcml_token_scores_grad(const sparcml_logits* in, const sparcm
  * formulas give (+Inf, where q > 0 and beta == 0), but its log probability does
  * not move: it has no derivative.  Where all tokens that are left to the
  * student are listed there is no rest, and its term is left out.  Factors
- * beyond fp32's range are held at its largest number.  What is computed of a
- * list is in fp64; sums over rows are taken in fp64 in a fixed order.
+ * beyond fp32's range are held at its largest number.  NaN or +Inf among a
+ * row's logits, or NaN among its values, makes its div, the sums and the row's
+ * gradient NaN (where nothing is left beside the list, its listed places).  What
+ * is computed of a list is in fp64; sums over rows are taken in fp64 in a fixed order.
  *   id       device int32, entry i of row t at id[t * ld + i]; value the same,
  *            of `type` (SPARCML_F32 / BF16 / F16).  1 <= count <= SPARCML_MAX_TOP,
  *            ld >= count.

@@ -216,7 +216,7 @@ __device__ __forceinline__ void finish_list(const DistillArgs& a, double scale, 
     const uint32_t lane = threadIdx.x & 63;
     const bool outside = rest.sum != 0.0f;
     const float M = fmaxf(s.top, outside ? rest.top : -INFINITY);
-    if (M == -INFINITY) {  // nothing but -Inf
+    if (M == -INFINITY && s.Z == 0.0) {  // nothing but -Inf (a sum of NaN has no largest)
         for (uint32_t i = lane; i < a.count; i += 64) list.e[i] = 0.0f;
         if (lane == 0) {
             list.row = DistillRow{0.0f, 0.0f, __builtin_nanf("")};

@@ -773,7 +773,7 @@ k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits, ui
         if (scored && s == 0 && tid < r.singles) single = (float)row[r.single(tid)];
         const float one = at == -INFINITY ? 0.0f : d_logp;
         double total = 0.0;
-        bool any = scored && ln > -INFINITY && (one != 0.0f || d_lse != 0.0f || d_h != 0.0f);
+        bool any = scored && ln != -INFINITY && (one != 0.0f || d_lse != 0.0f || d_h != 0.0f);
         if constexpr (LIST) {
             if (id < V) x = (float)row[id];
             if (x == -INFINITY) g = 0.0f;
@@ -793,7 +793,7 @@ k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits, ui
                 total += s_sum[w];
                 some |= s_some[w];
             }
-            any = any || (some && scored && ln > -INFINITY);
+            any = any || (some && scored && ln != -INFINITY);
         }
         if (!any) {
             const u32x4 zero = {0u, 0u, 0u, 0u};

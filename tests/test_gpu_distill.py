@@ -126,6 +126,38 @@ def test_masked_and_lost_places(T, V, kind):
             check(r, h, lab, ids, values, None, kind, **args)
 
 
+@pytest.mark.parametrize("T,V", [(9, 700), (9, 40000), (300, 700), (150, 140000)])
+def test_nan_stays_in_its_row_and_is_seen(T, V):
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    nan, K = float("nan"), 9
+    for rest, beta, hard in MODES:
+        say(f"[nan distill] {T} {V} {rest} {beta} {hard}")
+        x, label, _ = make(T, V, "float32", 11)
+        ids, values = teacher(x, K, 3, rest, 1.0)
+        lab = label if hard else None
+        good = S.distill_loss(x, ids, values, labels=lab, rest=rest, beta=beta, hard=hard)
+        off = torch.ones(T, V, device=dev, dtype=torch.bool).scatter_(1, ids.long(), False)
+        first = off.float().argmax(1)                  # an unlisted token of each row
+        x[0, first[0]] = nan
+        x[1, ids[1, 0].long()] = nan
+        x[2] = nan
+        x[3, first[3]] = INF
+        x[4, ids[4, 1].long()] = INF
+        x[5, off[5]], x[5, ids[5].long()] = -INF, nan  # nothing but NaN on the list
+        values[6, 2] = nan
+        for where in ("new", None, "inplace"):
+            r = S.distill_loss(x.clone(), ids, values, labels=lab, rest=rest, beta=beta, hard=hard, dlogits=where)
+            torch.cuda.synchronize()
+            assert bool(torch.isnan(r["div"][:7]).all()), r["div"][:7]
+            assert torch.equal(r["div"][7:], good["div"][7:]) and bool(torch.isnan(r["stats"][:2]).all())
+            if where:
+                bad = torch.isnan(r["dlogits"])
+                assert bool(bad[[0, 1, 2, 3, 4, 6]].all()), bad.all(1)[:7]
+                assert bool(bad[5, ids[5].long()].all())
+                assert torch.equal(r["dlogits"][7:], good["dlogits"][7:])
+
+
 def test_a_rest_of_little_is_not_lost():
     """Unlisted tokens that together have a ten millionth of the student's
     probability: their own gradient is as exact as any."""

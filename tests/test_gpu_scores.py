@@ -251,6 +251,24 @@ def test_rows_without_derivatives_are_not_read():
             assert bool(torch.isfinite(g.float()).all()) and not bool(g[2:4].any()) and bool(g[4].any())
 
 
+def test_gradient_of_nan_rows_is_nan():
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    for T, V in ((6, 30000), (400, 700), (1100, 40)):
+        x, label, gen = make(T, V, "float32", 9)
+        x[1, V // 2], x[2], x[3, V - 1] = float("nan"), float("nan"), INF
+        s = S.token_scores(x, label, 4)
+        rnd = lambda *shape: torch.randn(*shape, device=dev, generator=gen)  # noqa: E731
+        for more in (dict(d_logp=rnd(T)), dict(d_lse=rnd(T)), dict(entropy=s["entropy"], d_entropy=rnd(T)),
+                     dict(top_id=s["top_id"], d_top=rnd(T, 4))):
+            for where in ("new", "inplace"):
+                g = S.token_scores_grad(x.clone(), s["norm"], labels=label, dlogits=where, **more)
+                bad = torch.isnan(g).all(1)
+                # (no entry of row 2 is on its list, of which nothing is left)
+                assert bool(bad[1]) and bool(bad[3]) and (bool(bad[2]) or "d_top" in more), list(more)
+                assert bool(torch.isfinite(g[4:]).all()) and bool(torch.isfinite(g[0]).all())
+
+
 def test_masked_and_lowest_rows_have_gradients():
     from paper_1802_08021_amd import sparcml as S
     torch, dev = torch_dev()
