@@ -795,7 +795,8 @@ hipError_t distill_run(const Logits& in0, const DistillArgs& a0, float* div, flo
     // Threads of a row: 512 up to 7168 pieces (4096 x 56000 bf16 with 64 tokens 179
     // us against 183 with 1024, 60000 197 against 189; 2000 x 30000 fp32 99 against
     // 95), with pieces in LDS too (50001: 155 us against 166 without, 172 with 1024
-    // threads).
+    // threads; where several batches in turn leave nothing in cache 191, 195 with
+    // 1024 threads).
     const uint64_t most = cut.pieces <= 7168 ? 512 : 1024, size = in.type == kF32 ? 4 : 2;
     const uint64_t threads = 64 + std::max<uint64_t>(kMinThreads, (cut.pieces + kDistillHold * 64 - 1) / (kDistillHold * 64) * 64);
     const size_t lds = (in.vocab + 31) / 32 * 4 + 4;
