@@ -15,7 +15,7 @@
 // about 66 for n = 64).  A second launch finds it, looks through the groups that
 // reach it once more, and puts what it finds in order.  In the pass' own
 // workgroups, where a list keeps these from their next row, it takes 190 us
-// against 212 at 4096 x 131072 bf16 with 64 tokens, but 15.5 against 12.3 at 5 x
+// against 212 at 4096 x 131072 bf16 with 64 tokens, but 15.5 against 11.7 at 5 x
 // 131072 f32 with 20, 93 against 87 at 4096 x 50001 bf16 and 80 against 53 at
 // 8192 x 8000; without a list these are 163, 7, 66 and 33 us, of which the reads
 // alone take 151, 0.4, 58 and 18.
@@ -664,22 +664,39 @@ k_lists(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, const ScorePart
                     const uint32_t at = min(i + u * THREADS, (found << shift) - 1), j = piece_of(at);
                     if (at == i + u * THREADS && j < stop_of(s.who[at >> shift])) y[u].w = load_vec<u32x4, true>(row + r.piece(j));
                 }
-                // (a mark of each lane at a time: a place in the code for every element
-                // takes longer to fetch)
+                if constexpr (THREADS > 64) {
+                    // (all marks of a lane's in one run, their logits read again: 5 x 131072
+                    // fp32 with 256 tokens 23 us against 29)
+                    uint64_t marks = 0;
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (i - tid + u * THREADS >= found << shift) continue;
-                    uint32_t marks = 0;
+                    for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) marks |= (uint32_t)(y[u].get(e) >= least) << e;
-                    while (__any(marks != 0)) {
-                        if (marks) {
-                            const int e = __ffs((int)marks) - 1;
-                            marks &= marks - 1;
-                            float v = y[u].get(0);
+                        for (int e = 0; e < N; ++e) marks |= (uint64_t)(y[u].get(e) >= least) << (N * u + e);
+                    while (marks) {
+                        const uint32_t bit = (uint32_t)__ffsll((unsigned long long)marks) - 1;
+                        marks &= marks - 1;
+                        const uint32_t token = r.piece(piece_of(i + bit / N * THREADS)) + bit % N;
+                        add((float)row[token], token);
+                    }
+                } else {
+                    // (a piece's marks at a time, selected from registers: 4096 x 50001 bf16
+                    // with 20 tokens 87 us against 93; a place in the code for every element
+                    // takes longer to fetch)
 #pragma unroll
-                            for (int q = 1; q < N; ++q) v = e == q ? y[u].get(q) : v;
-                            add(v, r.piece(piece_of(i + u * THREADS)) + e);
+                    for (int u = 0; u < U; ++u) {
+                        if (i - tid + u * THREADS >= found << shift) continue;
+                        uint32_t marks = 0;
+#pragma unroll
+                        for (int e = 0; e < N; ++e) marks |= (uint32_t)(y[u].get(e) >= least) << e;
+                        while (__any(marks != 0)) {
+                            if (marks) {
+                                const int e = __ffs((int)marks) - 1;
+                                marks &= marks - 1;
+                                float v = y[u].get(0);
+#pragma unroll
+                                for (int q = 1; q < N; ++q) v = e == q ? y[u].get(q) : v;
+                                add(v, r.piece(piece_of(i + u * THREADS)) + e);
+                            }
                         }
                     }
                 }
