@@ -764,13 +764,14 @@ SPARCML_API int sparcml_token_scores_grad(const sparcml_logits* in, const sparcm
  * its token is listed before; a row without entries has div 0.  A row of
  * weight 0, or (with labels) without a token, is not in use: it is not read,
  * has div 0 and a zero gradient.  A row that holds nothing but -Inf adds
- * nothing.  A listed or given token whose own logit is -Inf adds what the
+ * nothing, whatever its list holds.  A listed or given token whose own logit is -Inf adds what the
  * formulas give (+Inf, where q > 0 and beta == 0), but its log probability does
  * not move: it has no derivative.  Where all tokens that are left to the
  * student are listed there is no rest, and its term is left out.  Factors
  * beyond fp32's range are held at its largest number.  NaN or +Inf among a
- * row's logits, or NaN among its values, makes its div, the sums and the row's
- * gradient NaN (where nothing is left beside the list, its listed places).  What
+ * row's logits makes its div, the sums and the row's gradient NaN (where nothing
+ * is left beside the list, its listed places); NaN among its values does the
+ * same but for the last two sums, in which values have no part.  What
  * is computed of a list is in fp64; sums over rows are taken in fp64 in a fixed order.
  *   id       device int32, entry i of row t at id[t * ld + i]; value the same,
  *            of `type` (SPARCML_F32 / BF16 / F16).  1 <= count <= SPARCML_MAX_TOP,

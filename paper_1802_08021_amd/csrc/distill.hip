@@ -193,7 +193,7 @@ __device__ __forceinline__ ListSums prepare_list(const DistillArgs& a, double sc
         s.off = (double)best * s.ts + ln64(s.Q);
         each = 1.0 / s.Q;
         s.QF *= each;
-        s.Q = 1.0;
+        s.Q = s.Q == s.Q ? 1.0 : s.Q;
     }
     const bool back = a.beta == 1.0f;  // (otherwise only beta == 0 has a use for these)
     for (uint32_t i = lane; i < a.count; i += 64)
@@ -255,6 +255,9 @@ __device__ __forceinline__ void finish_list(const DistillArgs& a, double scale, 
     if (a.rest && outside) out = share_of(a.beta, ln64(fmax(1.0 - s.Q, 0x1p-24)), far + part_ln(rest.sum) - all);
     div += out.div;
     F += out.f;
+    // (NaN among the values: a token that the student gives nothing hides it
+    // from every product, but not from Q)
+    if (s.Q != s.Q) div = F = s.Q;
     const double soft = 1.0 - (double)a.hard, hard = at != -INFINITY ? (double)a.hard : 0.0;
     const double k0 = (double)within((float)(weight * (double)a.grad_scale * scale));
     const double both = hard - soft * F;
@@ -558,8 +561,8 @@ k_distill_row(Logits in, DistillArgs a, float c, float* div, DistillTerms* terms
 
 // ---------------------------------------------------------------- gradient by slices
 
-// A factor of 0 takes an infinity away.
-__device__ __forceinline__ double weighed(double w, double x) { return w == 0.0 ? 0.0 : w * x; }
+// A factor of 0 takes an infinity away (not NaN).
+__device__ __forceinline__ double weighed(double w, double x) { return w == 0.0 && x == x ? 0.0 : w * x; }
 
 // The sums over rows, by one workgroup (fixed order).
 template <int U, class Load>
