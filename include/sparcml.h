@@ -694,8 +694,9 @@ SPARCML_API int sparcml_preference_loss(const sparcml_logits* in, int pairs, con
  * lse, log probability and norm[t][1] -Inf, norm[t][0] and entropy 0.  NaN or
  * +Inf among a row's logits makes its numbers NaN; the list then holds the
  * largest of the logits that are not NaN (a signalling NaN may hide others).
- * Sums are taken in fp32 over the differences to the maximum, both terms of the
- * entropy (log of the sum, mean difference) without cancellation.
+ * Sums are taken in fp32: where a row is sure of its token, entropy and log
+ * probability are off by some 10^-7, but no entropy is below 0, no log
+ * probability above.
  *   logp, lse, entropy  device float[rows] or NULL; norm float[rows][2] or NULL.
  *   top      0 <= top <= SPARCML_MAX_TOP, top <= vocab; top_id int32[rows][top]
  *            and top_logp float[rows][top], NULL only where top is 0.

@@ -5,8 +5,12 @@
 // With x the row's logits, M their maximum, s the inverse temperature, c = s
 // log2(e), d_v = c (x_v - M), Z = sum_v 2^d_v and U = sum_v -d_v 2^d_v: log
 // probabilities are ln 2 (d_v - log2 Z), the entropy is ln 2 (log2 Z + U / Z).
-// Both of its terms are positive, so nothing cancels.  U moves with the maximum
-// as Z does: from M to M' it becomes 2^-h (U + h Z), h = c (M' - M).
+// Neither of its terms is below 0, so they do not cancel each other.  U moves
+// with the maximum as Z does: from M to M' it becomes 2^-h (U + h Z), h = c (M' -
+// M).  Sums are taken against a whole number near c M and moved to it behind the
+// pass, where Z is held at 1 and U at 0: an entropy near 0 is off by some 10^-7
+// (up to 6e-7 at 3001 logits, however small it is), but not below 0, and no log
+// probability above.
 //
 // The n most likely tokens of a row: the pass over its logits leaves the largest
 // of each of up to 1024 groups of its lines (128 bytes; of up to 2048 groups of
@@ -127,7 +131,10 @@ struct Tally {
         const float b = wave_join<true>(sum == 0.0f ? 0.0f : f * (bend + h * sum));
         if (z == 0.0f) return ScorePart{high, 0.0f, 0.0f};
         const float off = __builtin_fmaf(-c, high, to), g = exp2_fast(off);
-        return ScorePart{high, z * g, g * __builtin_fmaf(-off, z, b)};
+        // (rounding leaves them a few 2^-24 off: the largest logit's own term is 1
+        // and 0; comparisons, as NaN has to stay)
+        const float Z = z * g, B = g * __builtin_fmaf(-off, z, b);
+        return ScorePart{high, Z < 1.0f ? 1.0f : Z, B < 0.0f ? 0.0f : B};
     }
 };
 
