@@ -773,7 +773,9 @@ SPARCML_API int sparcml_token_scores_grad(const sparcml_logits* in, const sparcm
  * row's logits makes its div, the sums and the row's gradient NaN (where nothing
  * is left beside the list, its listed places); NaN among its values does the
  * same but for the last two sums, in which values have no part.  What
- * is computed of a list is in fp64; sums over rows are taken in fp64 in a fixed order.
+ * is computed of a list is in fp64, from probabilities rounded to fp32, with
+ * logarithms within 10^-7 (so a div near 0 may lie that much below it); sums over
+ * rows are taken in fp64 in a fixed order.
  *   id       device int32, entry i of row t at id[t * ld + i]; value the same,
  *            of `type` (SPARCML_F32 / BF16 / F16).  1 <= count <= SPARCML_MAX_TOP,
  *            ld >= count.

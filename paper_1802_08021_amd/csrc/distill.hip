@@ -13,7 +13,8 @@
 // is right however small p_r is.
 //
 // A list's marks, a bit a token, lie in LDS while a row is summed; what is
-// computed of a list's entries is in fp64 (a few hundred a row).
+// computed of a list's entries is in fp64 (a few hundred a row), with logarithms
+// within 10^-7, and what is kept of each (q, e, its gradient) in fp32.
 #include "rows_device.h"
 
 #include <algorithm>
@@ -154,12 +155,15 @@ struct List {
     }
 };
 
-// Sums over a list: its largest logit (0: there is none), ln q = value ts - off,
-// Q = sum q, QF the same without tokens of -Inf, Z = sum e, and of the products
-// with logarithms those that beta needs (u against lq, w against scale (x - top)).
+// Sums over a list: its largest logit (-Inf: there is none), ln q = value ts - off,
+// Q = sum q, Z = sum e, and with the weights that beta needs (q, or e for beta 1),
+// as the list holds them in fp32, the products with logarithms (u against lq, w
+// against scale (x - top)) and the weights themselves without tokens of -Inf:
+// roundings of the weights then weigh differences of logarithms alone, which are
+// 0 where student and teacher agree.
 struct ListSums {
     float top;
-    double ts, off, Q, QF, Z, u, w;
+    double ts, off, Q, Z, u, w, mass;
 };
 __device__ __forceinline__ ListSums prepare_list(const DistillArgs& a, double scale, uint32_t V, List& list)
 {
@@ -182,17 +186,14 @@ __device__ __forceinline__ ListSums prepare_list(const DistillArgs& a, double sc
             list.q[i] = (float)q;
             list.e[i] = (float)e;
             s.Q += q;
-            s.QF += list.x[i] == -INFINITY ? 0.0 : q;
             s.Z += e;
         }
     s.Q = wave_sum(s.Q);
-    s.QF = wave_sum(s.QF);
     s.Z = wave_sum(s.Z);
     double each = 1.0;
     if (!a.rest && s.Q != 0.0) {
         s.off = (double)best * s.ts + ln64(s.Q);
         each = 1.0 / s.Q;
-        s.QF *= each;
         s.Q = s.Q == s.Q ? 1.0 : s.Q;
     }
     const bool back = a.beta == 1.0f;  // (otherwise only beta == 0 has a use for these)
@@ -202,9 +203,11 @@ __device__ __forceinline__ ListSums prepare_list(const DistillArgs& a, double sc
             list.q[i] = (float)q;
             s.u += product(p, (double)list.value[i] * s.ts - s.off);
             s.w += product(p, ((double)list.x[i] - (double)top) * scale);
+            s.mass += list.x[i] == -INFINITY ? 0.0 : p;
         }
     s.u = wave_sum(s.u);
     s.w = wave_sum(s.w);
+    s.mass = wave_sum(s.mass);
     return s;
 }
 
@@ -231,10 +234,10 @@ __device__ __forceinline__ void finish_list(const DistillArgs& a, double scale, 
     const double total = g * s.Z + h * (double)rest.sum, all = ln64(total), ln = all - step, one = g / total;
     double div, F;
     if (a.beta == 0.0f) {
-        div = s.u - s.w + ln * s.Q;
-        F = -s.QF;
+        div = s.u - s.w + ln * s.mass;  // (w takes a token of -Inf)
+        F = -s.mass;
     } else if (a.beta == 1.0f) {
-        div = F = one * (s.w - s.u - ln * s.Z);
+        div = F = one * (s.w - s.u - ln * s.mass);
     } else {
         div = F = 0.0;
         const double b = (double)a.beta;

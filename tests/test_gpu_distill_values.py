@@ -1,10 +1,11 @@
-"""Distillation: what a teacher's values may hold."""
+"""Distillation: what a teacher's values may hold, and a student that agrees
+with its teacher."""
 import numpy as np
 import pytest
 
 from gpu_util import say, torch_dev
 from test_gpu_distill import MODES, teacher
-from test_gpu_scores import make
+from test_gpu_scores import KINDS, make
 
 pytestmark = pytest.mark.gpu
 INF = np.inf
@@ -42,3 +43,23 @@ def test_nan_among_the_values_is_seen(T, V):
                 assert bool(bad[[0, 1, 3]].all()), bad.sum(1)[:4]
                 assert bool(bad[2, on[2]].all())
                 assert torch.equal(r["dlogits"][4:], good["dlogits"][4:])
+
+
+@pytest.mark.parametrize("T", [5, 200])
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_student_that_agrees_has_no_divergence(T, kind):
+    """The list is all there is, and the student's logits are its values: every
+    difference of logarithms is 0 but for fp64's rounding, 2^-52 of at most 60
+    for each of three sums over at most 256 tokens."""
+    from paper_1802_08021_amd import sparcml as S
+    torch, dev = torch_dev()
+    for V, K in ((300, 2), (5000, 64), (40001, 256)):
+        say(f"[agree] {T} {V} {K} {kind}")
+        x, _, gen = make(T, V, kind, K)
+        ids = torch.rand(T, V, device=dev, generator=gen).topk(K, 1)[1]
+        values = x.gather(1, ids).contiguous()
+        x.fill_(-INF)
+        x.scatter_(1, ids, values)
+        r = S.distill_loss(x, ids.int(), values, rest=False)
+        assert float(r["div"].abs().max()) <= 3 * 256 * 60 * 2.0**-52, r["div"]
+        assert bool((r["div"] == r["div"]).all())
