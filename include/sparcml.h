@@ -724,8 +724,9 @@ SPARCML_API int sparcml_token_scores(const sparcml_logits* in, const sparcml_sco
  * Rows that are not in use, rows of nothing but -Inf and rows whose derivatives
  * are all 0 have a zero gradient, whatever else they hold; a token whose own
  * logit is -Inf has no log probability that moves (its derivative is left out),
- * and no gradient.  Where norm is NaN all of the row's gradient is.  A derivative that is NULL is 0.  Entries of top_id outside
- * [0, vocab) are none; a token that is there twice counts twice.
+ * and no gradient.  Where norm is NaN all of the row's gradient is.  What p_v is
+ * multiplied with is held at 10^36, where the derivatives are finite.  A derivative that is NULL is 0.  Entries of
+ * top_id outside [0, vocab) are none; a token that is there twice counts twice.
  *   norm, entropy, top_id  as sparcml_token_scores wrote them for these logits
  *            and this scale (entropy only with d_entropy, top_id with d_top).
  *   d_logp, d_lse, d_entropy  device float[rows], d_top float[rows][top], or

@@ -749,6 +749,15 @@ k_lists(Logits in, ScoresOut o, uint32_t S, uint32_t W, float c, const ScorePart
 
 constexpr int kScoreGradU = 2;
 
+// Factors of the softmax, from derivatives that are finite, held where no product
+// with a logarithm (at least kNoShare, where 2^d is 0) leaves fp32: tokens without
+// probability, 0 times the factor, would have NaN.
+constexpr float kNoShare = -160.0f;
+__device__ __forceinline__ float held(double x)
+{
+    return (float)(fabs(x) > 1e36 && fabs(x) < INFINITY ? copysign(1e36, x) : x);
+}
+
 // The gradient of slice s of a row, W pieces: with p_v = 2^(d_v - log2 Z) the
 // softmax, s p_v (on - entropy' (ln p_v + H)) everywhere, and in the places of
 // the row's token and of its list their own derivatives beside it, stored once
@@ -826,12 +835,13 @@ k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits, ui
             if (LIST) __syncthreads();
             continue;
         }
-        const float l2 = ln * kLog2e, on = in.scale * (float)((double)d_lse - (double)one - total);
-        const float A = ENTROPY ? on - in.scale * d_h * a.entropy[t] : on;
-        const float B = ENTROPY ? -in.scale * d_h * 0.693147180559945309f : 0.0f;
+        const float l2 = ln * kLog2e;
+        const double scale = (double)in.scale, on = (double)d_lse - (double)one - total, h = (double)d_h;
+        const float A = held(scale * (ENTROPY ? on - h * (double)a.entropy[t] : on));
+        const float B = ENTROPY ? held(-scale * h * 0.693147180559945309) : 0.0f;
         auto entry_of = [&](float v) {
             const float d = (v - top) * c - l2, e = exp2_fast(d);
-            return ENTROPY ? e * __builtin_fmaf(B, fmaxf(d, -1e4f), A) : e * A;
+            return ENTROPY ? e * __builtin_fmaf(B, fmaxf(d, kNoShare), A) : e * A;
         };
         // (in place, the token and the list are read before any of it is written)
         __syncthreads();
