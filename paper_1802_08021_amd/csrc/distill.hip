@@ -779,7 +779,7 @@ hipError_t distill_run(const Logits& in0, const DistillArgs& a0, float* div, flo
     Logits in = in0;
     DistillArgs a = a0;
     const DistillCut cut = cut_distill(in.rows, in.vocab, in.type);
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     if (!cut.many) {
         const DistillSpace sp = carve_distill(ws, in.rows, in.rows, in.rows * cut.S, a.count, nullptr);
         const uint32_t slices = (uint32_t)std::min<uint64_t>(in.rows * (cut.S + 1), kDistillGrid);

@@ -678,7 +678,7 @@ template <bool GRAD, bool KEEP>
 void launch_row(const Cut& cut, Logits in, PolicyArgs a, float* logp, float* lse, const Space& sp, PolicyTerms* terms,
                 void* dlogits, uint64_t ldd, hipStream_t s)
 {
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     const uint64_t most = cut.pieces <= 1024 * kHold ? 512 : 1024;
     const uint64_t threads = std::max<uint64_t>(kMinThreads, (cut.pieces + kHold * 64 - 1) / (kHold * 64) * 64);
     const uint64_t rows = in.rows, size = in.type == kF32 ? 4 : 2;
@@ -723,7 +723,7 @@ template <bool KEEP>
 hipError_t rows_run(const Cut& cut, const Logits& in, const PolicyArgs* policy, const Space& sp, float* logp,
                     float* lse, hipStream_t s)
 {
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     const PolicyArgs a = policy ? *policy : PolicyArgs{};
     PolicyTerms* terms = policy ? sp.terms : nullptr;
     timer_begin(kTLossRows, s);
@@ -758,7 +758,7 @@ hipError_t logprob_run(const Logits& in, float* logp, float* lse, void* ws, hipS
     const uint32_t grid = (uint32_t)((in.rows * cut.g + 255) / 256);
     timer_begin(kTLossGrad, s);
     hipLaunchKernelGGL(k_join, dim3(grid), dim3(256), 0, s, in, (const float*)nullptr, cut.S, cut.g,
-                       in.scale * kLog2e, sp.part, sp.at_label, logp, lse);
+                       log2_scale(in.scale), sp.part, sp.at_label, logp, lse);
     timer_end(kTLossGrad, s);
     return hipGetLastError();
 }
@@ -768,7 +768,7 @@ hipError_t policy_run(const Logits& in, const PolicyArgs& a, float* logp, float*
 {
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
     const Space sp = carve(ws, Use::policy, in.rows, in.rows * cut.S, 0, nullptr);
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     const bool fused = dlogits && cut.many;
     if (fused) {
         timer_begin(kTLossRows, s);
@@ -806,7 +806,7 @@ hipError_t preference_run(const Logits& in, const PreferenceArgs& a, uint32_t pa
 {
     const Cut cut = cut_rows(in.rows, in.vocab, in.type);
     const Space sp = carve(ws, Use::preference, in.rows, in.rows * cut.S, pairs, nullptr);
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     // logits that fit the 256 MB cache are found there by the gradient pass (1000
     // rows of 131072 bf16: 132 -> 127 us; 4000 rows: 498 -> 522, so not those)
     const bool fits = in.rows * in.ld * (in.type == kF32 ? 4 : 2) <= (256u << 20);

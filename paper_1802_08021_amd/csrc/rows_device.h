@@ -11,6 +11,13 @@ namespace sparcml {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
+// c: the scale in powers of two, at most fp32's largest number (with an infinity
+// equal logits, a difference of 0, would be NaN apart).
+__host__ __device__ __forceinline__ float log2_scale(float scale)
+{
+    const float c = scale * kLog2e;
+    return c < 3.402823466e38f ? c : 3.402823466e38f;
+}
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -774,7 +774,7 @@ k_scores_grad(Logits in, ScoresGrad a, uint32_t S, uint32_t W, void* dlogits, ui
     __shared__ uint32_t s_id[LIST ? kMaxTop : 1], s_n[kWaves], s_some[kWaves], s_token;
     __shared__ float s_x[LIST ? kMaxTop : 1], s_g[LIST ? kMaxTop : 1];
     const uint32_t tid = threadIdx.x, V = (uint32_t)in.vocab;
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     for (uint64_t b = blockIdx.x; b < in.rows * S; b += gridDim.x) {
         const uint64_t t = b / S;
         const uint32_t s = (uint32_t)(b % S);
@@ -1006,7 +1006,7 @@ hipError_t scores_run(const Logits& in, const ScoresOut& o, void* ws, hipStream_
     const ScoreSpace sp = carve_scores(ws, in.rows * cut.S, in.rows * cut.S * cut.each, nullptr);
     const Groups groups = {sp.largest, cut.units, cut.each};
     const bool many = in.rows >= kManyLists;
-    const float c = in.scale * kLog2e;
+    const float c = log2_scale(in.scale);
     const uint32_t grid = (uint32_t)std::min<uint64_t>(in.rows * cut.S, kScoreGrid);
     const uint32_t rows = (uint32_t)std::min<uint64_t>(in.rows, kScoreGrid);
     timer_begin(kTScores, s);
