@@ -717,7 +717,11 @@ constexpr uint64_t kDistillSlices = 1024;   // of few rows together
 // tokens: 64 x 131072 30 us against 25 by slices and two launches, 128 x 131072
 // 30 against 38; 64 x 32000 16 against 15, 200 x 32000 17 against 24),
 constexpr uint64_t kDistillMany = 128;
-constexpr uint64_t kMarked = 5 * 32768;     // of at most so many logits (20 KB of marks)
+// of at most so many logits, 20 KB of marks.  (The two forms do not cross here: bf16
+// with 64 tokens 4096 x 163840 527 us against 1219 by slices, and with 32 KB of marks
+// 201088 661 against 1509, 262144 1000 against 1922, 128 x 200000 44 against 53; 512
+// x 170000 fp32 156 against 278.  Longer rows would gain by more room for marks.)
+constexpr uint64_t kMarked = 5 * 32768;
 constexpr uint64_t kDistillRows = 1u << 21; // of a launch with a workgroup a row (fewer than 2^32 threads)
 constexpr uint32_t kDistillHold = 8, kDistillHoldLds = 3;
 
